@@ -55,6 +55,10 @@ extern "C" {
 #define APPROXIFER_ERR_BAD_SIGN_MODE (-6)  /* sign_mode is neither 0 nor 1 */
 #define APPROXIFER_ERR_LAUNCH (-7)         /* the HIP runtime refused the launch */
 #define APPROXIFER_ERR_WORKSPACE_LIMIT (-8)/* approxifer_decode_byzantine_static(): the built-in workspace is too small */
+#define APPROXIFER_ERR_BAD_DTYPE (-9)      /* dtype is none of APPROXIFER_F32, APPROXIFER_F16, APPROXIFER_BF16 */
+#define APPROXIFER_ERR_ALIGNMENT (-10)     /* a pointer or stride is not aligned as the call asks */
+#define APPROXIFER_ERR_BAD_CACHE (-11)     /* sizes of a cache, of its sequences or of its heads that do not fit together */
+#define APPROXIFER_ERR_WORKSPACE (-12)     /* a call that cannot do without a workspace was given none, or too small a one */
 
 /* Decoder sign conventions, see approxifer_decode(). */
 #define APPROXIFER_SIGN_WORKER_INDEX 0
@@ -310,6 +314,174 @@ int approxifer_top1(const float *d_values, int32_t *d_top1, float *d_score, int6
  */
 int approxifer_wait_mask(const float *d_arrival, uint8_t *d_mask, int32_t *d_count,
                          int64_t G, int N, int wait_for, void *stream);
+
+/*
+ * Sequences kept by the workers.
+ *
+ * A hosted model that reads sequences keeps the keys and values of the tokens it has seen.  The code's weights sum to
+ * one (Section 3, "ApproxIFER Encoding"), so what all queries of a group have in common, a prompt for one, is coded
+ * into itself: its keys and values are computed once and shared by the N workers' sequences, which go apart with the
+ * first token that differs.  They therefore live in pages that sequences can share.
+ *
+ *   pool    [P][Hkv][page][Dh] of one dtype: P pages of `page` tokens for Hkv heads of Dh values.  A layer has two, one
+ *           of keys and one of values; page p is the same place in all of them.  16-byte aligned.
+ *   table   [B][M] int32: place t of sequence b lives in page table[b][t / page], slot t % page
+ *   lens    [B] int32: tokens of each sequence; a sequence holds its first ceil(lens / page) table entries, the
+ *           entries behind them mean nothing
+ *   refs    [P] int32: how many holders each page has, 0: free
+ *   starts  [B + 1] int32: the calls below work on T rows, one per NEW token; rows starts[b] .. starts[b + 1] - 1 are
+ *           the last tokens of sequence b.  With n of them, row i of the sequence is at place lens[b] - n + i.
+ *           Sequences without new tokens have n = 0.
+ *
+ * All sizes and indices that the device holds are checked there before they are used; what is wrong with a sequence
+ * is told in d_status [B] (int32, written, or NULL), and a bad sequence does not disturb the others:
+ *   APPROXIFER_GROUP_OK
+ *   APPROXIFER_SEQUENCE_BAD        its rows lie outside 0 .. T, or its length outside 0 .. M page: nothing is written
+ *   APPROXIFER_SEQUENCE_BAD_PAGE   a table entry that the call needs is not in 0 .. P - 1: see the calls
+ *   APPROXIFER_SEQUENCE_NO_PAGES, APPROXIFER_SEQUENCE_SHARED_PAGE   see the calls that take pages
+ *
+ * Sizes: page a power of two up to 4096; Dh a multiple of 8 up to 256; Hq a multiple of Hkv, Hq <= 1024; T up to 2^24, B up
+ * to 2^20, P and M page below 2^31 (pools may be larger than that), M and P at least 1.  APPROXIFER_ERR_BAD_CACHE,
+ * or APPROXIFER_ERR_LIMIT for sizes that are merely too large.
+ */
+#define APPROXIFER_F32 0
+#define APPROXIFER_F16 1
+#define APPROXIFER_BF16 2
+
+#define APPROXIFER_SEQUENCE_BAD 1
+#define APPROXIFER_SEQUENCE_BAD_PAGE 2
+#define APPROXIFER_SEQUENCE_NO_PAGES 3
+#define APPROXIFER_SEQUENCE_SHARED_PAGE 4
+
+#define APPROXIFER_MAX_HEAD_DIM 256
+#define APPROXIFER_MAX_HEADS 1024
+#define APPROXIFER_MAX_PAGE 4096
+#define APPROXIFER_MAX_AXES 4
+#define APPROXIFER_MAX_ROWS (1 << 24)
+#define APPROXIFER_MAX_SEQUENCES (1 << 20)
+
+typedef struct approxifer_sequences {   /* host memory, read before the call returns */
+    const int32_t *d_table;             /* [B][M] device */
+    const int32_t *d_lens;              /* [B] device */
+    const int32_t *d_starts;            /* [B + 1] device */
+    int64_t T, B, M, P;
+    int32_t page;
+} approxifer_sequences;
+
+/* Rotation frequencies h_freq[i] = base^(-i / pairs), i = 0..pairs-1, in radians per position (host memory, written).
+ * Returns OK, ERR_NULL_POINTER or ERR_BAD_SHAPE (pairs < 1, base not finite or not positive). */
+int approxifer_rotary_frequencies(int pairs, double base, double *h_freq);
+
+/*
+ * Appends the T new tokens to the cache: norm of every head of the queries and keys, rotation by position, and keys
+ * and values written into their pages, in one pass.  For one head's vector x of a token,
+ *     y = x w / sqrt(mean(x^2) + eps)      (w the weight; without one y = x)
+ *     angle_i = position[axis_i] freq_i,   i < pairs
+ *     (a, b) -> (a cos - b sin, a sin + b cos)   for (a, b) = (y_i, y_{i + pairs}), or (y_{2i}, y_{2i+1}) if interleaved;
+ * values of y behind the first 2 pairs stay as they are.
+ *
+ *   d_q [T][Hq][Dh], d_k, d_v [T][Hkv][Dh]   read only; a token's heads are contiguous, tokens q_stride, k_stride, v_stride
+ *                     values apart (so slices of one projection's output need no copy; any alignment, 16 bytes is fastest)
+ *   d_q_out           [T][Hq][Dh] written, contiguous, 16-byte aligned; may be d_q itself if that is contiguous
+ *   d_k_pool, d_v_pool   one layer's pools; the new tokens' slots are written, nothing else.  No two of the sequences
+ *                     may hold the page that a new token goes to (approxifer_cache_reserve() sees to it).
+ *   d_q_weight, d_k_weight   [Dh] of the same dtype, device, or NULL: no norm
+ *   d_positions       [T][axes] int32, device, or NULL: the token's place in its sequence (axes must be 1)
+ *   h_freq            [pairs] float64, host; h_axis [pairs] int32, host, 0 <= h_axis[i] < axes, or NULL: all 0
+ *   pairs             0 <= 2 pairs <= Dh;  1 <= axes <= APPROXIFER_MAX_AXES
+ * Angles are reduced in float64, norms and rotations computed in float32, each output rounded once.  A new token whose place
+ * is negative (more rows than the length) or whose page is bad is written to d_q_out, but not to the pools.
+ * The rows of a sequence that is APPROXIFER_SEQUENCE_BAD are not written at all.
+ * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE (pairs, axes, strides, eps), ERR_BAD_CACHE, ERR_LIMIT, ERR_BAD_DTYPE,
+ * ERR_BAD_NODES (a frequency that is not finite), ERR_ALIGNMENT or ERR_LAUNCH.
+ */
+int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype,
+                      const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride,
+                      void *d_q_out, void *d_k_pool, void *d_v_pool,
+                      const void *d_q_weight, const void *d_k_weight, double eps,
+                      const int32_t *d_positions, int axes, const double *h_freq, const int32_t *h_axis, int pairs,
+                      int interleaved, int32_t *d_status, void *stream);
+
+/*
+ * Attention of the T new tokens to what their sequences hold, themselves included (append first).  For the row at place t,
+ * query head h and the cache's head h / (Hq / Hkv),
+ *     out = sum_j softmax_j(scale q . k_j) v_j   over the visible places j <= t:
+ *           all of them if window = 0, else those with j > t - window or j < sinks.
+ * A row that sees nothing (its place is negative) gets zeros.  What a row does not see has no effect on it, whatever it
+ * holds (infinities and NaN included); what lies behind a sequence's length is never read.
+ *
+ *   d_q     [T][Hq][Dh], tokens q_stride values apart, read only;  d_out [T][Hq][Dh] written, contiguous, 16-byte aligned,
+ *           must not overlap d_q
+ *   max_rows, max_len   bounds of the sequences' numbers of new tokens and lengths: a sequence beyond one is
+ *           APPROXIFER_SEQUENCE_BAD.  The work is laid out for them, so close bounds are faster.
+ *   window >= 0, sinks >= 0, scale finite
+ *   d_workspace, workspace_bytes   scratch of the caller's, 16-byte aligned, or NULL / 0, as for
+ *           approxifer_decode_byzantine(): long sequences with few rows are split over the GPU, and the parts meet there.
+ *           approxifer_attend_workspace_bytes() gives the size with which the call is fastest; with less it is split
+ *           less, and as correct.
+ * Rows that see a place in a bad page are NaN.  Scores, softmax and sums are float32 (for 16-bit types the weights are
+ * rounded to the type before they multiply the values); each output is rounded once.
+ * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE, ERR_BAD_CACHE, ERR_LIMIT, ERR_BAD_DTYPE, ERR_ALIGNMENT or ERR_LAUNCH; the
+ * call may consist of two launches.
+ */
+int approxifer_attend(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype,
+                      const void *d_q, int64_t q_stride, const void *d_k_pool, const void *d_v_pool, void *d_out,
+                      int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks, double scale,
+                      int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream);
+size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows,
+                                         int64_t max_len, int64_t window, int64_t sinks);
+
+/*
+ * Room for d_add[b] >= 0 more tokens of every sequence: lens[b] += add[b], and the pages this takes are the free ones of
+ * lowest index, given out in the order of the sequences; their refs become 1.  All in place.
+ *   APPROXIFER_SEQUENCE_SHARED_PAGE   the sequence's last page is not full and has another holder: fork the sequence first
+ *   APPROXIFER_SEQUENCE_NO_PAGES      the free pages end before this sequence; later ones that want any end so too
+ *   APPROXIFER_SEQUENCE_BAD           add[b] < 0, lens[b] < 0, or more tokens than M page
+ *   APPROXIFER_SEQUENCE_BAD_PAGE      the last page, which is not full, is not in 0 .. P - 1
+ * A sequence with any of these stays as it is; it takes no pages (one without free pages keeps those behind it
+ * from taking any).  The same holders are seen by all calls: several calls of one cache must not overlap.
+ * Returns OK, ERR_NULL_POINTER, ERR_BAD_CACHE, ERR_LIMIT or ERR_LAUNCH.
+ */
+int approxifer_cache_reserve(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, const int32_t *d_add, int32_t *d_status,
+                             int64_t B, int64_t M, int64_t P, int page, void *stream);
+
+/*
+ * New sequences out of old ones: forks, reorders, shortens and ends sequences.  New sequence i (0 <= i < B_out) continues
+ * old sequence d_parents[i], all of it or its first d_keep[i] tokens; d_parents[i] = -1 is an empty sequence, and an old
+ * sequence that nobody continues gives its pages back.  Full pages are shared.  A last page that is not full is taken over if
+ * no other holder is left and i is the first to want it, else its copy is the free page of lowest index, in the order of i:
+ * `page_bytes` bytes of each of the `planes` pools [planes][P][page_bytes] are copied.
+ * d_refs_out = d_refs - what the old sequences held + what the new ones hold: holders that are no sequence stay counted.
+ *   d_keep      [B_out] int32, device, or NULL: as many tokens as there are
+ *   d_table_out [B_out][M], d_lens_out [B_out], d_refs_out [P]  written; must not overlap the inputs.  Entries of d_table_out
+ *               behind a sequence's pages are -1.
+ *   d_pools     16-byte aligned, page_bytes a multiple of 16; may be NULL with planes = 0
+ *   d_status    [B_out]: APPROXIFER_SEQUENCE_BAD (parent outside -1 .. B - 1, keep < 0, or a parent's length outside 0 .. M page),
+ *               APPROXIFER_SEQUENCE_BAD_PAGE (of the parent), APPROXIFER_SEQUENCE_NO_PAGES: the new sequence is empty
+ *   d_workspace at least approxifer_cache_workspace_bytes(B, B_out, P) bytes, 16-byte aligned
+ * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE (planes, page_bytes), ERR_BAD_CACHE, ERR_LIMIT, ERR_ALIGNMENT, ERR_WORKSPACE or
+ * ERR_LAUNCH; the call consists of several launches.
+ */
+int approxifer_cache_fork(const int32_t *d_table, const int32_t *d_lens, const int32_t *d_refs, const int32_t *d_parents,
+                          const int32_t *d_keep, int32_t *d_table_out, int32_t *d_lens_out, int32_t *d_refs_out,
+                          int32_t *d_status, void *d_pools, int64_t planes, int64_t page_bytes, int64_t B, int64_t B_out,
+                          int64_t M, int64_t P, int page, void *d_workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Moves the live pages together: with L of them, the ones at L and above go to the free places below L, both in ascending
+ * order, in all pools; d_table and d_refs follow, in place.  Afterwards pages 0 .. L - 1 are live, the others free.
+ *   d_moved     [P] int32, written: where each page that was live is now, -1 for the others (for holders that are no
+ *               sequence)
+ *   d_live      [1] int32, written: L
+ *   others as approxifer_cache_fork().  Table entries that are no live page stay as they are.
+ */
+int approxifer_cache_compact(int32_t *d_table, const int32_t *d_lens, int32_t *d_refs, int32_t *d_moved, int32_t *d_live,
+                             void *d_pools, int64_t planes, int64_t page_bytes, int64_t B, int64_t M, int64_t P, int page,
+                             void *d_workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace that approxifer_cache_fork() (with B_out new sequences) and approxifer_cache_compact() need; 0 for sizes
+ * that they refuse.  Host arithmetic only. */
+size_t approxifer_cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P);
 
 /* Text for a return code; never NULL.  The string is static. */
 const char *approxifer_strerror(int code);

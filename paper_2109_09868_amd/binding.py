@@ -24,6 +24,8 @@ MAX_AVAIL_BYZ = 64
 SIGN_WORKER_INDEX = 0
 SIGN_SURVIVOR_RANK = 1
 S_FROM_MASK = -1
+F32, F16, BF16 = 0, 1, 2
+SEQUENCE_OK, SEQUENCE_BAD, SEQUENCE_BAD_PAGE, SEQUENCE_NO_PAGES, SEQUENCE_SHARED_PAGE = range(5)
 
 EXPORTS = (
     "approxifer_version",
@@ -41,7 +43,23 @@ EXPORTS = (
     "approxifer_group_count",
     "approxifer_pad_last_group",
     "approxifer_top1",
+    "approxifer_rotary_frequencies",
+    "approxifer_append",
+    "approxifer_attend",
+    "approxifer_attend_workspace_bytes",
+    "approxifer_cache_reserve",
+    "approxifer_cache_fork",
+    "approxifer_cache_compact",
+    "approxifer_cache_workspace_bytes",
 )
+
+
+class _Sequences(ctypes.Structure):
+    """approxifer_sequences."""
+    _fields_ = [("d_table", ctypes.c_void_p), ("d_lens", ctypes.c_void_p), ("d_starts", ctypes.c_void_p),
+                ("T", ctypes.c_int64), ("B", ctypes.c_int64), ("M", ctypes.c_int64), ("P", ctypes.c_int64),
+                ("page", ctypes.c_int32)]
+
 
 _lib = None
 
@@ -103,6 +121,24 @@ def load() -> ctypes.CDLL:
     lib.approxifer_decode_byzantine_homogeneous.argtypes = lib.approxifer_decode_byzantine.argtypes
     lib.approxifer_wait_mask.restype = ctypes.c_int
     lib.approxifer_wait_mask.argtypes = [vp, vp, vp, ctypes.c_int64, ctypes.c_int, ctypes.c_int, vp]
+    i, q, f, z = ctypes.c_int, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
+    seq = ctypes.POINTER(_Sequences)
+    lib.approxifer_rotary_frequencies.restype = i
+    lib.approxifer_rotary_frequencies.argtypes = [i, f, c_dp]
+    lib.approxifer_append.restype = i
+    lib.approxifer_append.argtypes = [seq, i, i, i, i, vp, q, vp, q, vp, q, vp, vp, vp, vp, vp, f, vp, i, c_dp, vp, i, i, vp, vp]
+    lib.approxifer_attend.restype = i
+    lib.approxifer_attend.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, q, q, q, q, f, vp, vp, z, vp]
+    lib.approxifer_attend_workspace_bytes.restype = z
+    lib.approxifer_attend_workspace_bytes.argtypes = [q, q, i, i, i, i, q, q, q, q]
+    lib.approxifer_cache_reserve.restype = i
+    lib.approxifer_cache_reserve.argtypes = [vp, vp, vp, vp, vp, q, q, q, i, vp]
+    lib.approxifer_cache_fork.restype = i
+    lib.approxifer_cache_fork.argtypes = [vp] * 10 + [q] * 6 + [i, vp, z, vp]
+    lib.approxifer_cache_compact.restype = i
+    lib.approxifer_cache_compact.argtypes = [vp] * 6 + [q] * 5 + [i, vp, z, vp]
+    lib.approxifer_cache_workspace_bytes.restype = z
+    lib.approxifer_cache_workspace_bytes.argtypes = [q, q, q]
     _lib = lib
     return lib
 
@@ -460,3 +496,212 @@ def approxifer_wait_mask(arrival, wait_for, mask=None, count=None, stream=None):
                                          _dev(count, torch.int32, (G,)), G, N, int(wait_for),
                                          _stream_handle(stream)))
     return mask, count
+
+
+# ---- sequences in pages -------------------------------------------------------------------------------------------------
+def approxifer_rotary_frequencies(pairs: int, base: float = 10000.0):
+    """float64 numpy array [pairs]: base ** (-i / pairs), radians per position."""
+    freq = np.empty(max(int(pairs), 0), dtype=np.float64)
+    _check(load().approxifer_rotary_frequencies(int(pairs), float(base), freq.ctypes.data_as(ctypes.POINTER(ctypes.c_double))))
+    return freq
+
+
+def _dtype_code(dtype) -> int:
+    import torch
+    codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    if dtype not in codes:
+        raise TypeError("expected float32, float16 or bfloat16, got %s" % dtype)
+    return codes[dtype]
+
+
+def _rows(t, dtype):
+    """(address, elements between tokens) of a [T, heads, Dh] device tensor whose tokens are contiguous, at any distance."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("expected a tensor in device memory")
+    if t.dtype != dtype or t.dim() != 3:
+        raise TypeError("expected a %s tensor of three dimensions, got %s of %d" % (dtype, t.dtype, t.dim()))
+    T, H, D = t.shape
+    if T and ((D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D)):
+        raise TypeError("the heads of a token must be contiguous")
+    return t.data_ptr(), t.stride(0) if T > 1 else H * D
+
+
+def _pools(k_pool, v_pool, dtype, kv=None, Dh=None):
+    import torch
+    if not isinstance(k_pool, torch.Tensor) or k_pool.dim() != 4:
+        raise TypeError("a pool is a tensor [P, Hkv, page, Dh]")
+    if (kv is not None and k_pool.shape[1] != kv) or (Dh is not None and k_pool.shape[3] != Dh):
+        raise ValueError("the pool's heads do not fit: %s" % (tuple(k_pool.shape),))
+    return _dev(k_pool, dtype), _dev(v_pool, dtype, k_pool.shape)
+
+
+def _sequences(table, lens, starts, T, pool):
+    import torch
+    B, M = table.shape
+    return _Sequences(_dev(table, torch.int32), _dev(lens, torch.int32, (B,)), _dev(starts, torch.int32, (B + 1,)), T, B, M,
+                      pool.shape[0], pool.shape[2])
+
+
+def approxifer_append(q, k, v, k_pool, v_pool, table, lens, starts, freq, q_weight=None, k_weight=None, eps=1e-6, positions=None,
+                      axis=None, interleaved=False, q_out=None, status=None, stream=None):
+    """Norms (with q_weight, k_weight [Dh]) and rotates the heads of T new tokens' queries and keys and writes keys and values
+    into their pages.  q [T, Hq, Dh], k and v [T, Hkv, Dh] (slices of one projection's output will do), pools [P, Hkv, page,
+    Dh], table [B, M], lens [B] and starts [B + 1] int32, freq [pairs] float64 on the host; positions [T, axes] int32 and
+    axis [pairs] int32 on the host, or None: places in the sequence.  Returns (q_out [T, Hq, Dh], status [B] int32)."""
+    import torch
+    dtype = k_pool.dtype
+    code = _dtype_code(dtype)
+    T, Hq, Dh = q.shape
+    Hkv = k_pool.shape[1]
+    if tuple(k.shape) != (T, Hkv, Dh) or tuple(v.shape) != (T, Hkv, Dh):
+        raise ValueError("k and v must be [T, Hkv, Dh] = %s" % ((T, Hkv, Dh),))
+    kp, vp = _pools(k_pool, v_pool, dtype, Hkv, Dh)
+    qp, q_stride = _rows(q, dtype)
+    kk, k_stride = _rows(k, dtype)
+    vv, v_stride = _rows(v, dtype)
+    if q_out is None:
+        q_out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+    if status is None:
+        status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
+    seq = _sequences(table, lens, starts, T, k_pool)
+    pairs, fp = _nodes(freq)
+    axes = 1
+    if positions is not None:
+        axes = positions.shape[1] if positions.dim() == 2 else 1
+    ap = None
+    if axis is not None:
+        a = np.ascontiguousarray(axis, dtype=np.int32)
+        if a.shape != (pairs,):
+            raise ValueError("axis must have one entry for each frequency")
+        ap = a.tobytes()
+    _check(_entry().approxifer_append(
+        ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kk, k_stride, vv, v_stride, _dev(q_out, dtype, (T, Hq, Dh)), kp, vp,
+        _dev(q_weight, dtype, (Dh,)) if q_weight is not None else None,
+        _dev(k_weight, dtype, (Dh,)) if k_weight is not None else None, float(eps),
+        _dev(positions, torch.int32, (T, axes) if positions.dim() == 2 else (T,)) if positions is not None else None, axes, fp, ap,
+        pairs, int(bool(interleaved)), _dev(status, torch.int32, (table.shape[0],)), _stream_handle(stream)))
+    return q_out, status
+
+
+def approxifer_attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window=0, sinks=0) -> int:
+    """Bytes of scratch memory with which approxifer_attend is fastest (0: none); dtype a torch dtype."""
+    return int(load().approxifer_attend_workspace_bytes(int(T), int(B), int(Hq), int(Hkv), int(Dh), _dtype_code(dtype), int(max_rows),
+                                                        int(max_len), int(window), int(sinks)))
+
+
+def _scratch(workspace):
+    import torch
+    if workspace is NO_WORKSPACE:
+        return None, 0
+    if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or not workspace.is_contiguous():
+        raise TypeError("workspace must be a contiguous tensor in device memory")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len, window=0, sinks=0, scale=None, out=None,
+                      status=None, workspace=None, stream=None):
+    """Causal attention of T new tokens (already appended) to their sequences: q [T, Hq, Dh], the rest as approxifer_append;
+    max_rows and max_len bound the sequences' new tokens and lengths.  window (0: none) and sinks limit what a token sees,
+    scale defaults to Dh ** -0.5.  workspace as approxifer_decode_byzantine's, of approxifer_attend_workspace_bytes().
+    Returns (out [T, Hq, Dh], status [B] int32)."""
+    import torch
+    dtype = k_pool.dtype
+    code = _dtype_code(dtype)
+    T, Hq, Dh = q.shape
+    Hkv = k_pool.shape[1]
+    kp, vp = _pools(k_pool, v_pool, dtype, None, Dh)
+    qp, q_stride = _rows(q, dtype)
+    if out is None:
+        out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+    if status is None:
+        status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
+    if workspace is None:
+        need = approxifer_attend_workspace_bytes(T, table.shape[0], Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else NO_WORKSPACE
+    ws_ptr, ws_bytes = _scratch(workspace)
+    seq = _sequences(table, lens, starts, T, k_pool)
+    _check(_entry().approxifer_attend(
+        ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kp, vp, _dev(out, dtype, (T, Hq, Dh)), int(max_rows), int(max_len),
+        int(window), int(sinks), Dh ** -0.5 if scale is None else float(scale), _dev(status, torch.int32, (table.shape[0],)), ws_ptr,
+        ws_bytes, _stream_handle(stream)))
+    return out, status
+
+
+def approxifer_cache_reserve(table, lens, refs, add, page, status=None, stream=None):
+    """Room for add[b] more tokens of every sequence, in place: table [B, M], lens [B], refs [P], add [B] int32.
+    Returns status [B] int32."""
+    import torch
+    B, M = table.shape
+    if status is None:
+        status = torch.full((B,), -1, dtype=torch.int32, device=table.device)
+    _check(_entry().approxifer_cache_reserve(_dev(table, torch.int32), _dev(lens, torch.int32, (B,)), _dev(refs, torch.int32),
+                                             _dev(add, torch.int32, (B,)), _dev(status, torch.int32, (B,)), B, M, refs.numel(),
+                                             int(page), _stream_handle(stream)))
+    return status
+
+
+def approxifer_cache_workspace_bytes(B: int, B_out: int, P: int) -> int:
+    """Bytes of scratch memory that approxifer_cache_fork and approxifer_cache_compact need."""
+    return int(load().approxifer_cache_workspace_bytes(int(B), int(B_out), int(P)))
+
+
+def _planes(pools, P):
+    """(address, planes, bytes of a page, tokens of a page) of pools [.., P, Hkv, page, Dh]."""
+    import torch
+    if not isinstance(pools, torch.Tensor) or not pools.is_cuda or not pools.is_contiguous() or pools.dim() < 4:
+        raise TypeError("pools must be a contiguous tensor [.., P, Hkv, page, Dh] in device memory")
+    if pools.shape[-4] != P:
+        raise ValueError("the pools have %d pages, refs %d" % (pools.shape[-4], P))
+    page_bytes = pools.shape[-3] * pools.shape[-2] * pools.shape[-1] * pools.element_size()
+    return pools.data_ptr(), pools.shape[:-4].numel(), page_bytes, pools.shape[-2]
+
+
+def approxifer_cache_fork(pools, table, lens, refs, parents, keep=None, table_out=None, lens_out=None, refs_out=None, status=None,
+                          workspace=None, stream=None):
+    """New sequences out of old ones: sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens.
+    pools [.., P, Hkv, page, Dh] hold all layers' keys and values; table [B, M], lens [B], refs [P], parents and keep [B_out]
+    int32.  Returns (table_out [B_out, M], lens_out [B_out], refs_out [P], status [B_out])."""
+    import torch
+    i32 = torch.int32
+    B, M = table.shape
+    P, n = refs.numel(), parents.numel()
+    at, planes, page_bytes, page = _planes(pools, P)
+    if table_out is None:
+        table_out = torch.empty((n, M), dtype=i32, device=table.device)
+    if lens_out is None:
+        lens_out = torch.empty((n,), dtype=i32, device=table.device)
+    if refs_out is None:
+        refs_out = torch.empty((P,), dtype=i32, device=table.device)
+    if status is None:
+        status = torch.full((n,), -1, dtype=i32, device=table.device)
+    if workspace is None:
+        workspace = torch.empty((approxifer_cache_workspace_bytes(B, n, P),), dtype=torch.uint8, device=table.device)
+    ws_ptr, ws_bytes = _scratch(workspace)
+    _check(_entry().approxifer_cache_fork(
+        _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(parents, i32, (n,)),
+        _dev(keep, i32, (n,)) if keep is not None else None, _dev(table_out, i32, (n, M)), _dev(lens_out, i32, (n,)),
+        _dev(refs_out, i32, (P,)), _dev(status, i32, (n,)), at, planes, page_bytes, B, n, M, P, page, ws_ptr, ws_bytes,
+        _stream_handle(stream)))
+    return table_out, lens_out, refs_out, status
+
+
+def approxifer_cache_compact(pools, table, lens, refs, moved=None, live=None, workspace=None, stream=None):
+    """Moves the live pages of all pools together, in place; table and refs follow.  Returns (moved [P] int32: where each page
+    is now, -1 for free ones; live [1] int32)."""
+    import torch
+    i32 = torch.int32
+    B, M = table.shape
+    P = refs.numel()
+    at, planes, page_bytes, page = _planes(pools, P)
+    if moved is None:
+        moved = torch.empty((P,), dtype=i32, device=table.device)
+    if live is None:
+        live = torch.empty((1,), dtype=i32, device=table.device)
+    if workspace is None:
+        workspace = torch.empty((approxifer_cache_workspace_bytes(B, B, P),), dtype=torch.uint8, device=table.device)
+    ws_ptr, ws_bytes = _scratch(workspace)
+    _check(_entry().approxifer_cache_compact(
+        _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(moved, i32, (P,)), _dev(live, i32, (1,)), at, planes,
+        page_bytes, B, M, P, page, ws_ptr, ws_bytes, _stream_handle(stream)))
+    return moved, live

@@ -2,7 +2,7 @@
 // launch on the caller's stream.  See include/approxifer.h for the contract.
 #include <cmath>
 
-#include "common.h"
+#include "sequences.h"
 
 using approxifer::Nodes;
 
@@ -39,11 +39,49 @@ int check_common(int K, int N, const double *h_alpha, const double *h_beta, Node
     return APPROXIFER_OK;
 }
 
+// Sizes of a cache; *shift: log2 of the page.
+int check_cache(int64_t B, int64_t M, int64_t P, int page, int *shift) {
+    if (B < 0 || M < 1 || P < 1 || page < 1 || (page & (page - 1)) != 0) return APPROXIFER_ERR_BAD_CACHE;
+    if (page > APPROXIFER_MAX_PAGE || B > APPROXIFER_MAX_SEQUENCES || P > 0x7fffffffLL || M > 0x7fffffffLL / page)
+        return APPROXIFER_ERR_LIMIT;
+    *shift = __builtin_ctz(static_cast<unsigned>(page));
+    return APPROXIFER_OK;
+}
+
+bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+int check_sequences(const approxifer_sequences *h, int Hq, int Hkv, int Dh, int dtype, approxifer::Sequences *s) {
+    if (h == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    if (h->T < 0 || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 || Dh < 1 || Dh % 8 != 0) return APPROXIFER_ERR_BAD_CACHE;
+    if (dtype != APPROXIFER_F32 && dtype != APPROXIFER_F16 && dtype != APPROXIFER_BF16) return APPROXIFER_ERR_BAD_DTYPE;
+    int shift = 0;
+    const int rc = check_cache(h->B, h->M, h->P, h->page, &shift);
+    if (rc != APPROXIFER_OK) return rc;
+    if (h->T > APPROXIFER_MAX_ROWS || Hq > APPROXIFER_MAX_HEADS || Dh > APPROXIFER_MAX_HEAD_DIM) return APPROXIFER_ERR_LIMIT;
+    *s = approxifer::Sequences{h->d_table, h->d_lens, h->d_starts, h->T, static_cast<int>(h->B), static_cast<int>(h->M),
+                               static_cast<int>(h->P), shift};
+    return APPROXIFER_OK;
+}
+
+// Rows of `values` elements, `stride` elements apart: whether they can be read element by element.
+int check_rows(const void *p, int64_t stride, int64_t values, int dtype) {
+    if (stride < values || stride > (1LL << 31)) return APPROXIFER_ERR_BAD_SHAPE;
+    return aligned(p, dtype == APPROXIFER_F32 ? 4 : 2) ? APPROXIFER_OK : APPROXIFER_ERR_ALIGNMENT;
+}
+
+int check_pools(const void *d_pools, int64_t planes, int64_t page_bytes, int64_t P) {
+    if (planes < 0 || page_bytes < 0) return APPROXIFER_ERR_BAD_SHAPE;
+    if (planes == 0 || page_bytes == 0) return APPROXIFER_OK;
+    if (planes > (1 << 20) || page_bytes > (1LL << 31) || P * page_bytes > (1LL << 48) / planes) return APPROXIFER_ERR_LIMIT;
+    if (d_pools == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    return aligned(d_pools, 16) && page_bytes % 16 == 0 ? APPROXIFER_OK : APPROXIFER_ERR_ALIGNMENT;
+}
+
 }  // namespace
 
 extern "C" {
 
-int approxifer_version(void) { return 300; }   // 0.3.0: workspace arguments of the Byzantine decoders
+int approxifer_version(void) { return 400; }   // 0.4.0: sequences in pages
 
 const char *approxifer_strerror(int code) {
     switch (code) {
@@ -58,6 +96,12 @@ const char *approxifer_strerror(int code) {
         case APPROXIFER_ERR_WORKSPACE_LIMIT:
             return "the shape needs more scratch memory than the built-in workspace holds (APPROXIFER_STATIC_WORKSPACE_BYTES); "
                    "use approxifer_decode_byzantine with a workspace of approxifer_workspace_bytes()";
+        case APPROXIFER_ERR_BAD_DTYPE: return "dtype must be APPROXIFER_F32, APPROXIFER_F16 or APPROXIFER_BF16";
+        case APPROXIFER_ERR_ALIGNMENT: return "pools, outputs and workspaces must be 16-byte aligned, rows aligned to their type";
+        case APPROXIFER_ERR_BAD_CACHE:
+            return "bad cache: need T, B >= 0, M, P >= 1, a page that is a power of two, Dh a positive multiple of 8, Hq a positive "
+                   "multiple of Hkv";
+        case APPROXIFER_ERR_WORKSPACE: return "the call needs a workspace of approxifer_cache_workspace_bytes()";
         default: return "unknown approxifer error code";
     }
 }
@@ -226,6 +270,147 @@ int approxifer_wait_mask(const float *d_arrival, uint8_t *d_mask, int32_t *d_cou
     if (G == 0) return APPROXIFER_OK;
     if (d_arrival == nullptr || d_mask == nullptr) return APPROXIFER_ERR_NULL_POINTER;
     return approxifer::launch_wait_mask(d_arrival, d_mask, d_count, G, N, wait_for, static_cast<hipStream_t>(stream));
+}
+
+int approxifer_rotary_frequencies(int pairs, double base, double *h_freq) {
+    if (h_freq == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    if (pairs < 1 || !std::isfinite(base) || base <= 0.0) return APPROXIFER_ERR_BAD_SHAPE;
+    for (int i = 0; i < pairs; ++i) h_freq[i] = std::pow(base, -static_cast<double>(i) / pairs);
+    return APPROXIFER_OK;
+}
+
+int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,
+                      const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride, void *d_q_out, void *d_k_pool,
+                      void *d_v_pool, const void *d_q_weight, const void *d_k_weight, double eps, const int32_t *d_positions,
+                      int axes, const double *h_freq, const int32_t *h_axis, int pairs, int interleaved, int32_t *d_status,
+                      void *stream) {
+    approxifer::Sequences s;
+    int rc = check_sequences(h_seq, Hq, Hkv, Dh, dtype, &s);
+    if (rc != APPROXIFER_OK) return rc;
+    if (pairs < 0 || 2 * static_cast<int64_t>(pairs) > Dh || axes < 1 || (d_positions == nullptr && axes != 1) || !std::isfinite(eps) ||
+        eps < 0.0)
+        return APPROXIFER_ERR_BAD_SHAPE;
+    if (axes > APPROXIFER_MAX_AXES) return APPROXIFER_ERR_LIMIT;
+    if (pairs > 0 && h_freq == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    for (int i = 0; i < pairs; ++i) {
+        if (!std::isfinite(h_freq[i])) return APPROXIFER_ERR_BAD_NODES;
+        if (h_axis != nullptr && (h_axis[i] < 0 || h_axis[i] >= axes)) return APPROXIFER_ERR_BAD_SHAPE;
+    }
+    if (s.B == 0 && s.T > 0) return APPROXIFER_ERR_BAD_CACHE;
+    if (s.B == 0) return APPROXIFER_OK;
+    if (s.table == nullptr || s.lens == nullptr || s.starts == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    if (s.T == 0 && d_status == nullptr) return APPROXIFER_OK;
+    if (s.T > 0) {
+        if (d_q == nullptr || d_k == nullptr || d_v == nullptr || d_q_out == nullptr || d_k_pool == nullptr || d_v_pool == nullptr)
+            return APPROXIFER_ERR_NULL_POINTER;
+        if ((rc = check_rows(d_q, q_stride, static_cast<int64_t>(Hq) * Dh, dtype)) != APPROXIFER_OK ||
+            (rc = check_rows(d_k, k_stride, static_cast<int64_t>(Hkv) * Dh, dtype)) != APPROXIFER_OK ||
+            (rc = check_rows(d_v, v_stride, static_cast<int64_t>(Hkv) * Dh, dtype)) != APPROXIFER_OK)
+            return rc;
+        if (!aligned(d_q_out, 16) || !aligned(d_k_pool, 16) || !aligned(d_v_pool, 16) || !aligned(d_q_weight, dtype == APPROXIFER_F32 ? 4 : 2) ||
+            !aligned(d_k_weight, dtype == APPROXIFER_F32 ? 4 : 2))
+            return APPROXIFER_ERR_ALIGNMENT;
+    }
+    return approxifer::launch_append(s, Hq, Hkv, Dh, dtype, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_q_out, d_k_pool, d_v_pool,
+                                     d_q_weight, d_k_weight, eps, d_positions, axes, h_freq, h_axis, pairs, interleaved != 0, d_status,
+                                     static_cast<hipStream_t>(stream));
+}
+
+int approxifer_attend(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,
+                      const void *d_k_pool, const void *d_v_pool, void *d_out, int64_t max_rows, int64_t max_len, int64_t window,
+                      int64_t sinks, double scale, int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream) {
+    approxifer::AttendCall c;
+    int rc = check_sequences(h_seq, Hq, Hkv, Dh, dtype, &c.seq);
+    if (rc != APPROXIFER_OK) return rc;
+    if (max_rows < 0 || max_len < 0 || window < 0 || sinks < 0 || !std::isfinite(scale)) return APPROXIFER_ERR_BAD_SHAPE;
+    if (c.seq.B == 0 && c.seq.T > 0) return APPROXIFER_ERR_BAD_CACHE;
+    if (c.seq.B == 0) return APPROXIFER_OK;
+    if (c.seq.table == nullptr || c.seq.lens == nullptr || c.seq.starts == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    if (c.seq.T == 0 && d_status == nullptr) return APPROXIFER_OK;
+    if (c.seq.T > 0) {
+        if (d_q == nullptr || d_k_pool == nullptr || d_v_pool == nullptr || d_out == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+        if ((rc = check_rows(d_q, q_stride, static_cast<int64_t>(Hq) * Dh, dtype)) != APPROXIFER_OK) return rc;
+        if (!aligned(d_out, 16) || !aligned(d_k_pool, 16) || !aligned(d_v_pool, 16)) return APPROXIFER_ERR_ALIGNMENT;
+        if (d_workspace != nullptr && !aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
+    }
+    const int64_t most = h_seq->M * h_seq->page;              // no sequence is longer, no window reaches further
+    c.Hq = Hq;
+    c.Hkv = Hkv;
+    c.Dh = Dh;
+    c.dtype = dtype;
+    c.q = d_q;
+    c.q_stride = q_stride;
+    c.k_pool = d_k_pool;
+    c.v_pool = d_v_pool;
+    c.out = d_out;
+    c.status = d_status;
+    c.max_rows = static_cast<int>(max_rows < c.seq.T ? max_rows : c.seq.T);
+    c.max_len = static_cast<int>(max_len < most ? max_len : most);
+    c.window = static_cast<int>(window < most ? window : 0);
+    c.sinks = c.window == 0 ? 0 : static_cast<int>(sinks < most ? sinks : most);
+    c.scale = static_cast<float>(scale);
+    return approxifer::launch_attend(c, d_workspace, d_workspace != nullptr ? workspace_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
+size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                                         int64_t window, int64_t sinks) {
+    if (T < 1 || T > APPROXIFER_MAX_ROWS || B < 1 || B > APPROXIFER_MAX_SEQUENCES || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 ||
+        Hq > APPROXIFER_MAX_HEADS || Dh < 1 || Dh % 8 != 0 || Dh > APPROXIFER_MAX_HEAD_DIM || dtype < APPROXIFER_F32 ||
+        dtype > APPROXIFER_BF16 || max_rows < 1 || max_len < 1 || window < 0 || sinks < 0)
+        return 0;
+    return approxifer::attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
+}
+
+int approxifer_cache_reserve(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, const int32_t *d_add, int32_t *d_status, int64_t B,
+                             int64_t M, int64_t P, int page, void *stream) {
+    int shift = 0;
+    const int rc = check_cache(B, M, P, page, &shift);
+    if (rc != APPROXIFER_OK) return rc;
+    if (B == 0) return APPROXIFER_OK;
+    if (d_table == nullptr || d_lens == nullptr || d_refs == nullptr || d_add == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    return approxifer::launch_cache_reserve(d_table, d_lens, d_refs, d_add, d_status, static_cast<int>(B), static_cast<int>(M),
+                                            static_cast<int>(P), shift, static_cast<hipStream_t>(stream));
+}
+
+int approxifer_cache_fork(const int32_t *d_table, const int32_t *d_lens, const int32_t *d_refs, const int32_t *d_parents,
+                          const int32_t *d_keep, int32_t *d_table_out, int32_t *d_lens_out, int32_t *d_refs_out,
+                          int32_t *d_status, void *d_pools, int64_t planes, int64_t page_bytes, int64_t B, int64_t B_out, int64_t M,
+                          int64_t P, int page, void *d_workspace, size_t workspace_bytes, void *stream) {
+    int shift = 0;
+    int rc = check_cache(B, M, P, page, &shift);
+    if (rc == APPROXIFER_OK) rc = check_cache(B_out, M, P, page, &shift);
+    if (rc == APPROXIFER_OK) rc = check_pools(d_pools, planes, page_bytes, P);
+    if (rc != APPROXIFER_OK) return rc;
+    if (d_refs == nullptr || d_refs_out == nullptr || (B > 0 && (d_table == nullptr || d_lens == nullptr)) ||
+        (B_out > 0 && (d_parents == nullptr || d_table_out == nullptr || d_lens_out == nullptr)))
+        return APPROXIFER_ERR_NULL_POINTER;
+    if (d_workspace == nullptr || workspace_bytes < approxifer_cache_workspace_bytes(B, B_out, P)) return APPROXIFER_ERR_WORKSPACE;
+    if (!aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
+    return approxifer::launch_cache_fork(d_table, d_lens, d_refs, d_parents, d_keep, d_table_out, d_lens_out, d_refs_out, d_status,
+                                         d_pools, planes, page_bytes, static_cast<int>(B), static_cast<int>(B_out),
+                                         static_cast<int>(M), static_cast<int>(P), shift, d_workspace,
+                                         static_cast<hipStream_t>(stream));
+}
+
+int approxifer_cache_compact(int32_t *d_table, const int32_t *d_lens, int32_t *d_refs, int32_t *d_moved, int32_t *d_live, void *d_pools,
+                             int64_t planes, int64_t page_bytes, int64_t B, int64_t M, int64_t P, int page, void *d_workspace,
+                             size_t workspace_bytes, void *stream) {
+    int shift = 0;
+    int rc = check_cache(B, M, P, page, &shift);
+    if (rc == APPROXIFER_OK) rc = check_pools(d_pools, planes, page_bytes, P);
+    if (rc != APPROXIFER_OK) return rc;
+    if (d_refs == nullptr || d_moved == nullptr || d_live == nullptr || (B > 0 && (d_table == nullptr || d_lens == nullptr)))
+        return APPROXIFER_ERR_NULL_POINTER;
+    if (d_workspace == nullptr || workspace_bytes < approxifer_cache_workspace_bytes(B, B, P)) return APPROXIFER_ERR_WORKSPACE;
+    if (!aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
+    return approxifer::launch_cache_compact(d_table, d_lens, d_refs, d_moved, d_live, d_pools, planes, page_bytes, static_cast<int>(B),
+                                            static_cast<int>(M), static_cast<int>(P), shift, d_workspace,
+                                            static_cast<hipStream_t>(stream));
+}
+
+size_t approxifer_cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P) {
+    if (B < 0 || B_out < 0 || P < 1 || B > APPROXIFER_MAX_SEQUENCES || B_out > APPROXIFER_MAX_SEQUENCES || P > 0x7fffffffLL) return 0;
+    return approxifer::cache_workspace_bytes(B, B_out, P);
 }
 
 }  // extern "C"
