@@ -1,5 +1,5 @@
 // Attention over a cache in pages.
-#include "attend_row.h"
+#include "attend_tiles.h"
 
 namespace approxifer {
 
@@ -27,6 +27,10 @@ __global__ __launch_bounds__(kWave) void attend_rows_kernel(AttendCall c) {
 size_t attend_workspace_bytes(int64_t, int64_t, int, int, int, int, int64_t, int64_t, int64_t, int64_t) { return 0; }
 
 int launch_attend(const AttendCall &c, void *, size_t, hipStream_t stream) {
+    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) >= 32)
+        return launch_status(c.dtype == APPROXIFER_F32   ? launch_tiles_f32(c, stream)
+                             : c.dtype == APPROXIFER_F16 ? launch_tiles_f16(c, stream)
+                                                         : launch_tiles_bf16(c, stream));
     const int64_t blocks = c.seq.T + (c.status != nullptr ? (c.seq.B + c.Hq - 1) / c.Hq : 0);
     const dim3 grid(static_cast<unsigned>(blocks), c.Hq), block(kWave);
     const auto kernel = c.dtype == APPROXIFER_F32   ? attend_rows_kernel<F32>

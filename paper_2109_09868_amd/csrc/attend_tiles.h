@@ -1,0 +1,379 @@
+// Attention of many rows: tiles of rows against tiles of keys on the matrix cores.
+//
+// The rows of a sequence and one head of the cache are packed, token by token and within a token head by head of the group that shares
+// the cache's head, so that a group needs its keys and values once whatever its size.  A workgroup has kWaves x 32 such rows and
+// walks over the tiles of keys that any of them sees: the first tokens' and the window's.  Per tile a wave forms
+//   S^T = K Q^T   [keys x 32 rows],  P = exp2(c S - c top),  O^T += V^T P^T   [Dh x 32 rows]
+// with its running maximum `top` and sum per row.  Scores come transposed so that a row's scores sit in one lane and the one 32
+// lanes away: a maximum is 31 local steps and one exchange; and so that a lane's scores are, after rounding, the operand of
+// the second product as they stand: which 8 of 16 keys a lane holds only has to be the same for V, whose operand is read from LDS
+// with the transposing load, 4 keys at a time.
+//
+// Keys and values go through LDS, the next tile's in registers while this one is computed, two tiles of each in LDS and one
+// barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
+#pragma once
+
+#include "attend_row.h"
+
+namespace approxifer {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef short v8s __attribute__((ext_vector_type(8)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+// D += A B of 16-byte pieces: A [32 x 2 pieces], B [2 pieces x 32]; lane l has row (column) l % 32 and piece l / 32.
+template <class E>
+__device__ __forceinline__ v16f multiply(v4i a, v4i b, v16f d);
+template <>
+__device__ __forceinline__ v16f multiply<BF16>(v4i a, v4i b, v16f d) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), d, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ v16f multiply<F16>(v4i a, v4i b, v16f d) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), d, 0, 0, 0);
+}
+template <>
+__device__ __forceinline__ v16f multiply<F32>(v4i a, v4i b, v16f d) {
+    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) d = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k], y[k], d, 0, 0, 0);
+    return d;
+}
+
+// Eight floats rounded to 16 bits.
+template <class E>
+__device__ __forceinline__ v4i rounded8(const float *p) {
+    typedef typename E::Value V8 __attribute__((ext_vector_type(8)));
+    V8 x;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = E::store(p[k]);
+    return __builtin_bit_cast(v4i, x);
+}
+
+// Whether any of a piece's values is an infinity or NaN: its exponent has all ones.
+template <class E>
+__device__ __forceinline__ bool not_finite(v4i x) {
+    constexpr bool kWide = sizeof(typename E::Value) == 4;
+    constexpr unsigned kMask = kWide ? 0x7f800000u : std::is_same<E, F16>::value ? 0x7c007c00u : 0x7f807f80u;
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const unsigned u = static_cast<unsigned>(x[k]) & kMask;
+        if (kWide) bad |= u == kMask;
+        else bad |= (u & 0xffffu) == (kMask & 0xffffu) || (u >> 16) == (kMask >> 16);
+    }
+    return bad;
+}
+
+// The other half's value as well as this one's: lanes l and l ^ 32 combined.
+__device__ __forceinline__ float half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return __int_as_float(r[0]) + __int_as_float(r[1]);
+}
+
+constexpr int pow2_at_least(int n, int p = 1) { return p >= n ? p : pow2_at_least(n, 2 * p); }
+
+template <class E, int DP>
+struct TileShape {
+    static constexpr int kSize = sizeof(typename E::Value);
+    static constexpr int kPerPiece = 16 / kSize;              // elements of 16 bytes
+    static constexpr int kPieces = DP * kSize / 16;           // of a row
+    static constexpr int kStride = pow2_at_least(kPieces);    // pieces between rows in LDS
+    static constexpr int kKeys = kStride * 16 > 512 || DP > 128 ? 32 : 64;
+    static constexpr int kWaves = 4;
+    static constexpr int kRows = 32 * kWaves;
+    static constexpr int kThreads = 64 * kWaves;
+    static constexpr int kLoads = kKeys * kPieces / kThreads; // pieces per thread and operand
+    static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
+    static constexpr int kLds = 4 * kBytes + 64;
+    static constexpr int kGroups = kLds <= 80 * 1024 ? 2 : 1; // workgroups that share a CU
+    static_assert(kKeys * kPieces % kThreads == 0, "whole pieces per thread");
+    // a row's permutation: reads of one piece by 16 rows, and of four neighbouring pieces by 4 rows, meet all banks
+    static __device__ __forceinline__ int permuted(int row) {
+        return kStride == 8 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3));
+    }
+    static __device__ __forceinline__ int at(int row, int piece) { return row * kStride * 16 + ((piece ^ permuted(row)) << 4); }
+};
+
+template <class E, int DP>
+__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int tiles, int pairs) {
+    typedef typename E::Value V;
+    typedef TileShape<E, DP> S;
+    constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
+    __shared__ __align__(16) char lds[S::kLds];
+    int *const dirty = reinterpret_cast<int *>(lds + 4 * S::kBytes);
+    const int lane = lane_id(), wave = wave_id(), half = lane >> 5, row32 = lane & 31;
+    const int64_t work = static_cast<int64_t>(tiles) * pairs;
+    if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
+        const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
+        if (b >= c.seq.B) return;
+        const int st = attend_status(c, static_cast<int>(b));
+        if (lane == 0) c.status[b] = st;
+        return;
+    }
+    // late rows see most: their tiles come first.  A pair of sequence and head keeps its XCD where pairs are a multiple of 8.
+    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / pairs, pair = static_cast<int>(blockIdx.x) % pairs;
+    const int h = pair % c.Hkv, group = c.Hq / c.Hkv;
+    const Rows rows = rows_of(c.seq, pair / c.Hkv);
+    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(tile) * S::kRows;
+    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || first >= row_count) return;
+    if (threadIdx.x == 0) *dirty = 0;
+
+    // this lane's row; lanes behind the last row repeat it
+    const int64_t row = min(first + wave * 32 + row32, row_count - 1);
+    const int token = static_cast<int>(row / group), head = h * group + static_cast<int>(row % group);
+    const int place = rows.place(token);
+    const int p0 = rows.place(static_cast<int>(first / group));
+    const int p1 = rows.place(static_cast<int>(min(first + S::kRows - 1, row_count - 1) / group));
+    const int w0 = __builtin_amdgcn_readfirstlane(place);
+    const int w1 = __builtin_amdgcn_readlane(place, 31);
+
+    v4i q[kSteps];
+    {
+        const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
+        const bool whole = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
+        const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            const int d = (2 * s + half) * S::kPerPiece;
+            v4i y = {0, 0, 0, 0};
+            if (d < c.Dh) {
+                if (whole) {
+                    y = *reinterpret_cast<const v4i *>(x + d);
+                } else {
+                    typedef V VP __attribute__((ext_vector_type(16 / sizeof(V))));
+                    VP z;
+#pragma unroll
+                    for (int k = 0; k < S::kPerPiece; ++k) z[k] = x[d + k];
+                    y = __builtin_bit_cast(v4i, z);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] ^= flip;
+            q[s] = y;
+        }
+    }
+    const float scale = fabsf(c.scale) * 1.44269504088896340736f;
+
+    // tiles of keys: those of the first tokens, then those of the window
+    const int from = c.window > 0 ? max(p0 - c.window + 1, 0) : 0;
+    const int sink_tiles = (min(c.sinks, from) + kKeys - 1) / kKeys;
+    const int main_tile = max(from / kKeys, sink_tiles);
+    const int steps = p1 < 0 ? 0 : sink_tiles + max(p1 / kKeys + 1 - main_tile, 0);
+    const auto begin_of = [&](int it) { return (it < sink_tiles ? it : main_tile + it - sink_tiles) * kKeys; };
+    const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
+    const int shift = c.seq.page_shift, slots = (1 << shift) - 1;
+    const auto page_at = [&](int it) {                        // of key `lane` of the tile; behind the last row's place: its page
+        const int j = min(begin_of(min(it, steps - 1)) + (lane & (kKeys - 1)), p1);
+        return table[j >> shift];
+    };
+    const V *const k_pool = static_cast<const V *>(c.k_pool), *const v_pool = static_cast<const V *>(c.v_pool);
+
+    v4i k_next[S::kLoads], v_next[S::kLoads];
+    unsigned long long bad_next = 0, bad = 0;
+    int page_next = steps > 0 ? page_at(0) : 0;
+    const auto load = [&](int it) {                           // tile `it` into registers
+        const bool off = page_next < 0 || page_next >= c.seq.P;
+        bad_next = __ballot(off);
+        const int page = off ? 0 : page_next;
+        const int j0 = begin_of(it);
+#pragma unroll
+        for (int n = 0; n < S::kLoads; ++n) {
+            const int index = n * S::kThreads + threadIdx.x, key = index / S::kPieces, piece = index % S::kPieces;
+            const int j = min(j0 + key, p1), p = __shfl(page, key);
+            const int64_t at = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j & slots)) * c.Dh + piece * S::kPerPiece;
+            const bool there = DP == c.Dh || piece * S::kPerPiece < c.Dh;
+            k_next[n] = there ? *reinterpret_cast<const v4i *>(k_pool + at) : v4i{0, 0, 0, 0};
+            v_next[n] = there ? *reinterpret_cast<const v4i *>(v_pool + at) : v4i{0, 0, 0, 0};
+        }
+        page_next = page_at(it + 1);
+    };
+    const auto whole_tile = [&](int j0, int a, int b) {       // every row from place a to place b sees every key
+        return j0 + kKeys - 1 <= a && (c.window == 0 || j0 > b - c.window || j0 + kKeys <= c.sinks);
+    };
+    const auto put = [&](int it) {                            // from the registers into LDS
+        char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
+        bool odd = false;
+#pragma unroll
+        for (int n = 0; n < S::kLoads; ++n) {
+            const int index = n * S::kThreads + threadIdx.x, key = index / S::kPieces, piece = index % S::kPieces;
+            *reinterpret_cast<v4i *>(kt + S::at(key, piece)) = k_next[n];
+            *reinterpret_cast<v4i *>(vt + S::at(key, piece)) = v_next[n];
+        }
+        if (!whole_tile(begin_of(it), p0, p1)) {              // 0 times what is no number: the product cannot hide it
+#pragma unroll
+            for (int n = 0; n < S::kLoads; ++n) odd |= not_finite<E>(v_next[n]);
+            if (__any(odd) && lane == 0) *dirty = 1;
+        }
+        bad = bad_next;
+    };
+
+    v16f out[kOut];
+#pragma unroll
+    for (int n = 0; n < kOut; ++n)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) out[n][k] = 0.0f;
+    float top = -INFINITY, total = 0.0f;
+
+    if (steps > 0) load(0);
+    __syncthreads();                                          // *dirty is 0
+    if (steps > 0) put(0);
+    __syncthreads();
+    for (int it = 0; it < steps; ++it) {
+        const int j0 = begin_of(it);
+        const unsigned long long bad_now = bad;
+        if (it + 1 < steps) load(it + 1);
+        const char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
+        const bool none = j0 > w1 || (c.window > 0 && j0 + kKeys - 1 <= w0 - c.window && j0 >= c.sinks);
+        if (!none) {
+            v16f s[kBlocks];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) s[b][k] = 0.0f;
+#pragma unroll
+                for (int n = 0; n < kSteps; ++n)
+                    s[b] = multiply<E>(*reinterpret_cast<const v4i *>(kt + S::at(b * 32 + row32, 2 * n + half)), q[n], s[b]);
+            }
+            const bool masked = !whole_tile(j0, w0, w1) || bad_now != 0;
+            if (masked) {
+                const int reach = place - j0 - 4 * half, start = c.sinks - j0 - 4 * half;
+                const unsigned long long off = bad_now >> (4 * half);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int key = b * 32 + 8 * (k / 4) + k % 4;
+                        const bool sees = key <= reach && (c.window == 0 || key > reach - c.window || key < start);
+                        if (off >> key & 1) s[b][k] = NAN;
+                        s[b][k] = sees ? s[b][k] : -INFINITY;
+                    }
+            }
+            float most = s[0][0];
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) most = fmaxf(most, s[b][k]);
+            most = fmaxf(half_max(most), top);
+            // the maximum moves only where it has grown by a factor of 256 in the weights: they stay below that, and within their types
+            if (__any((most - top) * scale > 8.0f || (top == -INFINITY && most > -INFINITY))) {
+                const float shrink = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((top - most) * scale);
+                const float f = top == -INFINITY ? 0.0f : shrink;
+                total *= f;
+#pragma unroll
+                for (int n = 0; n < kOut; ++n)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) out[n][k] *= f;
+                top = most;
+            }
+            const float base = top == -INFINITY ? 0.0f : top * scale;
+            float sum = 0.0f;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float was = s[b][k];
+                    float w = __builtin_amdgcn_exp2f(fmaf(was, scale, -base));
+                    if (masked) w = was == -INFINITY ? 0.0f : w;
+                    s[b][k] = w;
+                    sum += w;
+                }
+            total += sum;
+            if constexpr (S::kSize == 2) {
+                const int i = lane & 15, quad = lane >> 4 & 1;
+#pragma unroll
+                for (int n = 0; n < kKeys / 16; ++n) {
+                    float w[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = s[n / 2][8 * (n % 2) + k];
+                    const v4i p = rounded8<E>(w);
+#pragma unroll
+                    for (int o = 0; o < kOut; ++o) {
+                        v4s x[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int key = 16 * n + 8 * u + 4 * half + (i >> 2);
+                            const char *a = vt + S::at(key, 4 * o + 2 * quad + (i >> 1 & 1)) + (i & 1) * 8;
+                            x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(a));
+                        }
+                        const v8s y = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
+                        out[o] = multiply<E>(__builtin_bit_cast(v4i, y), p, out[o]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        const int key = b * 32 + 8 * (k / 4) + 4 * half + k % 4;
+#pragma unroll
+                        for (int o = 0; o < kOut; ++o) {
+                            const float x = *reinterpret_cast<const float *>(vt + S::at(key, 8 * o + (row32 >> 2)) + (row32 & 3) * 4);
+                            out[o] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[b][k], out[o], 0, 0, 0);
+                        }
+                    }
+            }
+        }
+        if (it + 1 < steps) put(it + 1);
+        __syncthreads();
+    }
+
+    if (*dirty != 0) {                                        // rows that must not see what a tile's product cannot hide
+        float *const scratch = reinterpret_cast<float *>(lds) + wave * (APPROXIFER_MAX_HEAD_DIM + kWave);
+        for (int n = 0; n < 32; ++n) {
+            const int64_t r = first + wave * 32 + n;
+            if (r < row_count)
+                attend_row<E>(c, rows, static_cast<int>(r / group), h * group + static_cast<int>(r % group), scratch,
+                              scratch + APPROXIFER_MAX_HEAD_DIM);
+        }
+        return;
+    }
+    total = half_sum(total);
+    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    if (first + wave * 32 + row32 < row_count) {
+        V *y = static_cast<V *>(c.out) + ((rows.start + token) * c.Hq + head) * c.Dh;
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int d = 32 * o + 8 * k + 4 * half;
+                typedef V V4 __attribute__((ext_vector_type(4)));
+                V4 x;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = E::store(out[o][4 * k + e] * inverse);
+                if (DP == c.Dh || d < c.Dh) *reinterpret_cast<V4 *>(y + d) = x;
+            }
+    }
+}
+
+template <class E, int DP>
+hipError_t launch_tiles(const AttendCall &c, hipStream_t stream) {
+    typedef TileShape<E, DP> S;
+    const int64_t group = c.Hq / c.Hkv, tiles = (c.max_rows * group + S::kRows - 1) / S::kRows, pairs = static_cast<int64_t>(c.seq.B) * c.Hkv;
+    const int64_t blocks = tiles * pairs + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
+    const auto kernel = attend_tiles_kernel<E, DP>;
+    return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c, static_cast<int>(tiles),
+                         static_cast<int>(pairs));
+}
+
+template <class E>
+hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
+    if (c.Dh <= 64) return launch_tiles<E, 64>(c, stream);
+    if (c.Dh <= 96) return launch_tiles<E, 96>(c, stream);
+    if (c.Dh <= 128) return launch_tiles<E, 128>(c, stream);
+    if (c.Dh <= 192) return launch_tiles<E, 192>(c, stream);
+    return launch_tiles<E, 256>(c, stream);
+}
+
+hipError_t launch_tiles_f32(const AttendCall &c, hipStream_t stream);
+hipError_t launch_tiles_f16(const AttendCall &c, hipStream_t stream);
+hipError_t launch_tiles_bf16(const AttendCall &c, hipStream_t stream);
+
+}  // namespace approxifer
