@@ -12,7 +12,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libapproxifer.so")
 SOURCES = ["api.hip", "encode.hip", "decode.hip", "byzantine.hip", "byzantine_pairs_large.hip",
            "byzantine_null_pairs_large.hip", "byzantine_pairs_medium.hip", "byzantine_null_pairs_medium.hip",
            "byzantine_pairs_small.hip", "byzantine_null_pairs_small.hip", "append.hip", "attend.hip",
-           "attend_tiles_f32.hip", "attend_tiles_f16.hip", "attend_tiles_bf16.hip", "pages.hip"]
+           "attend_tiles_f32.hip", "attend_tiles_f16.hip", "attend_tiles_bf16.hip",
+           "attend_tokens_f32.hip", "attend_tokens_f16.hip", "attend_tokens_bf16.hip", "pages.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

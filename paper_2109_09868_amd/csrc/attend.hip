@@ -1,42 +1,62 @@
-// Attention over a cache in pages.
+// Attention over a cache in pages: which kernel a call takes, and how its keys are cut.
 #include "attend_tiles.h"
+#include "attend_tokens.h"
 
 namespace approxifer {
 
 namespace {
 
-// One wave per row and head; behind the T rows a wave per sequence for the status.
-template <class E>
-__global__ __launch_bounds__(kWave) void attend_rows_kernel(AttendCall c) {
-    __shared__ float q[APPROXIFER_MAX_HEAD_DIM], p[kWave];
-    const int64_t t = blockIdx.x;
-    if (t >= c.seq.T) {
-        const int64_t b = (t - c.seq.T) * c.Hq + blockIdx.y;
-        if (c.status == nullptr || b >= c.seq.B) return;
-        const int st = attend_status(c, static_cast<int>(b));
-        if (lane_id() == 0) c.status[b] = st;
-        return;
+constexpr int kTokenRows = 32;                                // most rows of a sequence and head that the tokens kernel takes
+constexpr int64_t kTokenGroups = 1024;                        // workgroups that it is given if keys are cut
+
+// How the tokens kernel cuts the keys of a call into parts, given what workspace there is.
+TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
+                     size_t workspace_bytes) {
+    const int64_t group = Hq / Hkv, pairs = B * Hkv, blocks = (max_rows * group + 15) / 16;
+    const int64_t keys = dtype != APPROXIFER_F32 || Dh <= 64 ? 32 : 16;
+    int64_t tiles = (max_len + keys - 1) / keys;
+    if (window > 0) {                                         // no block of 16 rows sees more
+        const int64_t most = (sinks + keys - 1) / keys + (window + 16) / keys + 2;
+        tiles = tiles < most ? tiles : most;
     }
-    const Rows r = rows_of(c.seq, sequence_of(c.seq, t));
-    if (!r.ok || t < r.start || t >= r.start + r.n || r.n > c.max_rows || r.length > c.max_len) return;
-    attend_row<E>(c, r, static_cast<int>(t - r.start), blockIdx.y, q, p);
+    int64_t parts = kTokenGroups / (pairs * blocks > 0 ? pairs * blocks : 1);
+    parts = parts < (tiles + 7) / 8 ? parts : (tiles + 7) / 8;           // two tiles a wave at least
+    const int64_t room = static_cast<int64_t>(workspace_bytes) / (pairs * blocks * part_floats(Dh) * 4 + 1);
+    parts = parts < room ? parts : room;
+    TokenGrid g;
+    g.pairs = static_cast<int>(pairs);
+    g.blocks = static_cast<int>(blocks);
+    if (parts < 2) {
+        g.parts = 1;
+        g.chunk = 0x7fffffff;
+        return g;
+    }
+    g.chunk = static_cast<int>(((tiles + parts - 1) / parts + 3) / 4 * 4);
+    g.parts = static_cast<int>((tiles + g.chunk - 1) / g.chunk);
+    return g;
 }
 
 }  // namespace
 
-size_t attend_workspace_bytes(int64_t, int64_t, int, int, int, int, int64_t, int64_t, int64_t, int64_t) { return 0; }
+size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                              int64_t window, int64_t sinks) {
+    max_rows = max_rows < T ? max_rows : T;
+    if (max_rows * (Hq / Hkv) > kTokenRows) return 0;
+    const TokenGrid g = token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, static_cast<size_t>(1) << 60);
+    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(Dh) * 4;
+}
 
-int launch_attend(const AttendCall &c, void *, size_t, hipStream_t stream) {
-    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) >= 32)
-        return launch_status(c.dtype == APPROXIFER_F32   ? launch_tiles_f32(c, stream)
-                             : c.dtype == APPROXIFER_F16 ? launch_tiles_f16(c, stream)
-                                                         : launch_tiles_bf16(c, stream));
-    const int64_t blocks = c.seq.T + (c.status != nullptr ? (c.seq.B + c.Hq - 1) / c.Hq : 0);
-    const dim3 grid(static_cast<unsigned>(blocks), c.Hq), block(kWave);
-    const auto kernel = c.dtype == APPROXIFER_F32   ? attend_rows_kernel<F32>
-                        : c.dtype == APPROXIFER_F16 ? attend_rows_kernel<F16>
-                                                    : attend_rows_kernel<BF16>;
-    return launch_status(launch_kernel(kernel, grid, block, 0, stream, c));
+int launch_attend(const AttendCall &c, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    const int dtype = c.dtype;
+    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) > kTokenRows)
+        return launch_status(dtype == APPROXIFER_F32   ? launch_tiles_f32(c, stream)
+                             : dtype == APPROXIFER_F16 ? launch_tiles_f16(c, stream)
+                                                       : launch_tiles_bf16(c, stream));
+    const TokenGrid g = token_grid(c.seq.B, c.Hq, c.Hkv, c.Dh, dtype, c.max_rows, c.max_len, c.window, c.sinks, workspace_bytes);
+    float *const w = static_cast<float *>(workspace);
+    return launch_status(dtype == APPROXIFER_F32   ? launch_tokens_f32(c, g, w, stream)
+                         : dtype == APPROXIFER_F16 ? launch_tokens_f16(c, g, w, stream)
+                                                   : launch_tokens_bf16(c, g, w, stream));
 }
 
 }  // namespace approxifer

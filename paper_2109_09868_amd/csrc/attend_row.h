@@ -17,9 +17,30 @@ struct Visible {
     __device__ __forceinline__ bool sees(int j) const { return j <= place && (j >= from || j < sinks_end); }
 };
 
-// q: [256] and p: [64] floats of LDS of this wave.
+// The keys that rows at places p0..p1 see, in tiles of kKeys: those of the first tokens, then those of the window.
+template <int kKeys>
+struct KeyTiles {
+    int last, from, sinks_end, sink_tiles, main_tile, steps;
+    __device__ __forceinline__ KeyTiles(int window, int sinks, int p0, int p1) : last(p1) {
+        from = window > 0 ? max(p0 - window + 1, 0) : 0;
+        sinks_end = min(sinks, from);
+        sink_tiles = (sinks_end + kKeys - 1) / kKeys;
+        main_tile = max(from / kKeys, sink_tiles);
+        steps = p1 < 0 ? 0 : sink_tiles + max(p1 / kKeys + 1 - main_tile, 0);
+    }
+    __device__ __forceinline__ int begin_of(int it) const { return (it < sink_tiles ? it : main_tile + it - sink_tiles) * kKeys; }
+    // the key itself, or one that some row sees where none sees this one: what nobody sees is not read
+    __device__ __forceinline__ int seen(int j) const { return j > last ? last : j < from && j >= sinks_end ? from : j; }
+};
+
+// One row over the places [a0, a1) and [b0, b1), as far as it sees them.  q: [256] and p: [64] floats of LDS of this wave.  Lane l
+// has dimensions l, l + 64, .. of `out`, not yet divided by `total`; both relative to exp(top).
+struct RowSum {
+    float out[APPROXIFER_MAX_HEAD_DIM / kWave], top, total;
+};
 template <class E>
-__device__ void attend_row(const AttendCall &c, const Rows &r, int i, int head, float *q, float *p) {
+__device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head, float *q, float *p, int a0, int a1, int b0,
+                             int b1) {
     typedef typename E::Value V;
     constexpr int kPerLane = APPROXIFER_MAX_HEAD_DIM / kWave;
     const int lane = lane_id(), h = head / (c.Hq / c.Hkv), size = 1 << c.seq.page_shift;
@@ -29,13 +50,15 @@ __device__ void attend_row(const AttendCall &c, const Rows &r, int i, int head, 
     __builtin_amdgcn_wave_barrier();
     __threadfence_block();
     const Visible see(c.window, c.sinks, r.place(i));
-    float out[kPerLane] = {}, top = -INFINITY, total = 0.0f;
+    RowSum y{};
+    y.top = -INFINITY;
     for (int part = 0; part < 2; ++part) {
-        const int from = part ? see.from : 0, to = part ? see.place + 1 : see.sinks_end;
+        const int from = part ? b0 : a0, to = min(part ? b1 : a1, see.place + 1);
         for (int j0 = from; j0 < to; j0 += kWave) {
             const int j = j0 + lane, count = min(to - j0, kWave);
+            const bool mine = j < to && see.sees(j);
             float s = -INFINITY;
-            if (j < to) {
+            if (mine) {
                 const int page = page_of(c.seq, r.b, j);
                 if (page < 0) {
                     s = NAN;
@@ -48,32 +71,42 @@ __device__ void attend_row(const AttendCall &c, const Rows &r, int i, int head, 
             }
             float m = s;
             for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-            const float next = fmaxf(top, m), safe = next == -INFINITY ? 0.0f : next;
-            const float w = j < to ? expf(s - safe) : 0.0f, shrink = expf(top - safe);
+            const float next = fmaxf(y.top, m), safe = next == -INFINITY ? 0.0f : next;
+            const float w = mine ? expf(s - safe) : 0.0f, shrink = expf(y.top - safe);
             float sum = w;
             for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            total = total * shrink + sum;
-            top = next;
+            y.total = y.total * shrink + sum;
+            y.top = next;
             p[lane] = w;
             __builtin_amdgcn_wave_barrier();
             __threadfence_block();
-            for (int k = 0; k < kPerLane; ++k) out[k] *= shrink;
+            for (int k = 0; k < kPerLane; ++k) y.out[k] *= shrink;
             for (int n = 0; n < count; ++n) {
+                if (!see.sees(j0 + n)) continue;
                 const int page = page_of(c.seq, r.b, j0 + n);
                 if (page < 0) continue;
                 const V *v = static_cast<const V *>(c.v_pool) +
                              ((static_cast<int64_t>(page) * c.Hkv + h) * size + ((j0 + n) & (size - 1))) * c.Dh;
                 for (int k = 0; k < kPerLane; ++k)
-                    if (lane + k * kWave < c.Dh) out[k] += p[n] * E::load(v[lane + k * kWave]);
+                    if (lane + k * kWave < c.Dh) y.out[k] += p[n] * E::load(v[lane + k * kWave]);
             }
             __builtin_amdgcn_wave_barrier();
             __threadfence_block();
         }
     }
-    V *y = static_cast<V *>(c.out) + (t * c.Hq + head) * c.Dh;
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-    for (int k = 0; k < kPerLane; ++k)
-        if (lane + k * kWave < c.Dh) y[lane + k * kWave] = E::store(out[k] * inverse);
+    return y;
+}
+
+// The same over all that it sees, and written.
+template <class E>
+__device__ void attend_whole_row(const AttendCall &c, const Rows &r, int i, int head, float *q, float *p) {
+    typedef typename E::Value V;
+    const Visible see(c.window, c.sinks, r.place(i));
+    const RowSum y = attend_row<E>(c, r, i, head, q, p, 0, see.sinks_end, see.from, see.place + 1);
+    V *out = static_cast<V *>(c.out) + ((r.start + i) * c.Hq + head) * c.Dh;
+    const float inverse = y.total == 0.0f ? 0.0f : 1.0f / y.total;
+    for (int k = 0; k < APPROXIFER_MAX_HEAD_DIM / kWave; ++k)
+        if (lane_id() + k * kWave < c.Dh) out[lane_id() + k * kWave] = E::store(y.out[k] * inverse);
 }
 
 // One wave: the status of sequence b.

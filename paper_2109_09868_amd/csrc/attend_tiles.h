@@ -13,72 +13,9 @@
 // barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
 #pragma once
 
-#include "attend_row.h"
+#include "attend_pieces.h"
 
 namespace approxifer {
-
-typedef float v16f __attribute__((ext_vector_type(16)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef short v8s __attribute__((ext_vector_type(8)));
-typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-
-// D += A B of 16-byte pieces: A [32 x 2 pieces], B [2 pieces x 32]; lane l has row (column) l % 32 and piece l / 32.
-template <class E>
-__device__ __forceinline__ v16f multiply(v4i a, v4i b, v16f d);
-template <>
-__device__ __forceinline__ v16f multiply<BF16>(v4i a, v4i b, v16f d) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), d, 0, 0, 0);
-}
-template <>
-__device__ __forceinline__ v16f multiply<F16>(v4i a, v4i b, v16f d) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), d, 0, 0, 0);
-}
-template <>
-__device__ __forceinline__ v16f multiply<F32>(v4i a, v4i b, v16f d) {
-    const v4f x = __builtin_bit_cast(v4f, a), y = __builtin_bit_cast(v4f, b);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) d = __builtin_amdgcn_mfma_f32_32x32x2f32(x[k], y[k], d, 0, 0, 0);
-    return d;
-}
-
-// Eight floats rounded to 16 bits.
-template <class E>
-__device__ __forceinline__ v4i rounded8(const float *p) {
-    typedef typename E::Value V8 __attribute__((ext_vector_type(8)));
-    V8 x;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = E::store(p[k]);
-    return __builtin_bit_cast(v4i, x);
-}
-
-// Whether any of a piece's values is an infinity or NaN: its exponent has all ones.
-template <class E>
-__device__ __forceinline__ bool not_finite(v4i x) {
-    constexpr bool kWide = sizeof(typename E::Value) == 4;
-    constexpr unsigned kMask = kWide ? 0x7f800000u : std::is_same<E, F16>::value ? 0x7c007c00u : 0x7f807f80u;
-    bool bad = false;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const unsigned u = static_cast<unsigned>(x[k]) & kMask;
-        if (kWide) bad |= u == kMask;
-        else bad |= (u & 0xffffu) == (kMask & 0xffffu) || (u >> 16) == (kMask >> 16);
-    }
-    return bad;
-}
-
-// The other half's value as well as this one's: lanes l and l ^ 32 combined.
-__device__ __forceinline__ float half_max(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-    return fmaxf(__int_as_float(r[0]), __int_as_float(r[1]));
-}
-__device__ __forceinline__ float half_sum(float v) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-    return __int_as_float(r[0]) + __int_as_float(r[1]);
-}
-
-constexpr int pow2_at_least(int n, int p = 1) { return p >= n ? p : pow2_at_least(n, 2 * p); }
 
 template <class E, int DP>
 struct TileShape {
@@ -93,13 +30,9 @@ struct TileShape {
     static constexpr int kLoads = kKeys * kPieces / kThreads; // pieces per thread and operand
     static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
     static constexpr int kLds = 4 * kBytes + 64;
-    static constexpr int kGroups = kLds <= 80 * 1024 ? 2 : 1; // workgroups that share a CU
+    static constexpr int kGroups = kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
     static_assert(kKeys * kPieces % kThreads == 0, "whole pieces per thread");
-    // a row's permutation: reads of one piece by 16 rows, and of four neighbouring pieces by 4 rows, meet all banks
-    static __device__ __forceinline__ int permuted(int row) {
-        return kStride == 8 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3));
-    }
-    static __device__ __forceinline__ int at(int row, int piece) { return row * kStride * 16 + ((piece ^ permuted(row)) << 4); }
+    static __device__ __forceinline__ int at(int row, int piece) { return piece_at<kStride>(row, piece); }
 };
 
 template <class E, int DP>
@@ -141,38 +74,17 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         const bool whole = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
         const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            const int d = (2 * s + half) * S::kPerPiece;
-            v4i y = {0, 0, 0, 0};
-            if (d < c.Dh) {
-                if (whole) {
-                    y = *reinterpret_cast<const v4i *>(x + d);
-                } else {
-                    typedef V VP __attribute__((ext_vector_type(16 / sizeof(V))));
-                    VP z;
-#pragma unroll
-                    for (int k = 0; k < S::kPerPiece; ++k) z[k] = x[d + k];
-                    y = __builtin_bit_cast(v4i, z);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] ^= flip;
-            q[s] = y;
-        }
+        for (int s = 0; s < kSteps; ++s) q[s] = query_piece<E>(x, (2 * s + half) * S::kPerPiece, c.Dh, whole, flip);
     }
     const float scale = fabsf(c.scale) * 1.44269504088896340736f;
 
-    // tiles of keys: those of the first tokens, then those of the window
-    const int from = c.window > 0 ? max(p0 - c.window + 1, 0) : 0;
-    const int sink_tiles = (min(c.sinks, from) + kKeys - 1) / kKeys;
-    const int main_tile = max(from / kKeys, sink_tiles);
-    const int steps = p1 < 0 ? 0 : sink_tiles + max(p1 / kKeys + 1 - main_tile, 0);
-    const auto begin_of = [&](int it) { return (it < sink_tiles ? it : main_tile + it - sink_tiles) * kKeys; };
+    const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
+    const int steps = keys.steps;
+    const auto begin_of = [&](int it) { return keys.begin_of(it); };
     const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
     const int shift = c.seq.page_shift, slots = (1 << shift) - 1;
-    const auto page_at = [&](int it) {                        // of key `lane` of the tile; behind the last row's place: its page
-        const int j = min(begin_of(min(it, steps - 1)) + (lane & (kKeys - 1)), p1);
-        return table[j >> shift];
+    const auto page_at = [&](int it) {                        // of key `lane` of the tile
+        return table[keys.seen(begin_of(min(it, steps - 1)) + (lane & (kKeys - 1))) >> shift];
     };
     const V *const k_pool = static_cast<const V *>(c.k_pool), *const v_pool = static_cast<const V *>(c.v_pool);
 
@@ -187,7 +99,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
             const int index = n * S::kThreads + threadIdx.x, key = index / S::kPieces, piece = index % S::kPieces;
-            const int j = min(j0 + key, p1), p = __shfl(page, key);
+            const int j = keys.seen(j0 + key), p = __shfl(page, key);
             const int64_t at = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j & slots)) * c.Dh + piece * S::kPerPiece;
             const bool there = DP == c.Dh || piece * S::kPerPiece < c.Dh;
             k_next[n] = there ? *reinterpret_cast<const v4i *>(k_pool + at) : v4i{0, 0, 0, 0};
@@ -301,7 +213,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                         for (int u = 0; u < 2; ++u) {
                             const int key = 16 * n + 8 * u + 4 * half + (i >> 2);
                             const char *a = vt + S::at(key, 4 * o + 2 * quad + (i >> 1 & 1)) + (i & 1) * 8;
-                            x[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s *)(a));
+                            x[u] = load_transposed(a);
                         }
                         const v8s y = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
                         out[o] = multiply<E>(__builtin_bit_cast(v4i, y), p, out[o]);
@@ -330,8 +242,8 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         for (int n = 0; n < 32; ++n) {
             const int64_t r = first + wave * 32 + n;
             if (r < row_count)
-                attend_row<E>(c, rows, static_cast<int>(r / group), h * group + static_cast<int>(r % group), scratch,
-                              scratch + APPROXIFER_MAX_HEAD_DIM);
+                attend_whole_row<E>(c, rows, static_cast<int>(r / group), h * group + static_cast<int>(r % group), scratch,
+                                    scratch + APPROXIFER_MAX_HEAD_DIM);
         }
         return;
     }
@@ -344,11 +256,9 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int d = 32 * o + 8 * k + 4 * half;
-                typedef V V4 __attribute__((ext_vector_type(4)));
-                V4 x;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = E::store(out[o][4 * k + e] * inverse);
-                if (DP == c.Dh || d < c.Dh) *reinterpret_cast<V4 *>(y + d) = x;
+                if (DP == c.Dh || d < c.Dh)
+                    store4<E>(y + d, out[o][4 * k] * inverse, out[o][4 * k + 1] * inverse, out[o][4 * k + 2] * inverse,
+                              out[o][4 * k + 3] * inverse);
             }
     }
 }
