@@ -30,7 +30,246 @@ __device__ __forceinline__ void angle_of(const Rotation &rot, int i, int positio
     sincospif(2.0f * static_cast<float>(t - rint(t)), s, c);
 }
 
-// One wave per head of a token: queries, keys, then values; behind the T tokens a wave per sequence for the status.
+// Sum over each aligned group of L lanes, in every lane of it.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+    if (L >= 2) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kDppQuadXor1, 0xF, 0xF, true));
+    if (L >= 4) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kDppQuadXor2, 0xF, 0xF, true));
+    if (L >= 8) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kDppRowHalfMirror, 0xF, 0xF, true));
+    if (L >= 16) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kDppRowMirror, 0xF, 0xF, true));
+    if (L >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+        v = __int_as_float(r[0]) + __int_as_float(r[1]);
+    }
+    return v;
+}
+
+// The sequence of each lane's token t, for tokens that rise with the lane from the wave's first: 64 starts at a time are compared at
+// once, so that the common cases take one or two loads where bisection takes one for every doubling of B.
+__device__ __forceinline__ int sequences_of(const Sequences &s, int64_t t, int lanes) {
+    const int lane = lane_id();
+    const int64_t t0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(t)));
+    int lo = 0, span = s.B;                                   // the first token's sequence is in lo .. lo + span - 1
+    while (span > kWave) {
+        const int step = (span + kWave - 1) / kWave, at = lo + lane * step;
+        const unsigned long long before = __ballot(lane * step < span && s.starts[at] <= t0);
+        const int k = max(__popcll(before) - 1, 0);
+        const int next = lo + k * step;
+        span = min(step, lo + span - next);
+        lo = next;
+    }
+    const int at = lo + 1 + lane;                             // the wave's other tokens: mostly within 64 sequences from there
+    const int start = at <= s.B ? s.starts[at] : 0x7fffffff;
+    int b = lo;
+    bool far = false;
+    for (int g = 0; g < kWave; g += lanes) {
+        const int tg = __builtin_amdgcn_readlane(static_cast<int>(t), g);
+        const int passed = __popcll(__ballot(start <= tg));
+        if (lane >= g) {
+            b = lo + passed;
+            far = passed == kWave;
+        }
+    }
+    if (far) b = sequence_of(s, t);
+    return min(b, s.B - 1);
+}
+
+__device__ __forceinline__ void append_status(const AppendCall &c, int b) {
+    const Rows r = rows_of(c.seq, b);
+    int st = APPROXIFER_SEQUENCE_BAD;
+    if (r.ok) st = pages_status(c.seq, b, max(r.place(0), 0), r.n > 0 ? r.length : 0, 0, 0);
+    if (lane_id() == 0) c.status[b] = st;
+}
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+// Heads in pieces of 16 bytes, HBM-bound: every value is read once and written once.
+// L lanes share a head, two pieces each: those whose values are rotated with each other, piece u and the one pairs further (neighbours are
+// rotated: pieces 2 u and 2 u + 1), so that a rotation stays in the lane.  A group of lanes has one token and `per` of its heads one
+// after the other, so that cosine and sine of its pairs (float64 reduction, about 80 instructions each) are computed once for all of them.
+// Heads go in fours whose loads are in flight together.
+template <class E, int L>
+__global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotation rot, int per, int slices) {
+    typedef typename E::Value V;
+    constexpr int kPer = 16 / sizeof(V), kGroups = kWave / L, kHeads = 4;
+    typedef V VP __attribute__((ext_vector_type(16 / sizeof(V))));
+    const int lane = lane_id(), u = lane % L;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + wave_id();
+    const int64_t work = (c.seq.T + kGroups - 1) / kGroups * slices;
+    if (unit >= work) {                                       // the last waves: statuses
+        const int64_t b = unit - work;
+        if (c.status != nullptr && b < c.seq.B) append_status(c, static_cast<int>(b));
+        return;
+    }
+    const int slice = static_cast<int>(unit % slices);
+    const int64_t t_raw = unit / slices * kGroups + lane / L, t = min(t_raw, c.seq.T - 1);
+    const int h0 = slice * per, h1 = min(h0 + per, c.Hq + 2 * c.Hkv);
+
+    // this lane's two pieces
+    const int pieces = c.Dh / kPer, apart = c.interleaved ? 0 : c.pairs / kPer;
+    int a, b;
+    if (u < apart) {
+        a = u;
+        b = u + apart;
+    } else {
+        a = 2 * apart + 2 * (u - apart);
+        b = a + 1;
+    }
+    const bool has_a = a < pieces, has_b = b < pieces;
+    const int at_a = (has_a ? a : 0) * kPer, at_b = (has_b ? b : 0) * kPer;
+
+    const auto source = [&](int h) {
+        return h < c.Hq           ? static_cast<const V *>(c.q) + t * c.q_stride + static_cast<int64_t>(h) * c.Dh
+               : h < c.Hq + c.Hkv ? static_cast<const V *>(c.k) + t * c.k_stride + static_cast<int64_t>(h - c.Hq) * c.Dh
+                                  : static_cast<const V *>(c.v) + t * c.v_stride + static_cast<int64_t>(h - c.Hq - c.Hkv) * c.Dh;
+    };
+    VP xa[kHeads], xb[kHeads];
+    const auto load = [&](int h) {
+#pragma unroll
+        for (int n = 0; n < kHeads; ++n) {
+            const V *x = source(min(h + n, h1 - 1));
+            xa[n] = *reinterpret_cast<const VP *>(x + at_a);
+            xb[n] = *reinterpret_cast<const VP *>(x + at_b);
+        }
+    };
+    load(h0);                                                 // on their way while the rest is looked up
+
+    const int seq = sequences_of(c.seq, t, L);
+    const Rows r = rows_of(c.seq, seq);
+    const bool mine = t_raw < c.seq.T && r.ok && t >= r.start && t < r.start + r.n;
+    const int place = r.place(static_cast<int>(t - r.start));
+    int page = -1;
+    if (mine && place >= 0 && h1 > c.Hq) page = page_of(c.seq, seq, place);
+    const int size = 1 << c.seq.page_shift;
+    const int64_t slot = static_cast<int64_t>(page) * c.Hkv * size + (place & (size - 1));
+
+    float cs[kPer], sn[kPer];
+    bool turned[kPer];
+    if (h0 < c.Hq + c.Hkv) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int i = u * kPer + k;
+            turned[k] = i < c.pairs && (c.interleaved || u < apart);
+            cs[k] = 1.0f;
+            sn[k] = 0.0f;
+            if (turned[k]) {
+                const int position = c.positions != nullptr ? c.positions[t * c.axes + rot.axis[i]] : place;
+                angle_of(rot, i, position, &cs[k], &sn[k]);
+            }
+        }
+    }
+    float wq[2][kPer], wk[2][kPer];
+    if (c.q_weight != nullptr) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            wq[0][k] = E::load(static_cast<const V *>(c.q_weight)[at_a + k]);
+            wq[1][k] = E::load(static_cast<const V *>(c.q_weight)[at_b + k]);
+        }
+    }
+    if (c.k_weight != nullptr) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            wk[0][k] = E::load(static_cast<const V *>(c.k_weight)[at_a + k]);
+            wk[1][k] = E::load(static_cast<const V *>(c.k_weight)[at_b + k]);
+        }
+    }
+
+    for (int h = h0; h < h1; h += kHeads) {
+        VP ya[kHeads], yb[kHeads];
+#pragma unroll
+        for (int n = 0; n < kHeads; ++n) {
+            ya[n] = xa[n];
+            yb[n] = xb[n];
+        }
+        if (h + kHeads < h1) load(h + kHeads);
+#pragma unroll
+        for (int n = 0; n < kHeads; ++n) {
+            const int head = h + n;
+            if (head >= h1) break;
+            const bool is_q = head < c.Hq, is_v = head >= c.Hq + c.Hkv;
+            VP za = ya[n], zb = yb[n];
+            if (!is_v) {
+                float p[kPer], q[kPer];
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    p[k] = E::load(za[k]);
+                    q[k] = E::load(zb[k]);
+                }
+                if ((is_q ? c.q_weight : c.k_weight) != nullptr) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) sum += has_a ? p[k] * p[k] : 0.0f;
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) sum += has_b ? q[k] * q[k] : 0.0f;
+                    const float scale = 1.0f / sqrtf(lanes_sum<L>(sum) / c.Dh + c.eps);
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) {
+                        p[k] *= scale * (is_q ? wq[0][k] : wk[0][k]);
+                        q[k] *= scale * (is_q ? wq[1][k] : wk[1][k]);
+                    }
+                }
+                if (c.interleaved) {
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) {          // pair u kPer + k: in the first piece, then in the second
+                        float &f = k < kPer / 2 ? p[2 * k] : q[2 * k - kPer], &g = k < kPer / 2 ? p[2 * k + 1] : q[2 * k - kPer + 1];
+                        const float x = f, y = g;
+                        f = turned[k] ? x * cs[k] - y * sn[k] : x;
+                        g = turned[k] ? x * sn[k] + y * cs[k] : y;
+                    }
+                } else if (u < apart) {
+#pragma unroll
+                    for (int k = 0; k < kPer; ++k) {
+                        const float x = p[k], y = q[k];
+                        p[k] = x * cs[k] - y * sn[k];
+                        q[k] = x * sn[k] + y * cs[k];
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    za[k] = E::store(p[k]);
+                    zb[k] = E::store(q[k]);
+                }
+            }
+            V *y = nullptr;
+            if (is_q) {
+                if (mine) y = static_cast<V *>(c.q_out) + (t * c.Hq + head) * c.Dh;
+            } else if (page >= 0) {
+                const int kv = head - (is_v ? c.Hq + c.Hkv : c.Hq);
+                y = static_cast<V *>(is_v ? c.v_pool : c.k_pool) + (slot + static_cast<int64_t>(kv) * size) * c.Dh;
+            }
+            if (y != nullptr) {
+                if (has_a) *reinterpret_cast<VP *>(y + at_a) = za;
+                if (has_b) *reinterpret_cast<VP *>(y + at_b) = zb;
+            }
+        }
+    }
+}
+
+template <class E, int L>
+hipError_t launch_pieces(const AppendCall &c, const Rotation &rot, hipStream_t stream) {
+    const int heads = c.Hq + 2 * c.Hkv;
+    const int64_t waves = (c.seq.T + kWave / L - 1) / (kWave / L);
+    // enough waves to fill the GPU four deep, a head each at the least; then whole tokens, whose angles are computed once
+    const int64_t most = (4096 + waves - 1) / waves;
+    const int slices_wanted = static_cast<int>(most < heads ? most : heads), per = (heads + slices_wanted - 1) / slices_wanted;
+    const int slices = (heads + per - 1) / per;
+    const int64_t units = waves * slices + (c.status != nullptr ? c.seq.B : 0);
+    return launch_kernel(append_pieces_kernel<E, L>, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, stream, c, rot, per,
+                         slices);
+}
+template <class E>
+hipError_t launch_pieces_of(const AppendCall &c, const Rotation &rot, hipStream_t stream) {
+    constexpr int kPer = 16 / sizeof(typename E::Value);
+    const int pieces = c.Dh / kPer, apart = c.interleaved ? 0 : c.pairs / kPer, units = apart + (pieces - 2 * apart + 1) / 2;
+    if (units <= 2) return launch_pieces<E, 2>(c, rot, stream);
+    if (units <= 4) return launch_pieces<E, 4>(c, rot, stream);
+    if (units <= 8) return launch_pieces<E, 8>(c, rot, stream);
+    if (units <= 16) return launch_pieces<E, 16>(c, rot, stream);
+    return launch_pieces<E, 32>(c, rot, stream);
+}
+
+// Heads element by element, for rows that do not begin at 16 bytes and halves that are no whole pieces.  One wave per head of a token: queries,
+// keys, then values; behind the T tokens a wave per sequence for the status.
 template <class E>
 __global__ __launch_bounds__(kWave) void append_kernel(AppendCall c, Rotation rot) {
     typedef typename E::Value V;
@@ -40,10 +279,7 @@ __global__ __launch_bounds__(kWave) void append_kernel(AppendCall c, Rotation ro
     if (t >= c.seq.T) {                                       // the last blocks: statuses
         const int64_t b = (t - c.seq.T) * heads + h;
         if (c.status == nullptr || b >= c.seq.B) return;
-        const Rows r = rows_of(c.seq, static_cast<int>(b));
-        int st = APPROXIFER_SEQUENCE_BAD;
-        if (r.ok) st = pages_status(c.seq, r.b, max(r.place(0), 0), r.n > 0 ? r.length : 0, 0, 0);
-        if (lane == 0) c.status[b] = st;
+        append_status(c, static_cast<int>(b));
         return;
     }
     const int b = sequence_of(c.seq, t);
@@ -116,6 +352,12 @@ int launch_append(const Sequences &s, int Hq, int Hkv, int Dh, int dtype, const 
     }
     const AppendCall c{s, Hq, Hkv, Dh, pairs, axes, interleaved, q, k, v, q_stride, k_stride, v_stride, q_out, k_pool, v_pool,
                        q_weight, k_weight, static_cast<float>(eps), positions, status};
+    const int per = dtype == APPROXIFER_F32 ? 4 : 8;
+    const auto whole = [&](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % per == 0; };
+    if (s.T > 0 && whole(q, q_stride) && whole(k, k_stride) && whole(v, v_stride) && (interleaved || pairs % per == 0))
+        return launch_status(dtype == APPROXIFER_F32   ? launch_pieces_of<F32>(c, rot, stream)
+                             : dtype == APPROXIFER_F16 ? launch_pieces_of<F16>(c, rot, stream)
+                                                       : launch_pieces_of<BF16>(c, rot, stream));
     const int heads = Hq + 2 * Hkv;
     const int64_t blocks = s.T + (status != nullptr ? (s.B + heads - 1) / heads : 0);
     const dim3 grid(static_cast<unsigned>(blocks), heads), block(kWave);
