@@ -202,7 +202,7 @@ def _marshal():
         module, handle = _marshal_module(), None
         if module is not None:
             names = ("encode", "decode", "decode_top1", "decode_byzantine", "decode_byzantine_homogeneous", "pad_last_group",
-                     "top1", "wait_mask")
+                     "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact")
             handle = module.bind(*(ctypes.cast(getattr(lib, "approxifer_" + n), ctypes.c_void_p).value for n in names))
         _ordinary = (lib, module, handle)
     return _ordinary[1], _ordinary[2]
@@ -549,6 +549,11 @@ def approxifer_append(q, k, v, k_pool, v_pool, table, lens, starts, freq, q_weig
     into their pages.  q [T, Hq, Dh], k and v [T, Hkv, Dh] (slices of one projection's output will do), pools [P, Hkv, page,
     Dh], table [B, M], lens [B] and starts [B + 1] int32, freq [pairs] float64 on the host; positions [T, axes] int32 and
     axis [pairs] int32 on the host, or None: places in the sequence.  Returns (q_out [T, Hq, Dh], status [B] int32)."""
+    if q_out is not None and status is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.append(lib, q, k, v, k_pool, v_pool, table, lens, starts, freq, q_weight, k_weight,
+                                                      eps, positions, axis, interleaved, q_out, status)):
+            return q_out, status
     import torch
     dtype = k_pool.dtype
     code = _dtype_code(dtype)
@@ -605,6 +610,11 @@ def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len,
     max_rows and max_len bound the sequences' new tokens and lengths.  window (0: none) and sinks limit what a token sees,
     scale defaults to Dh ** -0.5.  workspace as approxifer_decode_byzantine's, of approxifer_attend_workspace_bytes().
     Returns (out [T, Hq, Dh], status [B] int32)."""
+    if out is not None and status is not None and workspace is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.attend(lib, q, k_pool, v_pool, table, lens, starts, max_rows, max_len, window, sinks,
+                                                      scale, out, status, None if workspace is NO_WORKSPACE else workspace)):
+            return out, status
     import torch
     dtype = k_pool.dtype
     code = _dtype_code(dtype)
@@ -631,6 +641,10 @@ def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len,
 def approxifer_cache_reserve(table, lens, refs, add, page, status=None, stream=None):
     """Room for add[b] more tokens of every sequence, in place: table [B, M], lens [B], refs [P], add [B] int32.
     Returns status [B] int32."""
+    if status is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.cache_reserve(lib, table, lens, refs, add, page, status)):
+            return status
     import torch
     B, M = table.shape
     if status is None:
@@ -662,6 +676,12 @@ def approxifer_cache_fork(pools, table, lens, refs, parents, keep=None, table_ou
     """New sequences out of old ones: sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens.
     pools [.., P, Hkv, page, Dh] hold all layers' keys and values; table [B, M], lens [B], refs [P], parents and keep [B_out]
     int32.  Returns (table_out [B_out, M], lens_out [B_out], refs_out [P], status [B_out])."""
+    if (table_out is not None and lens_out is not None and refs_out is not None and status is not None and workspace is not None
+            and stream is None):
+        native, lib = _marshal()
+        if native is not None and _done(native.cache_fork(lib, pools, table, lens, refs, parents, keep, table_out, lens_out, refs_out,
+                                                          status, workspace)):
+            return table_out, lens_out, refs_out, status
     import torch
     i32 = torch.int32
     B, M = table.shape
@@ -689,6 +709,10 @@ def approxifer_cache_fork(pools, table, lens, refs, parents, keep=None, table_ou
 def approxifer_cache_compact(pools, table, lens, refs, moved=None, live=None, workspace=None, stream=None):
     """Moves the live pages of all pools together, in place; table and refs follow.  Returns (moved [P] int32: where each page
     is now, -1 for free ones; live [1] int32)."""
+    if moved is not None and live is not None and workspace is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.cache_compact(lib, pools, table, lens, refs, moved, live, workspace)):
+            return moved, live
     import torch
     i32 = torch.int32
     B, M = table.shape
