@@ -27,15 +27,17 @@ struct TileShape {
     static constexpr int kWaves = 4;
     static constexpr int kRows = 32 * kWaves;
     static constexpr int kThreads = 64 * kWaves;
-    static constexpr int kLoads = kKeys * kPieces / kThreads; // pieces per thread and operand
+    static constexpr int kOwn = kKeys / kWaves;               // keys of a tile that a wave loads
+    static constexpr int kLoads = kOwn * kPieces / kWave;     // pieces per lane and operand
     static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
     static constexpr int kLds = 4 * kBytes + 64;
     static constexpr int kGroups = kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
-    static_assert(kKeys * kPieces % kThreads == 0, "whole pieces per thread");
+    static_assert(kOwn * kPieces % kWave == 0, "whole pieces per lane");
     static __device__ __forceinline__ int at(int row, int piece) { return piece_at<kStride>(row, piece); }
 };
 
-template <class E, int DP>
+// kWhole: Dh is DP.
+template <class E, int DP, bool kWhole>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int tiles, int pairs) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
@@ -73,10 +75,11 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
         const bool whole = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
         const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
+        const int Dh = c.scale == 0.0f ? 0 : kWhole ? DP : c.Dh;  // scale 0: scores of 0 at scale 1
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) q[s] = query_piece<E>(x, (2 * s + half) * S::kPerPiece, c.Dh, whole, flip);
+        for (int s = 0; s < kSteps; ++s) q[s] = query_piece<E>(x, (2 * s + half) * S::kPerPiece, Dh, whole, flip);
     }
-    const float scale = fabsf(c.scale) * 1.44269504088896340736f;
+    const float scale = c.scale == 0.0f ? 1.0f : fabsf(c.scale) * 1.44269504088896340736f;
 
     const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
     const int steps = keys.steps;
@@ -91,19 +94,35 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     v4i k_next[S::kLoads], v_next[S::kLoads];
     unsigned long long bad_next = 0, bad = 0;
     int page_next = steps > 0 ? page_at(0) : 0;
-    const auto load = [&](int it) {                           // tile `it` into registers
+    const int Dh = kWhole ? DP : c.Dh;
+    const auto load = [&](int it) {                           // this wave's keys of tile `it` into registers
         const bool off = page_next < 0 || page_next >= c.seq.P;
         bad_next = __ballot(off);
-        const int page = off ? 0 : page_next;
-        const int j0 = begin_of(it);
+        const int page = off ? 0 : page_next, j0 = begin_of(it) + wave * S::kOwn;
+        const auto piece = [&](const V *x, int at) {
+            v4i y = *reinterpret_cast<const v4i *>(x + (kWhole || at < Dh ? at : 0));
+            if (!kWhole && at >= Dh) y = v4i{0, 0, 0, 0};     // values behind the head
+            return y;
+        };
+        if (slots + 1 >= S::kOwn) {                           // one page: the address is the wave's, plus a constant of the lane's
+            const int p = __builtin_amdgcn_readlane(page, wave * S::kOwn);
+            const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j0 & slots)) * Dh;
+            const V *const k = k_pool + base, *const v = v_pool + base;
 #pragma unroll
-        for (int n = 0; n < S::kLoads; ++n) {
-            const int index = n * S::kThreads + threadIdx.x, key = index / S::kPieces, piece = index % S::kPieces;
-            const int j = keys.seen(j0 + key), p = __shfl(page, key);
-            const int64_t at = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j & slots)) * c.Dh + piece * S::kPerPiece;
-            const bool there = DP == c.Dh || piece * S::kPerPiece < c.Dh;
-            k_next[n] = there ? *reinterpret_cast<const v4i *>(k_pool + at) : v4i{0, 0, 0, 0};
-            v_next[n] = there ? *reinterpret_cast<const v4i *>(v_pool + at) : v4i{0, 0, 0, 0};
+            for (int n = 0; n < S::kLoads; ++n) {
+                const int index = n * kWave + lane, key = index / S::kPieces, at = index % S::kPieces * S::kPerPiece;
+                k_next[n] = piece(k + key * Dh, at);
+                v_next[n] = piece(v + key * Dh, at);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < S::kLoads; ++n) {
+                const int index = n * kWave + lane, key = index / S::kPieces, at = index % S::kPieces * S::kPerPiece;
+                const int p = __shfl(page, wave * S::kOwn + key);
+                const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + ((j0 + key) & slots)) * Dh;
+                k_next[n] = piece(k_pool + base, at);
+                v_next[n] = piece(v_pool + base, at);
+            }
         }
         page_next = page_at(it + 1);
     };
@@ -112,17 +131,21 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     };
     const auto put = [&](int it) {                            // from the registers into LDS
         char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
-        bool odd = false;
+        if (!whole_tile(begin_of(it), p0, p1)) {              // 0 times what is no number: the product cannot hide it
+            bool odd = false;
+#pragma unroll
+            for (int n = 0; n < S::kLoads; ++n) {
+                const int j = begin_of(it) + wave * S::kOwn + (n * kWave + lane) / S::kPieces;
+                if (keys.seen(j) != j) v_next[n] = v4i{0, 0, 0, 0};       // by nobody: whatever the page holds there
+                odd |= not_finite<E>(v_next[n]);
+            }
+            if (__any(odd) && lane == 0) *dirty = 1;
+        }
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
-            const int index = n * S::kThreads + threadIdx.x, key = index / S::kPieces, piece = index % S::kPieces;
+            const int index = n * kWave + lane, key = wave * S::kOwn + index / S::kPieces, piece = index % S::kPieces;
             *reinterpret_cast<v4i *>(kt + S::at(key, piece)) = k_next[n];
             *reinterpret_cast<v4i *>(vt + S::at(key, piece)) = v_next[n];
-        }
-        if (!whole_tile(begin_of(it), p0, p1)) {              // 0 times what is no number: the product cannot hide it
-#pragma unroll
-            for (int n = 0; n < S::kLoads; ++n) odd |= not_finite<E>(v_next[n]);
-            if (__any(odd) && lane == 0) *dirty = 1;
         }
         bad = bad_next;
     };
@@ -175,9 +198,8 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                 for (int k = 0; k < 16; ++k) most = fmaxf(most, s[b][k]);
             most = fmaxf(half_max(most), top);
             // the maximum moves only where it has grown by a factor of 256 in the weights: they stay below that, and within their types
-            if (__any((most - top) * scale > 8.0f || (top == -INFINITY && most > -INFINITY))) {
-                const float shrink = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((top - most) * scale);
-                const float f = top == -INFINITY ? 0.0f : shrink;
+            if (__any((most - top) * scale > 8.0f)) {
+                const float f = most == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((top - most) * scale);
                 total *= f;
 #pragma unroll
                 for (int n = 0; n < kOut; ++n)
@@ -191,11 +213,8 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
-                    const float was = s[b][k];
-                    float w = __builtin_amdgcn_exp2f(fmaf(was, scale, -base));
-                    if (masked) w = was == -INFINITY ? 0.0f : w;
-                    s[b][k] = w;
-                    sum += w;
+                    s[b][k] = __builtin_amdgcn_exp2f(fmaf(s[b][k], scale, -base));
+                    sum += s[b][k];
                 }
             total += sum;
             if constexpr (S::kSize == 2) {
@@ -256,30 +275,33 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int d = 32 * o + 8 * k + 4 * half;
-                if (DP == c.Dh || d < c.Dh)
+                if (kWhole || d < c.Dh)
                     store4<E>(y + d, out[o][4 * k] * inverse, out[o][4 * k + 1] * inverse, out[o][4 * k + 2] * inverse,
                               out[o][4 * k + 3] * inverse);
             }
     }
 }
 
-template <class E, int DP>
+template <class E, int DP, bool kWhole>
 hipError_t launch_tiles(const AttendCall &c, hipStream_t stream) {
     typedef TileShape<E, DP> S;
     const int64_t group = c.Hq / c.Hkv, tiles = (c.max_rows * group + S::kRows - 1) / S::kRows, pairs = static_cast<int64_t>(c.seq.B) * c.Hkv;
     const int64_t blocks = tiles * pairs + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
-    const auto kernel = attend_tiles_kernel<E, DP>;
+    const auto kernel = attend_tiles_kernel<E, DP, kWhole>;
     return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c, static_cast<int>(tiles),
                          static_cast<int>(pairs));
 }
 
 template <class E>
 hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
-    if (c.Dh <= 64) return launch_tiles<E, 64>(c, stream);
-    if (c.Dh <= 96) return launch_tiles<E, 96>(c, stream);
-    if (c.Dh <= 128) return launch_tiles<E, 128>(c, stream);
-    if (c.Dh <= 192) return launch_tiles<E, 192>(c, stream);
-    return launch_tiles<E, 256>(c, stream);
+    if (c.Dh == 64) return launch_tiles<E, 64, true>(c, stream);
+    if (c.Dh == 128) return launch_tiles<E, 128, true>(c, stream);
+    if (c.Dh == 256) return launch_tiles<E, 256, true>(c, stream);
+    if (c.Dh < 64) return launch_tiles<E, 64, false>(c, stream);
+    if (c.Dh <= 96) return launch_tiles<E, 96, false>(c, stream);
+    if (c.Dh < 128) return launch_tiles<E, 128, false>(c, stream);
+    if (c.Dh <= 192) return launch_tiles<E, 192, false>(c, stream);
+    return launch_tiles<E, 256, false>(c, stream);
 }
 
 hipError_t launch_tiles_f32(const AttendCall &c, hipStream_t stream);
