@@ -17,6 +17,8 @@
 
 namespace approxifer {
 
+constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
+
 template <class E, int DP>
 struct TileShape {
     static constexpr int kSize = sizeof(typename E::Value);
@@ -31,20 +33,21 @@ struct TileShape {
     static constexpr int kLoads = kOwn * kPieces / kWave;     // pieces per lane and operand
     static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
     static constexpr int kLds = 4 * kBytes + 64;
+    static constexpr int kAhead = 6;                          // operands in flight
     static constexpr int kGroups = kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
     static_assert(kOwn * kPieces % kWave == 0, "whole pieces per lane");
     static __device__ __forceinline__ int at(int row, int piece) { return piece_at<kStride>(row, piece); }
 };
 
-// kWhole: Dh is DP.
-template <class E, int DP, bool kWhole>
+// kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.
+template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int tiles, int pairs) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
     constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
     __shared__ __align__(16) char lds[S::kLds];
     int *const dirty = reinterpret_cast<int *>(lds + 4 * S::kBytes);
-    const int lane = lane_id(), wave = wave_id(), half = lane >> 5, row32 = lane & 31;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
     const int64_t work = static_cast<int64_t>(tiles) * pairs;
     if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
         const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
@@ -104,7 +107,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
             if (!kWhole && at >= Dh) y = v4i{0, 0, 0, 0};     // values behind the head
             return y;
         };
-        if (slots + 1 >= S::kOwn) {                           // one page: the address is the wave's, plus a constant of the lane's
+        if constexpr (!kSmall) {                         // one page: the address is the wave's, plus a constant of the lane's
             const int p = __builtin_amdgcn_readlane(page, wave * S::kOwn);
             const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j0 & slots)) * Dh;
             const V *const k = k_pool + base, *const v = v_pool + base;
@@ -177,6 +180,14 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                 for (int n = 0; n < kSteps; ++n)
                     s[b] = multiply<E>(*reinterpret_cast<const v4i *>(kt + S::at(b * 32 + row32, 2 * n + half)), q[n], s[b]);
             }
+            // the products one behind the other with kAhead operands on their way: left alone, each waits for its own read
+            __builtin_amdgcn_sched_group_barrier(kDsRead, S::kAhead, 0);
+#pragma unroll
+            for (int n = 0; n < kBlocks * kSteps - S::kAhead; ++n) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, S::kSize == 4 ? 4 : 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(kMfma, S::kAhead * (S::kSize == 4 ? 4 : 1), 0);
             const bool masked = !whole_tile(j0, w0, w1) || bad_now != 0;
             if (masked) {
                 const int reach = place - j0 - 4 * half, start = c.sinks - j0 - 4 * half;
@@ -282,26 +293,30 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     }
 }
 
-template <class E, int DP, bool kWhole>
+template <class E, int DP, bool kWhole, bool kSmall>
 hipError_t launch_tiles(const AttendCall &c, hipStream_t stream) {
     typedef TileShape<E, DP> S;
     const int64_t group = c.Hq / c.Hkv, tiles = (c.max_rows * group + S::kRows - 1) / S::kRows, pairs = static_cast<int64_t>(c.seq.B) * c.Hkv;
     const int64_t blocks = tiles * pairs + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
-    const auto kernel = attend_tiles_kernel<E, DP, kWhole>;
+    const auto kernel = attend_tiles_kernel<E, DP, kWhole, kSmall>;
     return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c, static_cast<int>(tiles),
                          static_cast<int>(pairs));
 }
 
+template <class E, bool kSmall>
+hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
+    if (c.Dh == 64) return launch_tiles<E, 64, true, kSmall>(c, stream);
+    if (c.Dh == 128) return launch_tiles<E, 128, true, kSmall>(c, stream);
+    if (c.Dh == 256) return launch_tiles<E, 256, true, kSmall>(c, stream);
+    if (c.Dh < 64) return launch_tiles<E, 64, false, kSmall>(c, stream);
+    if (c.Dh <= 96) return launch_tiles<E, 96, false, kSmall>(c, stream);
+    if (c.Dh < 128) return launch_tiles<E, 128, false, kSmall>(c, stream);
+    if (c.Dh <= 192) return launch_tiles<E, 192, false, kSmall>(c, stream);
+    return launch_tiles<E, 256, false, kSmall>(c, stream);
+}
 template <class E>
 hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
-    if (c.Dh == 64) return launch_tiles<E, 64, true>(c, stream);
-    if (c.Dh == 128) return launch_tiles<E, 128, true>(c, stream);
-    if (c.Dh == 256) return launch_tiles<E, 256, true>(c, stream);
-    if (c.Dh < 64) return launch_tiles<E, 64, false>(c, stream);
-    if (c.Dh <= 96) return launch_tiles<E, 96, false>(c, stream);
-    if (c.Dh < 128) return launch_tiles<E, 128, false>(c, stream);
-    if (c.Dh <= 192) return launch_tiles<E, 192, false>(c, stream);
-    return launch_tiles<E, 256, false>(c, stream);
+    return c.seq.page_shift >= 4 ? launch_tiles_of<E, false>(c, stream) : launch_tiles_of<E, true>(c, stream);
 }
 
 hipError_t launch_tiles_f32(const AttendCall &c, hipStream_t stream);
