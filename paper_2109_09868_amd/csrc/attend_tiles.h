@@ -17,7 +17,7 @@
 
 namespace approxifer {
 
-constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
+constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100, kTrans = 0x400;                   // of sched_group_barrier
 
 template <class E, int DP>
 struct TileShape {
@@ -32,23 +32,40 @@ struct TileShape {
     static constexpr int kOwn = kKeys / kWaves;               // keys of a tile that a wave loads
     static constexpr int kLoads = kOwn * kPieces / kWave;     // pieces per lane and operand
     static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
-    static constexpr int kLds = 4 * kBytes + 64;
+    static constexpr int kLds = 4 * kBytes;
     static constexpr int kAhead = 6;                          // operands in flight
     static constexpr int kGroups = kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
     static_assert(kOwn * kPieces % kWave == 0, "whole pieces per lane");
     static __device__ __forceinline__ int at(int row, int piece) { return piece_at<kStride>(row, piece); }
 };
 
+// Tiles of rows are numbered over all sequences: sequence b begins at tile starts[b] group / rows + b, which leaves each room for its
+// own and at most one that is empty.  (Tiles of every sequence up to the longest would leave most workgroups of a ragged batch empty;
+// that costs more than their launches: workgroups go to the parts of an XCD in turn, whether they are empty or not, and where every
+// second one was, half the CUs stood still.)  Returns the sequence of tile `slot` and its tile there.
+__device__ __forceinline__ int slot_owner(const Sequences &s, int64_t slot, int group, int rows, int64_t *tile) {
+    const auto begin_of = [&](int b) { return static_cast<int64_t>(s.starts[b]) * group / rows + b; };
+    int lo = 0, span = s.B;
+    while (span > 1) {                                        // 64 sequences at a time
+        const int step = (span + kWave - 1) / kWave, k = lane_id() * step;
+        const unsigned long long before = __ballot(k < span && begin_of(lo + k) <= slot);
+        const int last = before != 0 ? (63 - __clzll(before)) * step : 0;
+        span = min(step, span - last);
+        lo += last;
+    }
+    *tile = slot - begin_of(lo);
+    return lo;
+}
+
 // kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.
 template <class E, int DP, bool kWhole, bool kSmall>
-__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int tiles, int pairs) {
+__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int64_t slots, bool single) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
     constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
     __shared__ __align__(16) char lds[S::kLds];
-    int *const dirty = reinterpret_cast<int *>(lds + 4 * S::kBytes);
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
-    const int64_t work = static_cast<int64_t>(tiles) * pairs;
+    const int64_t work = slots * c.Hkv;
     if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
         const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
         if (b >= c.seq.B) return;
@@ -56,13 +73,13 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         if (lane == 0) c.status[b] = st;
         return;
     }
-    // late rows see most: their tiles come first.  A pair of sequence and head keeps its XCD where pairs are a multiple of 8.
-    const int tile = tiles - 1 - static_cast<int>(blockIdx.x) / pairs, pair = static_cast<int>(blockIdx.x) % pairs;
-    const int h = pair % c.Hkv, group = c.Hq / c.Hkv;
-    const Rows rows = rows_of(c.seq, pair / c.Hkv);
-    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(tile) * S::kRows;
-    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || first >= row_count) return;
-    if (threadIdx.x == 0) *dirty = 0;
+    const int h = static_cast<int>(blockIdx.x) % c.Hkv, group = c.Hq / c.Hkv;
+    const int64_t slot = slots - 1 - static_cast<int>(blockIdx.x) / c.Hkv;
+    int64_t tile = 0;
+    const int b = single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
+    const Rows rows = rows_of(c.seq, b);
+    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = tile * S::kRows;
+    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || tile < 0 || first >= row_count) return;
 
     // this lane's row; lanes behind the last row repeat it
     const int64_t row = min(first + wave * 32 + row32, row_count - 1);
@@ -88,13 +105,14 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     const int steps = keys.steps;
     const auto begin_of = [&](int it) { return keys.begin_of(it); };
     const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
-    const int shift = c.seq.page_shift, slots = (1 << shift) - 1;
+    const int shift = c.seq.page_shift, in_page = (1 << shift) - 1;
     const auto page_at = [&](int it) {                        // of key `lane` of the tile
         return table[keys.seen(begin_of(min(it, steps - 1)) + (lane & (kKeys - 1))) >> shift];
     };
     const V *const k_pool = static_cast<const V *>(c.k_pool), *const v_pool = static_cast<const V *>(c.v_pool);
 
     v4i k_next[S::kLoads], v_next[S::kLoads];
+    bool odd = false;                                         // a value that is no number, in a tile that not every row sees all of
     unsigned long long bad_next = 0, bad = 0;
     int page_next = steps > 0 ? page_at(0) : 0;
     const int Dh = kWhole ? DP : c.Dh;
@@ -109,7 +127,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         };
         if constexpr (!kSmall) {                         // one page: the address is the wave's, plus a constant of the lane's
             const int p = __builtin_amdgcn_readlane(page, wave * S::kOwn);
-            const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (j0 & slots)) * Dh;
+            const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (in_page + 1) + (j0 & in_page)) * Dh;
             const V *const k = k_pool + base, *const v = v_pool + base;
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) {
@@ -122,7 +140,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
             for (int n = 0; n < S::kLoads; ++n) {
                 const int index = n * kWave + lane, key = index / S::kPieces, at = index % S::kPieces * S::kPerPiece;
                 const int p = __shfl(page, wave * S::kOwn + key);
-                const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + ((j0 + key) & slots)) * Dh;
+                const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (in_page + 1) + ((j0 + key) & in_page)) * Dh;
                 k_next[n] = piece(k_pool + base, at);
                 v_next[n] = piece(v_pool + base, at);
             }
@@ -135,14 +153,12 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     const auto put = [&](int it) {                            // from the registers into LDS
         char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
         if (!whole_tile(begin_of(it), p0, p1)) {              // 0 times what is no number: the product cannot hide it
-            bool odd = false;
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) {
                 const int j = begin_of(it) + wave * S::kOwn + (n * kWave + lane) / S::kPieces;
                 if (keys.seen(j) != j) v_next[n] = v4i{0, 0, 0, 0};       // by nobody: whatever the page holds there
                 odd |= not_finite<E>(v_next[n]);
             }
-            if (__any(odd) && lane == 0) *dirty = 1;
         }
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
@@ -160,9 +176,10 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         for (int k = 0; k < 16; ++k) out[n][k] = 0.0f;
     float top = -INFINITY, total = 0.0f;
 
-    if (steps > 0) load(0);
-    __syncthreads();                                          // *dirty is 0
-    if (steps > 0) put(0);
+    if (steps > 0) {
+        load(0);
+        put(0);
+    }
     __syncthreads();
     for (int it = 0; it < steps; ++it) {
         const int j0 = begin_of(it);
@@ -249,6 +266,13 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                         out[o] = multiply<E>(__builtin_bit_cast(v4i, y), p, out[o]);
                     }
                 }
+                // as above, with the weights of the next 16 keys between the products of these
+                __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
+#pragma unroll
+                for (int n = 0; n < kKeys / 16 * kOut; ++n) {
+                    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+                }
             } else {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
@@ -267,7 +291,13 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         __syncthreads();
     }
 
-    if (*dirty != 0) {                                        // rows that must not see what a tile's product cannot hide
+    int *const flags = reinterpret_cast<int *>(lds);          // the tiles are done with
+    if (lane == 0) flags[wave] = 0;
+    if (__any(odd) && lane == 0) flags[wave] = 1;
+    __syncthreads();
+    const v4i any_odd = *reinterpret_cast<const v4i *>(flags);
+    __syncthreads();
+    if ((any_odd[0] | any_odd[1] | any_odd[2] | any_odd[3]) != 0) {                                     // rows that must not see what a tile's product cannot hide
         float *const scratch = reinterpret_cast<float *>(lds) + wave * (APPROXIFER_MAX_HEAD_DIM + kWave);
         for (int n = 0; n < 32; ++n) {
             const int64_t r = first + wave * 32 + n;
@@ -296,11 +326,13 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
 template <class E, int DP, bool kWhole, bool kSmall>
 hipError_t launch_tiles(const AttendCall &c, hipStream_t stream) {
     typedef TileShape<E, DP> S;
-    const int64_t group = c.Hq / c.Hkv, tiles = (c.max_rows * group + S::kRows - 1) / S::kRows, pairs = static_cast<int64_t>(c.seq.B) * c.Hkv;
-    const int64_t blocks = tiles * pairs + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
-    const auto kernel = attend_tiles_kernel<E, DP, kWhole, kSmall>;
-    return launch_kernel(kernel, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c, static_cast<int>(tiles),
-                         static_cast<int>(pairs));
+    // late rows see most: their tiles come first.  A head of the cache keeps its XCD where there are 8 of them.
+    const int64_t group = c.Hq / c.Hkv;
+    const bool single = c.max_rows * group <= S::kRows;       // a tile for each sequence
+    const int64_t slots = single ? c.seq.B : c.seq.T * group / S::kRows + c.seq.B;
+    const int64_t blocks = slots * c.Hkv + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
+    return launch_kernel(attend_tiles_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c,
+                         slots, single);
 }
 
 template <class E, bool kSmall>
