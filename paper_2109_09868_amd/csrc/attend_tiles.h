@@ -9,15 +9,16 @@
 // the second product as they stand: which 8 of 16 keys a lane holds only has to be the same for V, whose operand is read from LDS
 // with the transposing load, 4 keys at a time.
 //
-// Keys and values go through LDS, the next tile's in registers while this one is computed, two tiles of each in LDS and one
-// barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
+// Keys and values go through LDS, the next tile's on their way while this one is computed: straight there where heads and pages are whole
+// (else by registers), two tiles of each and one barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
 #pragma once
 
 #include "attend_pieces.h"
 
 namespace approxifer {
 
-constexpr int kValu = 0x2, kMfma = 0x8, kDsRead = 0x100, kTrans = 0x400;                   // of sched_group_barrier
+constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
+constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
 
 template <class E, int DP>
 struct TileShape {
@@ -62,6 +63,7 @@ template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int64_t slots, bool single) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
+    constexpr bool kDirect = kWhole && !kSmall && S::kStride == S::kPieces;
     constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
     __shared__ __align__(16) char lds[S::kLds];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
@@ -147,6 +149,27 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         }
         page_next = page_at(it + 1);
     };
+    // The same straight into LDS, without a register: LDS takes the lanes' 16 bytes one behind the other, so each lane asks for the piece that
+    // the row's permutation has there.
+    const auto fetch = [&](int it) {
+        char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
+        const bool off = page_next < 0 || page_next >= c.seq.P;
+        bad_next = __ballot(off);
+        const int page = off ? 0 : page_next, j0 = begin_of(it) + wave * S::kOwn;
+        const int p = __builtin_amdgcn_readlane(page, wave * S::kOwn);
+        const int64_t base = ((static_cast<int64_t>(p) * c.Hkv + h) * (in_page + 1) + (j0 & in_page)) * Dh;
+#pragma unroll
+        for (int n = 0; n < S::kLoads; ++n) {
+            const int index = n * kWave + lane, key = index / S::kStride;
+            const int at = key * Dh + ((index % S::kStride) ^ permuted<S::kStride>(wave * S::kOwn + key)) * S::kPerPiece;
+            const int to = wave * S::kOwn * S::kStride * 16 + n * kWave * 16;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(k_pool + base + at),
+                                             (__attribute__((address_space(3))) void *)(kt + to), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(v_pool + base + at),
+                                             (__attribute__((address_space(3))) void *)(vt + to), 16, 0, 0);
+        }
+        page_next = page_at(it + 1);
+    };
     const auto whole_tile = [&](int j0, int a, int b) {       // every row from place a to place b sees every key
         return j0 + kKeys - 1 <= a && (c.window == 0 || j0 > b - c.window || j0 + kKeys <= c.sinks);
     };
@@ -168,6 +191,20 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         }
         bad = bad_next;
     };
+    const auto settle = [&](int it) {                         // what fetch() brings is there, and looked at as put() does
+        __builtin_amdgcn_s_waitcnt(kNoVmem);
+        if (!whole_tile(begin_of(it), p0, p1)) {
+            char *const vt = lds + (it & 1) * 2 * S::kBytes + S::kBytes + wave * S::kOwn * S::kStride * 16;
+#pragma unroll
+            for (int n = 0; n < S::kLoads; ++n) {
+                const int index = n * kWave + lane, j = begin_of(it) + wave * S::kOwn + index / S::kStride;
+                v4i *const at = reinterpret_cast<v4i *>(vt + index * 16);
+                if (keys.seen(j) != j) *at = v4i{0, 0, 0, 0};
+                else odd |= not_finite<E>(*at);
+            }
+        }
+        bad = bad_next;
+    };
 
     v16f out[kOut];
 #pragma unroll
@@ -177,14 +214,22 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     float top = -INFINITY, total = 0.0f;
 
     if (steps > 0) {
-        load(0);
-        put(0);
+        if constexpr (kDirect) {
+            fetch(0);
+            settle(0);
+        } else {
+            load(0);
+            put(0);
+        }
     }
     __syncthreads();
     for (int it = 0; it < steps; ++it) {
         const int j0 = begin_of(it);
         const unsigned long long bad_now = bad;
-        if (it + 1 < steps) load(it + 1);
+        if (it + 1 < steps) {
+            if constexpr (kDirect) fetch(it + 1);
+            else load(it + 1);
+        }
         const char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
         const bool none = j0 > w1 || (c.window > 0 && j0 + kKeys - 1 <= w0 - c.window && j0 >= c.sinks);
         if (!none) {
@@ -287,7 +332,10 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                     }
             }
         }
-        if (it + 1 < steps) put(it + 1);
+        if (it + 1 < steps) {
+            if constexpr (kDirect) settle(it + 1);
+            else put(it + 1);
+        }
         __syncthreads();
     }
 
