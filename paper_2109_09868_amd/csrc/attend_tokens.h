@@ -33,9 +33,10 @@ struct TokenShape {
 // A part's sums in the workspace: rows x Dh floats, then 16 maxima (of c S, base 2) and 16 totals.
 __device__ __host__ __forceinline__ int64_t part_floats(int Dh) { return 16 * static_cast<int64_t>(Dh) + 32; }
 
-// parts: workgroups that share a block of rows, each with `chunk` tiles; blocks: blocks of 16 rows of the longest sequence.
+// parts: workgroups that share a block of rows, each with `chunk` tiles; blocks: blocks of 16 rows of the longest sequence; rows: of those
+// 16, as many as there can be.
 struct TokenGrid {
-    int pairs, blocks, parts, chunk;
+    int pairs, blocks, parts, chunk, rows;
 };
 
 template <class E, int DP>
@@ -289,17 +290,22 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     }
 }
 
-// The parts of a row joined: a wave per row.
-template <class E, int DP>
+// The parts of a row joined, always in the same order, eight parts' sums on their way at a time.  kWaves of a workgroup share a row, every
+// kWaves-th part to each: 4 for many parts (one wave and one part after the other took 38 us for 43 parts, a seventh of the call), 1 for a
+// few, where rows are many.
+template <class E, int DP, int kWaves>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall c, TokenGrid g, const float *workspace) {
     typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
-    constexpr int kPerLane = (DP + kWave - 1) / kWave;
+    constexpr int kPerLane = (DP + kWave - 1) / kWave, kAhead = 8;
+    __shared__ float outs[kWaves][kPerLane * kWave], tops[kWaves], totals[kWaves];
     const int lane = lane_id(), group = c.Hq / c.Hkv;
-    const int64_t index = static_cast<int64_t>(blockIdx.x) * 4 + wave_id(), all = static_cast<int64_t>(g.pairs) * g.blocks * S::kRows;
-    if (index >= all) return;
-    const int n = static_cast<int>(index % S::kRows), block = static_cast<int>(index / S::kRows % g.blocks),
-              pair = static_cast<int>(index / S::kRows / g.blocks);
+    const int wave = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id());
+    const int64_t index = kWaves == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave_id() : blockIdx.x;
+    const int n = static_cast<int>(index % g.rows), block = static_cast<int>(index / g.rows % g.blocks);
+    const int64_t pair64 = index / g.rows / g.blocks;
+    if (pair64 >= g.pairs) return;
+    const int pair = static_cast<int>(pair64);
     const Rows rows = rows_of(c.seq, pair / c.Hkv);
     const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(block) * S::kRows, row = first + n;
     if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || row >= row_count) return;
@@ -308,27 +314,71 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall c, TokenGri
     const KeyTiles<S::kKeys> keys(c.window, c.sinks, p0, p1);
     if (keys.steps <= g.chunk) return;                        // written already
     const int parts = (keys.steps + g.chunk - 1) / g.chunk;
-    const float *const base = workspace + (static_cast<int64_t>(pair) * g.blocks + block) * g.parts * part_floats(c.Dh);
-    float top = -INFINITY;
-    for (int p = lane; p < parts; p += kWave) top = fmaxf(top, base[p * part_floats(c.Dh) + 16 * c.Dh + n]);
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float out[kPerLane] = {}, total = 0.0f;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const float *const x = base + p * part_floats(c.Dh);
-        const float m = x[16 * c.Dh + n], f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+    const int64_t stride = part_floats(c.Dh);
+    const float *const base = workspace + (static_cast<int64_t>(pair) * g.blocks + block) * g.parts * stride;
+    float top = -INFINITY, out[kPerLane] = {}, total = 0.0f;
+    for (int from = wave; from < parts; from += kWaves * kWave) {
+        const int p = from + kWaves * lane, count = min((parts - from + kWaves - 1) / kWaves, kWave);
+        const float m = p < parts ? base[p * stride + 16 * c.Dh + n] : -INFINITY;
+        const float l = p < parts ? base[p * stride + 16 * c.Dh + 16 + n] : 0.0f;
+        float most = fmaxf(m, top);
+        for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+        const float shrink = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most);
+        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
         // a part that saw nothing but what is no number has no maximum, and a total that says so
-        total += m == -INFINITY ? x[16 * c.Dh + 16 + n] : f * x[16 * c.Dh + 16 + n];
+        total = total * shrink + (m == -INFINITY ? l : f * l);
+        top = most;
 #pragma unroll
-        for (int k = 0; k < kPerLane; ++k)
-            if (lane + k * kWave < c.Dh) out[k] += f * x[n * c.Dh + lane + k * kWave];
+        for (int k = 0; k < kPerLane; ++k) out[k] *= shrink;
+        for (int i = 0; i < count; i += kAhead) {
+            float x[kAhead][kPerLane], w[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a) {
+                const int j = min(i + a, count - 1);
+                w[a] = i + a < count ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j)) : 0.0f;
+#pragma unroll
+                for (int k = 0; k < kPerLane; ++k)
+                    x[a][k] = lane + k * kWave < c.Dh ? base[(from + kWaves * j) * stride + n * c.Dh + lane + k * kWave] : 0.0f;
+            }
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                for (int k = 0; k < kPerLane; ++k) out[k] += i + a < count ? w[a] * x[a][k] : 0.0f;
+        }
     }
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
     const int64_t t = rows.start + row / group;
     V *const y = static_cast<V *>(c.out) + (t * c.Hq + pair % c.Hkv * group + row % group) * c.Dh;
+    if constexpr (kWaves == 1) {
+        const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
 #pragma unroll
-    for (int k = 0; k < kPerLane; ++k)
-        if (lane + k * kWave < c.Dh) y[lane + k * kWave] = E::store(out[k] * inverse);
+        for (int k = 0; k < kPerLane; ++k)
+            if (lane + k * kWave < c.Dh) y[lane + k * kWave] = E::store(out[k] * inverse);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) outs[wave][lane + k * kWave] = out[k];
+    if (lane == 0) {
+        tops[wave] = top;
+        totals[wave] = total;
+    }
+    __syncthreads();
+    float all = tops[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w]);
+    float sum = 0.0f, f[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        f[w] = tops[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(tops[w] - all);
+        sum += tops[w] == -INFINITY ? totals[w] : f[w] * totals[w];
+    }
+    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int d = threadIdx.x; d < c.Dh; d += 256) {
+        float x = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) x += f[w] * outs[w][d];
+        y[d] = E::store(x * inverse);
+    }
 }
 
 template <class E, int DP>
@@ -338,8 +388,10 @@ hipError_t launch_tokens(const AttendCall &c, const TokenGrid &g, float *workspa
     const int64_t blocks = work + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
     hipError_t e = launch_kernel(attend_tokens_kernel<E, DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
     if (e == hipSuccess && g.parts > 1) {
-        const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * S::kRows;
-        e = launch_kernel(attend_join_kernel<E, DP>, dim3(static_cast<unsigned>((all + 3) / 4)), dim3(256), 0, stream, c, g,
+        const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * g.rows;
+        const bool many = g.parts > 8;
+        e = launch_kernel(many ? attend_join_kernel<E, DP, 4> : attend_join_kernel<E, DP, 1>,
+                          dim3(static_cast<unsigned>(many ? all : (all + 3) / 4)), dim3(256), 0, stream, c, g,
                           static_cast<const float *>(workspace));
     }
     return e;
