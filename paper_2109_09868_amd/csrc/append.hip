@@ -5,6 +5,8 @@ namespace approxifer {
 
 namespace {
 
+constexpr int64_t kLastLevelCache = 256 << 20;
+
 // Rotation of the head: frequencies in turns per position (so that an angle is reduced by dropping whole turns, exactly, in
 // float64), and the axis that each pair's position is read from.
 struct Rotation {
@@ -44,34 +46,25 @@ __device__ __forceinline__ float lanes_sum(float v) {
     return v;
 }
 
-// The sequence of each lane's token t, for tokens that rise with the lane from the wave's first: 64 starts at a time are compared at
-// once, so that the common cases take one or two loads where bisection takes one for every doubling of B.
-__device__ __forceinline__ int sequences_of(const Sequences &s, int64_t t, int lanes) {
-    const int lane = lane_id();
-    const int64_t t0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(t)));
-    int lo = 0, span = s.B;                                   // the first token's sequence is in lo .. lo + span - 1
-    while (span > kWave) {
-        const int step = (span + kWave - 1) / kWave, at = lo + lane * step;
-        const unsigned long long before = __ballot(lane * step < span && s.starts[at] <= t0);
-        const int k = max(__popcll(before) - 1, 0);
-        const int next = lo + k * step;
-        span = min(step, lo + span - next);
-        lo = next;
+// The same for groups of any length: every lane adds the others of its group.
+__device__ __forceinline__ float group_sum(float v, int begin, int at, int L) {
+    float sum = v;
+    for (int o = 1; o < L; ++o) sum += __shfl(v, begin + (at + o < L ? at + o : at + o - L));
+    return sum;
+}
+
+// The sequence of the wave's token t: 64 starts are compared at once, so that the common cases take one load where bisection takes one
+// for every doubling of B.
+__device__ __forceinline__ int wave_sequence_of(const Sequences &s, int64_t t) {
+    int lo = 0, span = s.B;
+    while (span > 1) {
+        const int step = (span + kWave - 1) / kWave, k = lane_id() * step;
+        const unsigned long long before = __ballot(k < span && s.starts[lo + k] <= t);
+        const int last = before != 0 ? (63 - __clzll(before)) * step : 0;
+        span = min(step, span - last);
+        lo += last;
     }
-    const int at = lo + 1 + lane;                             // the wave's other tokens: mostly within 64 sequences from there
-    const int start = at <= s.B ? s.starts[at] : 0x7fffffff;
-    int b = lo;
-    bool far = false;
-    for (int g = 0; g < kWave; g += lanes) {
-        const int tg = __builtin_amdgcn_readlane(static_cast<int>(t), g);
-        const int passed = __popcll(__ballot(start <= tg));
-        if (lane >= g) {
-            b = lo + passed;
-            far = passed == kWave;
-        }
-    }
-    if (far) b = sequence_of(s, t);
-    return min(b, s.B - 1);
+    return lo;
 }
 
 __device__ __forceinline__ void append_status(const AppendCall &c, int b) {
@@ -84,26 +77,27 @@ __device__ __forceinline__ void append_status(const AppendCall &c, int b) {
 typedef int v4i __attribute__((ext_vector_type(4)));
 
 // Heads in pieces of 16 bytes, HBM-bound: every value is read once and written once.
-// L lanes share a head, two pieces each: those whose values are rotated with each other, piece u and the one pairs further (neighbours are
-// rotated: pieces 2 u and 2 u + 1), so that a rotation stays in the lane.  A group of lanes has one token and `per` of its heads one
-// after the other, so that cosine and sine of its pairs (float64 reduction, about 80 instructions each) are computed once for all of them.
-// Heads go in fours whose loads are in flight together.
-template <class E, int L>
-__global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotation rot, int per, int slices) {
+// A wave has one token and `per` of its heads.  `lanes` lanes (kLanes, or any number where that is 0) share a head, two pieces each: those
+// whose values are rotated with each other, piece u and the one `pairs` further (neighbours are rotated: pieces 2 u and 2 u + 1), so that a
+// rotation stays in the lane.  Heads that lie next to each other are read and written together, and all of kSteps rounds' loads are on
+// their way while cosines and sines (float64 reduction, about 80 instructions each) are computed, once for the token, a pair per lane.
+// kStream: a call that moves more than the last-level cache holds does not pass its stores through it.
+template <class E, int kLanes, bool kStream>
+__global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotation rot, int lanes, int per, int slices) {
     typedef typename E::Value V;
-    constexpr int kPer = 16 / sizeof(V), kGroups = kWave / L, kHeads = 4;
+    constexpr int kPer = 16 / sizeof(V), kSteps = 2;
     typedef V VP __attribute__((ext_vector_type(16 / sizeof(V))));
-    const int lane = lane_id(), u = lane % L;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + wave_id();
-    const int64_t work = (c.seq.T + kGroups - 1) / kGroups * slices;
+    __shared__ __align__(16) float turns[4][2][APPROXIFER_MAX_HEAD_DIM / 2];
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id());
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + wave, work = c.seq.T * slices;
     if (unit >= work) {                                       // the last waves: statuses
         const int64_t b = unit - work;
         if (c.status != nullptr && b < c.seq.B) append_status(c, static_cast<int>(b));
         return;
     }
-    const int slice = static_cast<int>(unit % slices);
-    const int64_t t_raw = unit / slices * kGroups + lane / L, t = min(t_raw, c.seq.T - 1);
-    const int h0 = slice * per, h1 = min(h0 + per, c.Hq + 2 * c.Hkv);
+    const int L = kLanes > 0 ? kLanes : lanes, groups = kWave / L, group = lane / L, u = lane - group * L;
+    const int64_t t = unit / slices;
+    const int h0 = static_cast<int>(unit % slices) * per, h1 = min(h0 + per, c.Hq + 2 * c.Hkv);
 
     // this lane's two pieces
     const int pieces = c.Dh / kPer, apart = c.interleaved ? 0 : c.pairs / kPer;
@@ -115,47 +109,44 @@ __global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotati
         a = 2 * apart + 2 * (u - apart);
         b = a + 1;
     }
-    const bool has_a = a < pieces, has_b = b < pieces;
+    const bool has_a = a < pieces && group < groups, has_b = b < pieces && group < groups;
     const int at_a = (has_a ? a : 0) * kPer, at_b = (has_b ? b : 0) * kPer;
 
-    const auto source = [&](int h) {
-        return h < c.Hq           ? static_cast<const V *>(c.q) + t * c.q_stride + static_cast<int64_t>(h) * c.Dh
-               : h < c.Hq + c.Hkv ? static_cast<const V *>(c.k) + t * c.k_stride + static_cast<int64_t>(h - c.Hq) * c.Dh
-                                  : static_cast<const V *>(c.v) + t * c.v_stride + static_cast<int64_t>(h - c.Hq - c.Hkv) * c.Dh;
-    };
-    VP xa[kHeads], xb[kHeads];
+    VP xa[kSteps], xb[kSteps];
     const auto load = [&](int h) {
 #pragma unroll
-        for (int n = 0; n < kHeads; ++n) {
-            const V *x = source(min(h + n, h1 - 1));
+        for (int n = 0; n < kSteps; ++n) {
+            const int head = min(h + n * groups + group, h1 - 1);
+            const V *x = head < c.Hq           ? static_cast<const V *>(c.q) + t * c.q_stride + static_cast<int64_t>(head) * c.Dh
+                         : head < c.Hq + c.Hkv ? static_cast<const V *>(c.k) + t * c.k_stride + static_cast<int64_t>(head - c.Hq) * c.Dh
+                                               : static_cast<const V *>(c.v) + t * c.v_stride + static_cast<int64_t>(head - c.Hq - c.Hkv) * c.Dh;
             xa[n] = *reinterpret_cast<const VP *>(x + at_a);
             xb[n] = *reinterpret_cast<const VP *>(x + at_b);
         }
     };
-    load(h0);                                                 // on their way while the rest is looked up
+    load(h0);
 
-    const int seq = sequences_of(c.seq, t, L);
+    const int seq = wave_sequence_of(c.seq, t);
     const Rows r = rows_of(c.seq, seq);
-    const bool mine = t_raw < c.seq.T && r.ok && t >= r.start && t < r.start + r.n;
+    if (!r.ok || t < r.start || t >= r.start + r.n) return;
     const int place = r.place(static_cast<int>(t - r.start));
-    int page = -1;
-    if (mine && place >= 0 && h1 > c.Hq) page = page_of(c.seq, seq, place);
+    const int page = place >= 0 && h1 > c.Hq ? page_of(c.seq, seq, place) : -1;
     const int size = 1 << c.seq.page_shift;
     const int64_t slot = static_cast<int64_t>(page) * c.Hkv * size + (place & (size - 1));
 
     float cs[kPer], sn[kPer];
-    bool turned[kPer];
-    if (h0 < c.Hq + c.Hkv) {
+    if (h0 < c.Hq + c.Hkv && c.pairs > 0) {
+        for (int i = lane; i < c.pairs; i += kWave) {
+            const int position = c.positions != nullptr ? c.positions[t * c.axes + rot.axis[i]] : place;
+            angle_of(rot, i, position, &turns[wave][0][i], &turns[wave][1][i]);
+        }
+        __builtin_amdgcn_wave_barrier();
+        __threadfence_block();
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
-            const int i = u * kPer + k;
-            turned[k] = i < c.pairs && (c.interleaved || u < apart);
-            cs[k] = 1.0f;
-            sn[k] = 0.0f;
-            if (turned[k]) {
-                const int position = c.positions != nullptr ? c.positions[t * c.axes + rot.axis[i]] : place;
-                angle_of(rot, i, position, &cs[k], &sn[k]);
-            }
+            const int i = min(u * kPer + k, c.pairs - 1);
+            cs[k] = turns[wave][0][i];
+            sn[k] = turns[wave][1][i];
         }
     }
     float wq[2][kPer], wk[2][kPer];
@@ -174,38 +165,41 @@ __global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotati
         }
     }
 
-    for (int h = h0; h < h1; h += kHeads) {
-        VP ya[kHeads], yb[kHeads];
+    for (int h = h0; h < h1; h += kSteps * groups) {
+        VP ya[kSteps], yb[kSteps];
 #pragma unroll
-        for (int n = 0; n < kHeads; ++n) {
+        for (int n = 0; n < kSteps; ++n) {
             ya[n] = xa[n];
             yb[n] = xb[n];
         }
-        if (h + kHeads < h1) load(h + kHeads);
+        if (h + kSteps * groups < h1) load(h + kSteps * groups);
 #pragma unroll
-        for (int n = 0; n < kHeads; ++n) {
-            const int head = h + n;
-            if (head >= h1) break;
+        for (int n = 0; n < kSteps; ++n) {
+            if (h + n * groups >= h1) break;
+            const int head = h + n * groups + group;
             const bool is_q = head < c.Hq, is_v = head >= c.Hq + c.Hkv;
             VP za = ya[n], zb = yb[n];
-            if (!is_v) {
+            if (h + n * groups < c.Hq + c.Hkv) {              // not values only
                 float p[kPer], q[kPer];
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) {
                     p[k] = E::load(za[k]);
                     q[k] = E::load(zb[k]);
                 }
-                if ((is_q ? c.q_weight : c.k_weight) != nullptr) {
+                if (c.q_weight != nullptr || c.k_weight != nullptr) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int k = 0; k < kPer; ++k) sum += has_a ? p[k] * p[k] : 0.0f;
 #pragma unroll
                     for (int k = 0; k < kPer; ++k) sum += has_b ? q[k] * q[k] : 0.0f;
-                    const float scale = 1.0f / sqrtf(lanes_sum<L>(sum) / c.Dh + c.eps);
+                    const float all = kLanes > 0 ? lanes_sum<kLanes>(sum) : group_sum(sum, group * L, u, L);
+                    if ((is_q ? c.q_weight : c.k_weight) != nullptr) {
+                        const float scale = 1.0f / sqrtf(all / c.Dh + c.eps);
 #pragma unroll
-                    for (int k = 0; k < kPer; ++k) {
-                        p[k] *= scale * (is_q ? wq[0][k] : wk[0][k]);
-                        q[k] *= scale * (is_q ? wq[1][k] : wk[1][k]);
+                        for (int k = 0; k < kPer; ++k) {
+                            p[k] *= scale * (is_q ? wq[0][k] : wk[0][k]);
+                            q[k] *= scale * (is_q ? wq[1][k] : wk[1][k]);
+                        }
                     }
                 }
                 if (c.interleaved) {
@@ -213,8 +207,9 @@ __global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotati
                     for (int k = 0; k < kPer; ++k) {          // pair u kPer + k: in the first piece, then in the second
                         float &f = k < kPer / 2 ? p[2 * k] : q[2 * k - kPer], &g = k < kPer / 2 ? p[2 * k + 1] : q[2 * k - kPer + 1];
                         const float x = f, y = g;
-                        f = turned[k] ? x * cs[k] - y * sn[k] : x;
-                        g = turned[k] ? x * sn[k] + y * cs[k] : y;
+                        const bool turned = u * kPer + k < c.pairs;
+                        f = turned ? x * cs[k] - y * sn[k] : x;
+                        g = turned ? x * sn[k] + y * cs[k] : y;
                     }
                 } else if (u < apart) {
 #pragma unroll
@@ -224,20 +219,27 @@ __global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotati
                         q[k] = x * sn[k] + y * cs[k];
                     }
                 }
+                if (!is_v) {
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    za[k] = E::store(p[k]);
-                    zb[k] = E::store(q[k]);
+                    for (int k = 0; k < kPer; ++k) {
+                        za[k] = E::store(p[k]);
+                        zb[k] = E::store(q[k]);
+                    }
                 }
             }
+            if (head >= h1) continue;
             V *y = nullptr;
             if (is_q) {
-                if (mine) y = static_cast<V *>(c.q_out) + (t * c.Hq + head) * c.Dh;
+                y = static_cast<V *>(c.q_out) + (t * c.Hq + head) * c.Dh;
             } else if (page >= 0) {
                 const int kv = head - (is_v ? c.Hq + c.Hkv : c.Hq);
                 y = static_cast<V *>(is_v ? c.v_pool : c.k_pool) + (slot + static_cast<int64_t>(kv) * size) * c.Dh;
             }
-            if (y != nullptr) {
+            if (y == nullptr) continue;
+            if constexpr (kStream) {
+                if (has_a) __builtin_nontemporal_store(za, reinterpret_cast<VP *>(y + at_a));
+                if (has_b) __builtin_nontemporal_store(zb, reinterpret_cast<VP *>(y + at_b));
+            } else {
                 if (has_a) *reinterpret_cast<VP *>(y + at_a) = za;
                 if (has_b) *reinterpret_cast<VP *>(y + at_b) = zb;
             }
@@ -245,27 +247,31 @@ __global__ __launch_bounds__(256) void append_pieces_kernel(AppendCall c, Rotati
     }
 }
 
-template <class E, int L>
-hipError_t launch_pieces(const AppendCall &c, const Rotation &rot, hipStream_t stream) {
-    const int heads = c.Hq + 2 * c.Hkv;
-    const int64_t waves = (c.seq.T + kWave / L - 1) / (kWave / L);
-    // enough waves to fill the GPU four deep, a head each at the least; then whole tokens, whose angles are computed once
-    const int64_t most = (4096 + waves - 1) / waves;
-    const int slices_wanted = static_cast<int>(most < heads ? most : heads), per = (heads + slices_wanted - 1) / slices_wanted;
-    const int slices = (heads + per - 1) / per;
-    const int64_t units = waves * slices + (c.status != nullptr ? c.seq.B : 0);
-    return launch_kernel(append_pieces_kernel<E, L>, dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, stream, c, rot, per,
-                         slices);
+template <class E, int kLanes>
+hipError_t launch_pieces(const AppendCall &c, const Rotation &rot, int lanes, hipStream_t stream) {
+    const int heads = c.Hq + 2 * c.Hkv, groups = kWave / lanes;
+    // enough waves to fill the GPU, `groups` heads each at the least; beyond that whole tokens
+    int64_t slices = (8192 + c.seq.T - 1) / (c.seq.T > 0 ? c.seq.T : 1);
+    const int most = (heads + groups - 1) / groups;
+    slices = slices < most ? slices : most;
+    const int per = static_cast<int>(((heads + slices - 1) / slices + groups - 1) / groups * groups);
+    slices = (heads + per - 1) / per;
+    const int64_t units = c.seq.T * slices + (c.status != nullptr ? c.seq.B : 0);
+    const int64_t bytes = 2 * c.seq.T * heads * c.Dh * static_cast<int64_t>(sizeof(typename E::Value));
+    return launch_kernel(bytes > kLastLevelCache ? append_pieces_kernel<E, kLanes, true> : append_pieces_kernel<E, kLanes, false>,
+                         dim3(static_cast<unsigned>((units + 3) / 4)), dim3(256), 0, stream, c, rot, lanes, per, static_cast<int>(slices));
 }
 template <class E>
 hipError_t launch_pieces_of(const AppendCall &c, const Rotation &rot, hipStream_t stream) {
     constexpr int kPer = 16 / sizeof(typename E::Value);
-    const int pieces = c.Dh / kPer, apart = c.interleaved ? 0 : c.pairs / kPer, units = apart + (pieces - 2 * apart + 1) / 2;
-    if (units <= 2) return launch_pieces<E, 2>(c, rot, stream);
-    if (units <= 4) return launch_pieces<E, 4>(c, rot, stream);
-    if (units <= 8) return launch_pieces<E, 8>(c, rot, stream);
-    if (units <= 16) return launch_pieces<E, 16>(c, rot, stream);
-    return launch_pieces<E, 32>(c, rot, stream);
+    const int pieces = c.Dh / kPer, apart = c.interleaved ? 0 : c.pairs / kPer, lanes = apart + (pieces - 2 * apart + 1) / 2;
+    switch (lanes) {
+        case 4: return launch_pieces<E, 4>(c, rot, lanes, stream);
+        case 8: return launch_pieces<E, 8>(c, rot, lanes, stream);
+        case 16: return launch_pieces<E, 16>(c, rot, lanes, stream);
+        case 32: return launch_pieces<E, 32>(c, rot, lanes, stream);
+        default: return launch_pieces<E, 0>(c, rot, lanes, stream);
+    }
 }
 
 // Heads element by element, for rows that do not begin at 16 bytes and halves that are no whole pieces.  One wave per head of a token: queries,
