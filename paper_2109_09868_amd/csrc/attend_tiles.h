@@ -26,7 +26,10 @@ struct TileShape {
     static constexpr int kPerPiece = 16 / kSize;              // elements of 16 bytes
     static constexpr int kPieces = DP * kSize / 16;           // of a row
     static constexpr int kStride = pow2_at_least(kPieces);    // pieces between rows in LDS
-    static constexpr int kKeys = kStride * 16 > 512 || DP > 128 ? 32 : 64;
+    // 32 keys a tile where 64 take too much LDS or too many registers, and for short 32-bit heads, where three workgroups share a CU so
+    // (192 sequences of 128 tokens, 12 heads of 64: 110 us, 125 with 64 keys and two workgroups)
+    static constexpr bool kShort = kSize == 4 && DP == 64;
+    static constexpr int kKeys = kStride * 16 > 512 || DP > 128 || kShort ? 32 : 64;
     static constexpr int kWaves = 4;
     static constexpr int kRows = 32 * kWaves;
     static constexpr int kThreads = 64 * kWaves;
@@ -35,7 +38,7 @@ struct TileShape {
     static constexpr int kBytes = kKeys * kStride * 16;       // of one operand's tile
     static constexpr int kLds = 4 * kBytes;
     static constexpr int kAhead = 6;                          // operands in flight
-    static constexpr int kGroups = kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
+    static constexpr int kGroups = kShort ? 3 : kLds <= 80 * 1024 && DP <= 128 ? 2 : 1; // workgroups that share a CU
     static_assert(kOwn * kPieces % kWave == 0, "whole pieces per lane");
     static __device__ __forceinline__ int at(int row, int piece) { return piece_at<kStride>(row, piece); }
 };
