@@ -36,17 +36,27 @@ __device__ __forceinline__ T block_scan(T v, T *sums, T *total) {
 }
 
 // The first `most` (at most kList) free pages from *cursor on, ascending, into list; how many there are.  Afterwards *cursor is
-// where to go on once those have been taken.  By the whole workgroup of kThreads.
-__device__ int find_free(const int32_t *refs, int P, int most, int *list, int *sums, int *cursor) {
+// where to go on once those have been taken.  By the whole workgroup of kThreads.  `ahead` holds the stretch's refs: those of the
+// cursor on entry.
+struct Stretch {
+    int32_t refs[4];
+    __device__ __forceinline__ void load(const int32_t *from, int at, int P) {
+        const int p = at + 4 * static_cast<int>(threadIdx.x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) refs[k] = p + k < P ? from[p + k] : 1;
+    }
+};
+__device__ __forceinline__ int find_free(const int32_t *refs, int P, int most, int *list, int *sums, int *cursor, Stretch ahead) {
     int found = 0, at = *cursor;
     while (found < most && at < P) {
         const int p0 = at + 4 * static_cast<int>(threadIdx.x);
         bool is_free[4];
         int count = 0;
         for (int k = 0; k < 4; ++k) {
-            is_free[k] = p0 + k < P && refs[p0 + k] == 0;
+            is_free[k] = ahead.refs[k] == 0;
             count += is_free[k];
         }
+        ahead.load(refs, at + 4 * kThreads, P);
         int total;
         int rank = found + block_scan(count, sums, &total);
         for (int k = 0; k < 4; ++k)
@@ -93,9 +103,13 @@ __global__ __launch_bounds__(kThreads) void cache_reserve_kernel(int32_t *table,
     __shared__ int sums[16];
     __shared__ long long wide_sums[16];                       // wishes of 1024 sequences may pass 2^31 together
     long long wanted = 0;
+    Stretch ahead;
+    ahead.load(refs, 0, P);                                   // on its way while the sequences are looked at
+    Wish mine{0, 0, 0, 0};                                    // of the first 1024 sequences: not looked up again
     for (int b0 = 0; b0 < B; b0 += kThreads) {
         const int b = b0 + threadIdx.x;
         const Wish w = b < B ? wish_of(table, lens, refs, add, b, M, P, shift) : Wish{0, 0, 0, 0};
+        if (b0 == 0) mine = w;
         long long total;
         block_scan<long long>(w.pages, wide_sums, &total);
         wanted += total;
@@ -113,14 +127,15 @@ __global__ __launch_bounds__(kThreads) void cache_reserve_kernel(int32_t *table,
     }
     int from = 0;                                             // pages given out in the rounds before
     do {
-        const int found = find_free(refs, P, min(most - from, kList), list, sums, &cursor);
+        const int found = find_free(refs, P, min(most - from, kList), list, sums, &cursor, ahead);
         if (most <= kList) available = found;
         const bool last = from + found >= available;
         long long upto = 0;
         for (int b0 = 0; b0 < B; b0 += kThreads) {
             const int b = b0 + threadIdx.x;
             Wish w{0, 0, 0, 0};
-            if (b < B) w = wish_of(table, lens, refs, add, b, M, P, shift);
+            if (b0 == 0) w = mine;
+            else if (b < B) w = wish_of(table, lens, refs, add, b, M, P, shift);
             long long total;
             const long long start = upto + block_scan<long long>(w.pages, wide_sums, &total);
             upto += total;
@@ -142,6 +157,7 @@ __global__ __launch_bounds__(kThreads) void cache_reserve_kernel(int32_t *table,
         from += found;
         if (last) break;
         __syncthreads();
+        ahead.load(refs, cursor, P);
     } while (true);
 }
 
@@ -240,7 +256,9 @@ __global__ __launch_bounds__(kThreads) void fork_pages_kernel(int32_t *table_out
     __syncthreads();
     int cursor = 0, from = 0;
     while (true) {
-        const int found = find_free(refs_out, P, min(wanted - from, kList), list, sums, &cursor);
+        Stretch ahead;
+        ahead.load(refs_out, cursor, P);
+        const int found = find_free(refs_out, P, min(wanted - from, kList), list, sums, &cursor, ahead);
         const bool last = from + found >= wanted || found < kList;
         int upto = 0;
         for (int i0 = 0; i0 < B_out; i0 += kThreads) {
