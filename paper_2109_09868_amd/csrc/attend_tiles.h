@@ -68,6 +68,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     typedef TileShape<E, DP> S;
     constexpr bool kDirect = kWhole && !kSmall && S::kStride == S::kPieces;
     constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
+    constexpr int kVec = S::kSize == 2 ? 1 : kOut % 4 == 0 ? 4 : kOut % 2 == 0 ? 2 : 1;
     __shared__ __align__(16) char lds[S::kLds];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
     const int64_t work = slots * c.Hkv;
@@ -253,18 +254,31 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                 __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
             }
             __builtin_amdgcn_sched_group_barrier(kMfma, S::kAhead * (S::kSize == 4 ? 4 : 1), 0);
-            const bool masked = !whole_tile(j0, w0, w1) || bad_now != 0;
-            if (masked) {
-                const int reach = place - j0 - 4 * half, start = c.sinks - j0 - 4 * half;
+            // what is hidden from a row: keys behind it, keys before its window; and keys of bad pages are no numbers.  Few tiles need any
+            // of it, and hardly one needs all.
+            const int reach = place - j0 - 4 * half;
+            if (bad_now != 0) {
                 const unsigned long long off = bad_now >> (4 * half);
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (off >> (b * 32 + 8 * (k / 4) + k % 4) & 1) s[b][k] = NAN;
+            }
+            if (j0 + kKeys - 1 > w0) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[b][k] = b * 32 + 8 * (k / 4) + k % 4 <= reach ? s[b][k] : -INFINITY;
+            }
+            if (c.window != 0 && j0 <= w1 - c.window && j0 + kKeys > c.sinks) {
+                const int start = c.sinks - j0 - 4 * half, back = reach - c.window;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         const int key = b * 32 + 8 * (k / 4) + k % 4;
-                        const bool sees = key <= reach && (c.window == 0 || key > reach - c.window || key < start);
-                        if (off >> key & 1) s[b][k] = NAN;
-                        s[b][k] = sees ? s[b][k] : -INFINITY;
+                        s[b][k] = key > back || key < start ? s[b][k] : -INFINITY;
                     }
             }
             float most = s[0][0];
@@ -322,15 +336,21 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                     __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
                 }
             } else {
+                // a lane reads kVec neighbouring values of a key at once: they are its operands of kVec products, whose rows are every
+                // kVec-th dimension
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) {
                         const int key = b * 32 + 8 * (k / 4) + 4 * half + k % 4;
 #pragma unroll
-                        for (int o = 0; o < kOut; ++o) {
-                            const float x = *reinterpret_cast<const float *>(vt + S::at(key, 8 * o + (row32 >> 2)) + (row32 & 3) * 4);
-                            out[o] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[b][k], out[o], 0, 0, 0);
+                        for (int o = 0; o < kOut; o += kVec) {
+                            typedef float VV __attribute__((ext_vector_type(kVec)));
+                            const int at = 32 * o + kVec * row32;
+                            const VV x = *reinterpret_cast<const VV *>(vt + S::at(key, at >> 2) + (at & 3) * 4);
+#pragma unroll
+                            for (int e = 0; e < kVec; ++e)
+                                out[o + e] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], s[b][k], out[o + e], 0, 0, 0);
                         }
                     }
             }
@@ -363,14 +383,15 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     if (first + wave * 32 + row32 < row_count) {
         V *y = static_cast<V *>(c.out) + ((rows.start + token) * c.Hq + head) * c.Dh;
 #pragma unroll
-        for (int o = 0; o < kOut; ++o)
+        for (int o = 0; o < kOut; o += kVec)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int d = 32 * o + 8 * k + 4 * half;
-                if (kWhole || d < c.Dh)
-                    store4<E>(y + d, out[o][4 * k] * inverse, out[o][4 * k + 1] * inverse, out[o][4 * k + 2] * inverse,
-                              out[o][4 * k + 3] * inverse);
-            }
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {              // values 4 j ..+3 of the 4 kVec that lie next to each other
+                    const int d = 32 * o + kVec * (8 * k + 4 * half) + 4 * j;
+                    const auto value = [&](int n) { return out[o + (4 * j + n) % kVec][4 * k + (4 * j + n) / kVec] * inverse; };
+                    if (kWhole || d < c.Dh) store4<E>(y + d, value(0), value(1), value(2), value(3));
+                }
     }
 }
 
