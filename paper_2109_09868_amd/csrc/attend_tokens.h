@@ -186,7 +186,14 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
             }
         if constexpr (S::kSize == 2) {
             const float w[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
+            // weights in two 16-bit pieces, what the first leaves in the second: the products wait for memory anyway, and the result is
+            // as exact as its own rounding
+            typedef V V8 __attribute__((ext_vector_type(8)));
             const v4i p = rounded8<E>(w);
+            float rest[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) rest[k] = w[k] - E::load(__builtin_bit_cast(V8, p)[k]);
+            const v4i p2 = rounded8<E>(rest);
 #pragma unroll
             for (int o = 0; o < kOut; ++o) {
                 v4s x[2];
@@ -196,6 +203,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
                                            (row16 & 1) * 8);
                 const v8s y = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
                 out[o] = multiply16<E>(__builtin_bit_cast(v4i, y), p, out[o]);
+                out[o] = multiply16<E>(__builtin_bit_cast(v4i, y), p2, out[o]);
             }
         } else {
 #pragma unroll
