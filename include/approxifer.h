@@ -336,13 +336,14 @@ int approxifer_wait_mask(const float *d_arrival, uint8_t *d_mask, int32_t *d_cou
  * All sizes and indices that the device holds are checked there before they are used; what is wrong with a sequence
  * is told in d_status [B] (int32, written, or NULL), and a bad sequence does not disturb the others:
  *   APPROXIFER_GROUP_OK
- *   APPROXIFER_SEQUENCE_BAD        its rows lie outside 0 .. T, or its length outside 0 .. M page: nothing is written
+ *   APPROXIFER_SEQUENCE_BAD        its rows lie outside 0 .. T, or its length outside 0 .. M page: nothing is written.  (starts
+ *                                  must not fall: where it does, rows of other sequences may stay unwritten too.)
  *   APPROXIFER_SEQUENCE_BAD_PAGE   a table entry that the call needs is not in 0 .. P - 1: see the calls
  *   APPROXIFER_SEQUENCE_NO_PAGES, APPROXIFER_SEQUENCE_SHARED_PAGE   see the calls that take pages
  *
  * Sizes: page a power of two up to 4096; Dh a multiple of 8 up to 256; Hq a multiple of Hkv, Hq <= 1024; T up to 2^24, B up
- * to 2^20, P and M page below 2^31 (pools may be larger than that), M and P at least 1.  APPROXIFER_ERR_BAD_CACHE,
- * or APPROXIFER_ERR_LIMIT for sizes that are merely too large.
+ * to 2^20, T Hq up to 2^30, B Hkv up to 2^22, P and M page below 2^31 (pools may be larger than that), M and P at least 1.
+ * APPROXIFER_ERR_BAD_CACHE, or APPROXIFER_ERR_LIMIT for sizes that are merely too large.
  */
 #define APPROXIFER_F32 0
 #define APPROXIFER_F16 1
@@ -408,7 +409,7 @@ int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
  *     out = sum_j softmax_j(scale q . k_j) v_j   over the visible places j <= t:
  *           all of them if window = 0, else those with j > t - window or j < sinks.
  * A row that sees nothing (its place is negative) gets zeros.  What a row does not see has no effect on it, whatever it
- * holds (infinities and NaN included); what lies behind a sequence's length is never read.
+ * holds (infinities and NaN included); neither has what lies behind a sequence's length.
  *
  *   d_q     [T][Hq][Dh], tokens q_stride values apart, read only;  d_out [T][Hq][Dh] written, contiguous, 16-byte aligned,
  *           must not overlap d_q
@@ -419,8 +420,9 @@ int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
  *           approxifer_decode_byzantine(): long sequences with few rows are split over the GPU, and the parts meet there.
  *           approxifer_attend_workspace_bytes() gives the size with which the call is fastest; with less it is split
  *           less, and as correct.
- * Rows that see a place in a bad page are NaN.  Scores, softmax and sums are float32 (for 16-bit types the weights are
- * rounded to the type before they multiply the values); each output is rounded once.
+ * Rows that see a place in a bad page are NaN.  Scores, softmax and sums are float32; for 16-bit types the weights are
+ * rounded before they multiply the values, for many rows to the type, for few (up to 16 of a sequence and head of the
+ * cache) to twice its length.  Each output is rounded once.
  * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE, ERR_BAD_CACHE, ERR_LIMIT, ERR_BAD_DTYPE, ERR_ALIGNMENT or ERR_LAUNCH; the
  * call may consist of two launches.
  */

@@ -58,6 +58,7 @@ int check_sequences(const approxifer_sequences *h, int Hq, int Hkv, int Dh, int 
     const int rc = check_cache(h->B, h->M, h->P, h->page, &shift);
     if (rc != APPROXIFER_OK) return rc;
     if (h->T > APPROXIFER_MAX_ROWS || Hq > APPROXIFER_MAX_HEADS || Dh > APPROXIFER_MAX_HEAD_DIM) return APPROXIFER_ERR_LIMIT;
+    if (h->T * Hq > (1LL << 30) || h->B * Hkv > (1LL << 22)) return APPROXIFER_ERR_LIMIT;    // workgroups of one launch
     *s = approxifer::Sequences{h->d_table, h->d_lens, h->d_starts, h->T, static_cast<int>(h->B), static_cast<int>(h->M),
                                static_cast<int>(h->P), shift};
     return APPROXIFER_OK;
@@ -356,7 +357,8 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
                                          int64_t window, int64_t sinks) {
     if (T < 1 || T > APPROXIFER_MAX_ROWS || B < 1 || B > APPROXIFER_MAX_SEQUENCES || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 ||
         Hq > APPROXIFER_MAX_HEADS || Dh < 1 || Dh % 8 != 0 || Dh > APPROXIFER_MAX_HEAD_DIM || dtype < APPROXIFER_F32 ||
-        dtype > APPROXIFER_BF16 || max_rows < 1 || max_len < 1 || window < 0 || sinks < 0)
+        dtype > APPROXIFER_BF16 || max_rows < 1 || max_len < 1 || window < 0 || sinks < 0 || T * Hq > (1LL << 30) ||
+        B * Hkv > (1LL << 22))
         return 0;
     return approxifer::attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
 }

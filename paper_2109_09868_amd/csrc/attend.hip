@@ -6,7 +6,11 @@ namespace approxifer {
 
 namespace {
 
-constexpr int kTokenRows = 32;                                // most rows of a sequence and head that the tokens kernel takes
+// Most rows of a sequence and cache head that the tokens kernel takes: more are read again for every 16, and the tiles kernel's products are
+// the better ones for them.  8 tokens by 4 heads (32 rows) of 8 sequences of up to 40000 keys: 284 us here, 186 there; 32-bit products cost
+// more than memory does, whichever kernel forms them, and the tiles kernel's 128 rows are mostly empty: 16 tokens (64 rows) of up to 6000
+// keys 108 us here, 121 there.
+int token_rows(int dtype) { return dtype == APPROXIFER_F32 ? 64 : 16; }
 // Workgroups that it is given if keys are cut: two on every CU, in one round.  With 256 / 512 / 768 / 1024 / 2048 three sequences of up to
 // 131072 keys take 258 / 244 / 257 / 257 / 255 us.
 constexpr int64_t kTokenGroups = 512;
@@ -23,7 +27,7 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     }
     int64_t parts = kTokenGroups / (pairs * blocks > 0 ? pairs * blocks : 1);
     parts = parts < (tiles + 7) / 8 ? parts : (tiles + 7) / 8;           // two tiles a wave at least
-    const int64_t room = static_cast<int64_t>(workspace_bytes) / (pairs * blocks * part_floats(Dh) * 4 + 1);
+    const int64_t room = static_cast<int64_t>(workspace_bytes) / (pairs * blocks * part_floats(16, Dh) * 4 + 1);
     parts = parts < room ? parts : room;
     TokenGrid g;
     g.pairs = static_cast<int>(pairs);
@@ -39,24 +43,56 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     return g;
 }
 
+// Workgroups that the tiles kernel is given if keys are cut, again two on every CU, and fewest tiles of 64 keys in a part.  With 512 / 768 /
+// 1024: 16 tokens of 4 sequences of up to 40000 keys 106 / 136 / 118 us, 64 of 60000 keys 107 / 101 / 118, 512 of 60000 612 / 635 / 579.
+constexpr int64_t kTileGroups = 512, kTileChunk = 8;
+
+TileGrid tile_grid(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
+                   size_t workspace_bytes) {
+    const int64_t group = Hq / Hkv;
+    TileGrid g;
+    g.single = max_rows * group <= kTileRows;                 // a tile for each sequence
+    g.slots = g.single ? B : T * group / kTileRows + B;
+    int64_t tiles = (max_len + 63) / 64;
+    if (window > 0) {                                         // no tile of rows sees more
+        const int64_t most = (sinks + 63) / 64 + (window + kTileRows) / 64 + 2;
+        tiles = tiles < most ? tiles : most;
+    }
+    // half of the tiles that only make up a sequence's number can be empty
+    const int64_t heads = (g.single ? B : T * group / kTileRows + (B + 1) / 2) * Hkv;
+    int64_t parts = kTileGroups / (heads > 0 ? heads : 1);
+    parts = parts < tiles / kTileChunk ? parts : tiles / kTileChunk;
+    const int64_t room = static_cast<int64_t>(workspace_bytes) / (g.slots * Hkv * part_floats(kTileRows, Dh) * 4 + 1);
+    parts = parts < room ? parts : room;
+    g.parts = static_cast<int>(parts < 2 ? 1 : parts);
+    g.chunk = static_cast<int>((tiles + g.parts - 1) / g.parts);
+    return g;
+}
+
 }  // namespace
 
 size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                               int64_t window, int64_t sinks) {
+    constexpr size_t kAll = static_cast<size_t>(1) << 60;
     max_rows = max_rows < T ? max_rows : T;
-    if (max_rows * (Hq / Hkv) > kTokenRows) return 0;
-    const TokenGrid g = token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, static_cast<size_t>(1) << 60);
-    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(Dh) * 4;
+    if (max_rows * (Hq / Hkv) > token_rows(dtype)) {
+        const TileGrid g = tile_grid(T, B, Hq, Hkv, Dh, max_rows, max_len, window, sinks, kAll);
+        return g.parts < 2 ? 0 : static_cast<size_t>(g.slots) * Hkv * g.parts * part_floats(kTileRows, Dh) * 4;
+    }
+    const TokenGrid g = token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll);
+    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(16, Dh) * 4;
 }
 
 int launch_attend(const AttendCall &c, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const int dtype = c.dtype;
-    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) > kTokenRows)
-        return launch_status(dtype == APPROXIFER_F32   ? launch_tiles_f32(c, stream)
-                             : dtype == APPROXIFER_F16 ? launch_tiles_f16(c, stream)
-                                                       : launch_tiles_bf16(c, stream));
-    const TokenGrid g = token_grid(c.seq.B, c.Hq, c.Hkv, c.Dh, dtype, c.max_rows, c.max_len, c.window, c.sinks, workspace_bytes);
     float *const w = static_cast<float *>(workspace);
+    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) > token_rows(dtype)) {
+        const TileGrid g = tile_grid(c.seq.T, c.seq.B, c.Hq, c.Hkv, c.Dh, c.max_rows, c.max_len, c.window, c.sinks, workspace_bytes);
+        return launch_status(dtype == APPROXIFER_F32   ? launch_tiles_f32(c, g, w, stream)
+                             : dtype == APPROXIFER_F16 ? launch_tiles_f16(c, g, w, stream)
+                                                       : launch_tiles_bf16(c, g, w, stream));
+    }
+    const TokenGrid g = token_grid(c.seq.B, c.Hq, c.Hkv, c.Dh, dtype, c.max_rows, c.max_len, c.window, c.sinks, workspace_bytes);
     return launch_status(dtype == APPROXIFER_F32   ? launch_tokens_f32(c, g, w, stream)
                          : dtype == APPROXIFER_F16 ? launch_tokens_f16(c, g, w, stream)
                                                    : launch_tokens_bf16(c, g, w, stream));

@@ -97,18 +97,6 @@ __device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head
     return y;
 }
 
-// The same over all that it sees, and written.
-template <class E>
-__device__ void attend_whole_row(const AttendCall &c, const Rows &r, int i, int head, float *q, float *p) {
-    typedef typename E::Value V;
-    const Visible see(c.window, c.sinks, r.place(i));
-    const RowSum y = attend_row<E>(c, r, i, head, q, p, 0, see.sinks_end, see.from, see.place + 1);
-    V *out = static_cast<V *>(c.out) + ((r.start + i) * c.Hq + head) * c.Dh;
-    const float inverse = y.total == 0.0f ? 0.0f : 1.0f / y.total;
-    for (int k = 0; k < APPROXIFER_MAX_HEAD_DIM / kWave; ++k)
-        if (lane_id() + k * kWave < c.Dh) out[lane_id() + k * kWave] = E::store(y.out[k] * inverse);
-}
-
 // One wave: the status of sequence b.
 __device__ __forceinline__ int attend_status(const AttendCall &c, int b) {
     const Rows r = rows_of(c.seq, b);

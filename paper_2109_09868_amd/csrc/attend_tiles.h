@@ -13,12 +13,25 @@
 // (else by registers), two tiles of each and one barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
 #pragma once
 
-#include "attend_pieces.h"
+#include "attend_join.h"
 
 namespace approxifer {
 
 constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
 constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
+
+// slots: tiles of rows of all sequences (single: one for each); parts: workgroups that share a tile's keys, `chunk` tiles of 64 each or
+// as many more as it takes.
+constexpr int kTileRows = 128;
+struct TileGrid {
+    int64_t slots;
+    int parts, chunk;
+    bool single;
+    template <int kKeys>
+    __device__ __forceinline__ int chunk_of(int steps) const {
+        return parts == 1 ? 0x7fffffff : max(chunk * (64 / kKeys), (steps + parts - 1) / parts);
+    }
+};
 
 template <class E, int DP>
 struct TileShape {
@@ -63,7 +76,7 @@ __device__ __forceinline__ int slot_owner(const Sequences &s, int64_t slot, int 
 
 // kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.
 template <class E, int DP, bool kWhole, bool kSmall>
-__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, int64_t slots, bool single) {
+__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, TileGrid g, float *workspace) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
     constexpr bool kDirect = kWhole && !kSmall && S::kStride == S::kPieces;
@@ -71,7 +84,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     constexpr int kVec = S::kSize == 2 ? 1 : kOut % 4 == 0 ? 4 : kOut % 2 == 0 ? 2 : 1;
     __shared__ __align__(16) char lds[S::kLds];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
-    const int64_t work = slots * c.Hkv;
+    const int64_t heads = g.slots * c.Hkv, work = heads * g.parts;
     if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
         const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
         if (b >= c.seq.B) return;
@@ -79,10 +92,11 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         if (lane == 0) c.status[b] = st;
         return;
     }
-    const int h = static_cast<int>(blockIdx.x) % c.Hkv, group = c.Hq / c.Hkv;
-    const int64_t slot = slots - 1 - static_cast<int>(blockIdx.x) / c.Hkv;
+    const int part = static_cast<int>(blockIdx.x / heads), index = static_cast<int>(blockIdx.x % heads);
+    const int h = index % c.Hkv, group = c.Hq / c.Hkv;
+    const int64_t slot = g.slots - 1 - index / c.Hkv;
     int64_t tile = 0;
-    const int b = single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
+    const int b = g.single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
     const Rows rows = rows_of(c.seq, b);
     const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = tile * S::kRows;
     if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || tile < 0 || first >= row_count) return;
@@ -108,7 +122,10 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     const float scale = c.scale == 0.0f ? 1.0f : fabsf(c.scale) * 1.44269504088896340736f;
 
     const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
-    const int steps = keys.steps;
+    const int chunk = g.chunk_of<kKeys>(keys.steps);
+    const int begin = part * chunk, steps = min(keys.steps, begin + chunk);       // this part's tiles: begin .. steps - 1
+    if (begin >= steps && part > 0) return;
+    const bool alone = keys.steps <= chunk;
     const auto begin_of = [&](int it) { return keys.begin_of(it); };
     const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
     const int shift = c.seq.page_shift, in_page = (1 << shift) - 1;
@@ -120,7 +137,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     v4i k_next[S::kLoads], v_next[S::kLoads];
     bool odd = false;                                         // a value that is no number, in a tile that not every row sees all of
     unsigned long long bad_next = 0, bad = 0;
-    int page_next = steps > 0 ? page_at(0) : 0;
+    int page_next = begin < steps ? page_at(begin) : 0;
     const int Dh = kWhole ? DP : c.Dh;
     const auto load = [&](int it) {                           // this wave's keys of tile `it` into registers
         const bool off = page_next < 0 || page_next >= c.seq.P;
@@ -217,17 +234,17 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         for (int k = 0; k < 16; ++k) out[n][k] = 0.0f;
     float top = -INFINITY, total = 0.0f;
 
-    if (steps > 0) {
+    if (begin < steps) {
         if constexpr (kDirect) {
-            fetch(0);
-            settle(0);
+            fetch(begin);
+            settle(begin);
         } else {
-            load(0);
-            put(0);
+            load(begin);
+            put(begin);
         }
     }
     __syncthreads();
-    for (int it = 0; it < steps; ++it) {
+    for (int it = begin; it < steps; ++it) {
         const int j0 = begin_of(it);
         const unsigned long long bad_now = bad;
         if (it + 1 < steps) {
@@ -362,6 +379,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         __syncthreads();
     }
 
+    float *const partial = workspace + (index * static_cast<int64_t>(g.parts) + part) * part_floats(S::kRows, c.Dh);
     int *const flags = reinterpret_cast<int *>(lds);          // the tiles are done with
     if (lane == 0) flags[wave] = 0;
     if (__any(odd) && lane == 0) flags[wave] = 1;
@@ -373,14 +391,18 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         for (int n = 0; n < 32; ++n) {
             const int64_t r = first + wave * 32 + n;
             if (r < row_count)
-                attend_whole_row<E>(c, rows, static_cast<int>(r / group), h * group + static_cast<int>(r % group), scratch,
-                                    scratch + APPROXIFER_MAX_HEAD_DIM);
+                attend_part<E>(c, rows, r, h, scratch, keys, begin, steps, alone, partial, S::kRows, wave * 32 + n);
         }
         return;
     }
     total = half_sum(total);
-    const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
     if (first + wave * 32 + row32 < row_count) {
+        const float inverse = !alone ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
+        const int n = wave * 32 + row32;
+        if (!alone && half == 0) {
+            partial[S::kRows * c.Dh + n] = top == -INFINITY ? top : top * scale;
+            partial[S::kRows * c.Dh + S::kRows + n] = total;
+        }
         V *y = static_cast<V *>(c.out) + ((rows.start + token) * c.Hq + head) * c.Dh;
 #pragma unroll
         for (int o = 0; o < kOut; o += kVec)
@@ -390,41 +412,74 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                 for (int j = 0; j < kVec; ++j) {              // values 4 j ..+3 of the 4 kVec that lie next to each other
                     const int d = 32 * o + kVec * (8 * k + 4 * half) + 4 * j;
                     const auto value = [&](int n) { return out[o + (4 * j + n) % kVec][4 * k + (4 * j + n) / kVec] * inverse; };
-                    if (kWhole || d < c.Dh) store4<E>(y + d, value(0), value(1), value(2), value(3));
+                    if (!kWhole && d >= c.Dh) continue;
+                    if (alone) store4<E>(y + d, value(0), value(1), value(2), value(3));
+                    else *reinterpret_cast<v4f *>(partial + n * c.Dh + d) = v4f{value(0), value(1), value(2), value(3)};
                 }
     }
 }
 
-template <class E, int DP, bool kWhole, bool kSmall>
-hipError_t launch_tiles(const AttendCall &c, hipStream_t stream) {
+template <class E, int DP, int kWaves>
+__global__ __launch_bounds__(256) void attend_join_tiles_kernel(AttendCall c, TileGrid g, const float *workspace) {
     typedef TileShape<E, DP> S;
+    const int group = c.Hq / c.Hkv;
+    const int64_t at = kWaves == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave_id() : blockIdx.x;
+    const int n = static_cast<int>(at % S::kRows);
+    const int64_t index = at / S::kRows;
+    if (index >= g.slots * c.Hkv) return;
+    const int h = static_cast<int>(index % c.Hkv);
+    const int64_t slot = g.slots - 1 - index / c.Hkv;
+    int64_t tile = 0;
+    const int b = g.single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
+    const Rows rows = rows_of(c.seq, b);
+    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = tile * S::kRows;
+    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || tile < 0 || first + n >= row_count) return;
+    const int p0 = rows.place(static_cast<int>(first / group));
+    const int p1 = rows.place(static_cast<int>(min(first + S::kRows - 1, row_count - 1) / group));
+    const KeyTiles<S::kKeys> keys(c.window, c.sinks, p0, p1);
+    const int chunk = g.chunk_of<S::kKeys>(keys.steps);
+    if (keys.steps <= chunk) return;                          // written already
+    join_row<E, DP, kWaves>(c, rows, first + n, h, workspace + index * g.parts * part_floats(S::kRows, c.Dh), S::kRows, n,
+                            (keys.steps + chunk - 1) / chunk);
+}
+
+template <class E, int DP, bool kWhole, bool kSmall>
+hipError_t launch_tiles(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream) {
+    typedef TileShape<E, DP> S;
+    static_assert(S::kRows == kTileRows, "rows of a tile");
     // late rows see most: their tiles come first.  A head of the cache keeps its XCD where there are 8 of them.
-    const int64_t group = c.Hq / c.Hkv;
-    const bool single = c.max_rows * group <= S::kRows;       // a tile for each sequence
-    const int64_t slots = single ? c.seq.B : c.seq.T * group / S::kRows + c.seq.B;
-    const int64_t blocks = slots * c.Hkv + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
-    return launch_kernel(attend_tiles_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0, stream, c,
-                         slots, single);
+    const int64_t heads = g.slots * c.Hkv;
+    const int64_t blocks = heads * g.parts + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
+    hipError_t e = launch_kernel(attend_tiles_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0,
+                                 stream, c, g, workspace);
+    if (e == hipSuccess && g.parts > 1) {
+        const bool many = g.parts > 8;
+        const int64_t all = heads * S::kRows;
+        e = launch_kernel(many ? attend_join_tiles_kernel<E, DP, 4> : attend_join_tiles_kernel<E, DP, 1>,
+                          dim3(static_cast<unsigned>(many ? all : (all + 3) / 4)), dim3(256), 0, stream, c, g,
+                          static_cast<const float *>(workspace));
+    }
+    return e;
 }
 
 template <class E, bool kSmall>
-hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
-    if (c.Dh == 64) return launch_tiles<E, 64, true, kSmall>(c, stream);
-    if (c.Dh == 128) return launch_tiles<E, 128, true, kSmall>(c, stream);
-    if (c.Dh == 256) return launch_tiles<E, 256, true, kSmall>(c, stream);
-    if (c.Dh < 64) return launch_tiles<E, 64, false, kSmall>(c, stream);
-    if (c.Dh <= 96) return launch_tiles<E, 96, false, kSmall>(c, stream);
-    if (c.Dh < 128) return launch_tiles<E, 128, false, kSmall>(c, stream);
-    if (c.Dh <= 192) return launch_tiles<E, 192, false, kSmall>(c, stream);
-    return launch_tiles<E, 256, false, kSmall>(c, stream);
+hipError_t launch_tiles_of(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream) {
+    if (c.Dh == 64) return launch_tiles<E, 64, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 128) return launch_tiles<E, 128, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 256) return launch_tiles<E, 256, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 64) return launch_tiles<E, 64, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 96) return launch_tiles<E, 96, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 128) return launch_tiles<E, 128, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 192) return launch_tiles<E, 192, false, kSmall>(c, g, workspace, stream);
+    return launch_tiles<E, 256, false, kSmall>(c, g, workspace, stream);
 }
 template <class E>
-hipError_t launch_tiles_of(const AttendCall &c, hipStream_t stream) {
-    return c.seq.page_shift >= 4 ? launch_tiles_of<E, false>(c, stream) : launch_tiles_of<E, true>(c, stream);
+hipError_t launch_tiles_of(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream) {
+    return c.seq.page_shift >= 4 ? launch_tiles_of<E, false>(c, g, workspace, stream) : launch_tiles_of<E, true>(c, g, workspace, stream);
 }
 
-hipError_t launch_tiles_f32(const AttendCall &c, hipStream_t stream);
-hipError_t launch_tiles_f16(const AttendCall &c, hipStream_t stream);
-hipError_t launch_tiles_bf16(const AttendCall &c, hipStream_t stream);
+hipError_t launch_tiles_f32(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream);
+hipError_t launch_tiles_f16(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream);
+hipError_t launch_tiles_bf16(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream);
 
 }  // namespace approxifer

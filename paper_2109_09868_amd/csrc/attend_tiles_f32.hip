@@ -2,6 +2,8 @@
 
 namespace approxifer {
 
-hipError_t launch_tiles_f32(const AttendCall &c, hipStream_t stream) { return launch_tiles_of<F32>(c, stream); }
+hipError_t launch_tiles_f32(const AttendCall &c, const TileGrid &g, float *workspace, hipStream_t stream) {
+    return launch_tiles_of<F32>(c, g, workspace, stream);
+}
 
 }  // namespace approxifer

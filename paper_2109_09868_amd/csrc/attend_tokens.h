@@ -8,7 +8,7 @@
 // tile's keys and values are on their way meanwhile: 16 KB a wave at 128 x 2 bytes, 128 KB a CU.
 #pragma once
 
-#include "attend_pieces.h"
+#include "attend_join.h"
 
 namespace approxifer {
 
@@ -30,13 +30,11 @@ struct TokenShape {
     static_assert(kPieces % 4 == 0 && kKeys * kPieces % kWave == 0, "whole pieces per lane");
 };
 
-// A part's sums in the workspace: rows x Dh floats, then 16 maxima (of c S, base 2) and 16 totals.
-__device__ __host__ __forceinline__ int64_t part_floats(int Dh) { return 16 * static_cast<int64_t>(Dh) + 32; }
-
-// parts: workgroups that share a block of rows, each with `chunk` tiles; blocks: blocks of 16 rows of the longest sequence; rows: of those
+// parts: workgroups that share a block of rows, each with `chunk` tiles, or as many more as it takes; blocks: blocks of 16 rows of the longest sequence; rows: of those
 // 16, as many as there can be.
 struct TokenGrid {
     int pairs, blocks, parts, chunk, rows;
+    __device__ __forceinline__ int chunk_of(int steps) const { return parts == 1 ? 0x7fffffff : max(chunk, (steps + parts - 1) / parts); }
 };
 
 template <class E, int DP>
@@ -69,7 +67,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     const int place = rows.place(token);
     const int p0 = __builtin_amdgcn_readfirstlane(place), p1 = __builtin_amdgcn_readlane(place, 15);
     const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
-    const int begin = part * g.chunk, end = min(keys.steps, begin + g.chunk);
+    const int chunk = g.chunk_of(keys.steps), begin = part * chunk, end = min(keys.steps, begin + chunk);
     if (begin >= end && part > 0) return;                     // the parts that there are end before this one
     if (threadIdx.x == 0) dirty = 0;
 
@@ -187,7 +185,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         if constexpr (S::kSize == 2) {
             const float w[8] = {s[0][0], s[0][1], s[0][2], s[0][3], s[1][0], s[1][1], s[1][2], s[1][3]};
             // weights in two 16-bit pieces, what the first leaves in the second: the products wait for memory anyway, and the result is
-            // as exact as its own rounding
+            // as exact as its own rounding.  (0, or a negative rest, times an infinity is wrong: see below.)
             typedef V V8 __attribute__((ext_vector_type(8)));
             const v4i p = rounded8<E>(w);
             float rest[8];
@@ -219,6 +217,13 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         }
     }
 
+    if constexpr (S::kSize == 2) {                            // infinities among the values: element by element
+#pragma unroll
+        for (int o = 0; o < kOut; ++o)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) odd |= !(fabsf(out[o][k]) <= 3.402823466e38f);
+    }
+
     // the waves meet: one maximum per row, sums relative to it
     total = quarters_sum(total);
     if (quarter == 0) {
@@ -239,33 +244,15 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
                 v4f{out[o][0] * f, out[o][1] * f, out[o][2] * f, out[o][3] * f};
     }
     __syncthreads();
-    const bool alone = keys.steps <= g.chunk;
+    const bool alone = keys.steps <= chunk;
     const int64_t slot = (static_cast<int64_t>(pair) * g.blocks + block) * g.parts + part;
-    float *const partial = workspace + slot * part_floats(c.Dh);
+    float *const partial = workspace + slot * part_floats(S::kRows, c.Dh);
     if (dirty != 0) {                                         // rows that must not see what the product cannot hide
         __syncthreads();
         float *const scratch = reinterpret_cast<float *>(vt);
-        const int sinks_to = min(end, keys.sink_tiles) * kKeys, main_from = max(begin, keys.sink_tiles);
-        for (int n = wave; n < S::kRows; n += S::kWaves) {
-            const int64_t r = first + n;
-            if (r >= row_count) break;
-            const int i = static_cast<int>(r / group), hq = h * group + static_cast<int>(r % group);
-            const RowSum y = attend_row<E>(c, rows, i, hq, scratch, scratch + APPROXIFER_MAX_HEAD_DIM, begin * kKeys, sinks_to,
-                                           main_from < end ? keys.begin_of(main_from) : 0,
-                                           main_from < end ? keys.begin_of(end - 1) + kKeys : 0);
-            V *const o = static_cast<V *>(c.out) + ((rows.start + i) * c.Hq + hq) * c.Dh;
-            const float inverse = y.total == 0.0f ? 0.0f : 1.0f / y.total;
-            for (int k = 0; k < APPROXIFER_MAX_HEAD_DIM / kWave; ++k) {
-                const int d = lane + k * kWave;
-                if (d >= c.Dh) break;
-                if (alone) o[d] = E::store(y.out[k] * inverse);
-                else partial[n * c.Dh + d] = y.out[k];
-            }
-            if (!alone && lane == 0) {
-                partial[16 * c.Dh + n] = y.top * 1.44269504088896340736f;
-                partial[16 * c.Dh + 16 + n] = y.total;
-            }
-        }
+        for (int n = wave; n < S::kRows; n += S::kWaves)
+            if (first + n < row_count)
+                attend_part<E>(c, rows, first + n, h, scratch, keys, begin, end, alone, partial, S::kRows, n);
         return;
     }
     constexpr int kQuads = DP / 4;
@@ -298,95 +285,26 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     }
 }
 
-// The parts of a row joined, always in the same order, eight parts' sums on their way at a time.  kWaves of a workgroup share a row, every
-// kWaves-th part to each: 4 for many parts (one wave and one part after the other took 38 us for 43 parts, a seventh of the call), 1 for a
-// few, where rows are many.
 template <class E, int DP, int kWaves>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall c, TokenGrid g, const float *workspace) {
-    typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
-    constexpr int kPerLane = (DP + kWave - 1) / kWave, kAhead = 8;
-    __shared__ float outs[kWaves][kPerLane * kWave], tops[kWaves], totals[kWaves];
-    const int lane = lane_id(), group = c.Hq / c.Hkv;
-    const int wave = kWaves == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id());
+    const int group = c.Hq / c.Hkv;
     const int64_t index = kWaves == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave_id() : blockIdx.x;
     const int n = static_cast<int>(index % g.rows), block = static_cast<int>(index / g.rows % g.blocks);
     const int64_t pair64 = index / g.rows / g.blocks;
     if (pair64 >= g.pairs) return;
     const int pair = static_cast<int>(pair64);
     const Rows rows = rows_of(c.seq, pair / c.Hkv);
-    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(block) * S::kRows, row = first + n;
-    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || row >= row_count) return;
+    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(block) * S::kRows;
+    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || first + n >= row_count) return;
     const int p0 = rows.place(static_cast<int>(first / group));
     const int p1 = rows.place(static_cast<int>(min(first + S::kRows - 1, row_count - 1) / group));
     const KeyTiles<S::kKeys> keys(c.window, c.sinks, p0, p1);
-    if (keys.steps <= g.chunk) return;                        // written already
-    const int parts = (keys.steps + g.chunk - 1) / g.chunk;
-    const int64_t stride = part_floats(c.Dh);
-    const float *const base = workspace + (static_cast<int64_t>(pair) * g.blocks + block) * g.parts * stride;
-    float top = -INFINITY, out[kPerLane] = {}, total = 0.0f;
-    for (int from = wave; from < parts; from += kWaves * kWave) {
-        const int p = from + kWaves * lane, count = min((parts - from + kWaves - 1) / kWaves, kWave);
-        const float m = p < parts ? base[p * stride + 16 * c.Dh + n] : -INFINITY;
-        const float l = p < parts ? base[p * stride + 16 * c.Dh + 16 + n] : 0.0f;
-        float most = fmaxf(m, top);
-        for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-        const float shrink = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - most);
-        const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - most);
-        // a part that saw nothing but what is no number has no maximum, and a total that says so
-        total = total * shrink + (m == -INFINITY ? l : f * l);
-        top = most;
-#pragma unroll
-        for (int k = 0; k < kPerLane; ++k) out[k] *= shrink;
-        for (int i = 0; i < count; i += kAhead) {
-            float x[kAhead][kPerLane], w[kAhead];
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int j = min(i + a, count - 1);
-                w[a] = i + a < count ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j)) : 0.0f;
-#pragma unroll
-                for (int k = 0; k < kPerLane; ++k)
-                    x[a][k] = lane + k * kWave < c.Dh ? base[(from + kWaves * j) * stride + n * c.Dh + lane + k * kWave] : 0.0f;
-            }
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-#pragma unroll
-                for (int k = 0; k < kPerLane; ++k) out[k] += i + a < count ? w[a] * x[a][k] : 0.0f;
-        }
-    }
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-    const int64_t t = rows.start + row / group;
-    V *const y = static_cast<V *>(c.out) + (t * c.Hq + pair % c.Hkv * group + row % group) * c.Dh;
-    if constexpr (kWaves == 1) {
-        const float inverse = total == 0.0f ? 0.0f : 1.0f / total;
-#pragma unroll
-        for (int k = 0; k < kPerLane; ++k)
-            if (lane + k * kWave < c.Dh) y[lane + k * kWave] = E::store(out[k] * inverse);
-        return;
-    }
-#pragma unroll
-    for (int k = 0; k < kPerLane; ++k) outs[wave][lane + k * kWave] = out[k];
-    if (lane == 0) {
-        tops[wave] = top;
-        totals[wave] = total;
-    }
-    __syncthreads();
-    float all = tops[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w]);
-    float sum = 0.0f, f[kWaves];
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        f[w] = tops[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(tops[w] - all);
-        sum += tops[w] == -INFINITY ? totals[w] : f[w] * totals[w];
-    }
-    const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
-    for (int d = threadIdx.x; d < c.Dh; d += 256) {
-        float x = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) x += f[w] * outs[w][d];
-        y[d] = E::store(x * inverse);
-    }
+    const int chunk = g.chunk_of(keys.steps);
+    if (keys.steps <= chunk) return;                          // written already
+    join_row<E, DP, kWaves>(c, rows, first + n, pair % c.Hkv,
+                            workspace + (static_cast<int64_t>(pair) * g.blocks + block) * g.parts * part_floats(S::kRows, c.Dh), S::kRows,
+                            n, (keys.steps + chunk - 1) / chunk);
 }
 
 template <class E, int DP>
