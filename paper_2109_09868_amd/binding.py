@@ -506,6 +506,16 @@ def approxifer_rotary_frequencies(pairs: int, base: float = 10000.0):
     return freq
 
 
+def _on(stream):
+    """Makes a call's stream the current one, so that what is allocated or filled for the call is ordered with it."""
+    import contextlib
+
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
 def _dtype_code(dtype) -> int:
     import torch
     codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
@@ -565,10 +575,11 @@ def approxifer_append(q, k, v, k_pool, v_pool, table, lens, starts, freq, q_weig
     qp, q_stride = _rows(q, dtype)
     kk, k_stride = _rows(k, dtype)
     vv, v_stride = _rows(v, dtype)
-    if q_out is None:
-        q_out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
-    if status is None:
-        status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
+    with _on(stream):
+        if q_out is None:
+            q_out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+        if status is None:
+            status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
     seq = _sequences(table, lens, starts, T, k_pool)
     pairs, fp = _nodes(freq)
     axes = 1
@@ -622,13 +633,14 @@ def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len,
     Hkv = k_pool.shape[1]
     kp, vp = _pools(k_pool, v_pool, dtype, None, Dh)
     qp, q_stride = _rows(q, dtype)
-    if out is None:
-        out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
-    if status is None:
-        status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
-    if workspace is None:
-        need = approxifer_attend_workspace_bytes(T, table.shape[0], Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else NO_WORKSPACE
+    with _on(stream):
+        if out is None:
+            out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+        if status is None:
+            status = torch.full((table.shape[0],), -1, dtype=torch.int32, device=q.device)
+        if workspace is None:
+            need = approxifer_attend_workspace_bytes(T, table.shape[0], Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else NO_WORKSPACE
     ws_ptr, ws_bytes = _scratch(workspace)
     seq = _sequences(table, lens, starts, T, k_pool)
     _check(_entry().approxifer_attend(
@@ -647,8 +659,9 @@ def approxifer_cache_reserve(table, lens, refs, add, page, status=None, stream=N
             return status
     import torch
     B, M = table.shape
-    if status is None:
-        status = torch.full((B,), -1, dtype=torch.int32, device=table.device)
+    with _on(stream):
+        if status is None:
+            status = torch.full((B,), -1, dtype=torch.int32, device=table.device)
     _check(_entry().approxifer_cache_reserve(_dev(table, torch.int32), _dev(lens, torch.int32, (B,)), _dev(refs, torch.int32),
                                              _dev(add, torch.int32, (B,)), _dev(status, torch.int32, (B,)), B, M, refs.numel(),
                                              int(page), _stream_handle(stream)))
@@ -687,16 +700,17 @@ def approxifer_cache_fork(pools, table, lens, refs, parents, keep=None, table_ou
     B, M = table.shape
     P, n = refs.numel(), parents.numel()
     at, planes, page_bytes, page = _planes(pools, P)
-    if table_out is None:
-        table_out = torch.empty((n, M), dtype=i32, device=table.device)
-    if lens_out is None:
-        lens_out = torch.empty((n,), dtype=i32, device=table.device)
-    if refs_out is None:
-        refs_out = torch.empty((P,), dtype=i32, device=table.device)
-    if status is None:
-        status = torch.full((n,), -1, dtype=i32, device=table.device)
-    if workspace is None:
-        workspace = torch.empty((approxifer_cache_workspace_bytes(B, n, P),), dtype=torch.uint8, device=table.device)
+    with _on(stream):
+        if table_out is None:
+            table_out = torch.empty((n, M), dtype=i32, device=table.device)
+        if lens_out is None:
+            lens_out = torch.empty((n,), dtype=i32, device=table.device)
+        if refs_out is None:
+            refs_out = torch.empty((P,), dtype=i32, device=table.device)
+        if status is None:
+            status = torch.full((n,), -1, dtype=i32, device=table.device)
+        if workspace is None:
+            workspace = torch.empty((approxifer_cache_workspace_bytes(B, n, P),), dtype=torch.uint8, device=table.device)
     ws_ptr, ws_bytes = _scratch(workspace)
     _check(_entry().approxifer_cache_fork(
         _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(parents, i32, (n,)),
@@ -718,12 +732,13 @@ def approxifer_cache_compact(pools, table, lens, refs, moved=None, live=None, wo
     B, M = table.shape
     P = refs.numel()
     at, planes, page_bytes, page = _planes(pools, P)
-    if moved is None:
-        moved = torch.empty((P,), dtype=i32, device=table.device)
-    if live is None:
-        live = torch.empty((1,), dtype=i32, device=table.device)
-    if workspace is None:
-        workspace = torch.empty((approxifer_cache_workspace_bytes(B, B, P),), dtype=torch.uint8, device=table.device)
+    with _on(stream):
+        if moved is None:
+            moved = torch.empty((P,), dtype=i32, device=table.device)
+        if live is None:
+            live = torch.empty((1,), dtype=i32, device=table.device)
+        if workspace is None:
+            workspace = torch.empty((approxifer_cache_workspace_bytes(B, B, P),), dtype=torch.uint8, device=table.device)
     ws_ptr, ws_bytes = _scratch(workspace)
     _check(_entry().approxifer_cache_compact(
         _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(moved, i32, (P,)), _dev(live, i32, (1,)), at, planes,

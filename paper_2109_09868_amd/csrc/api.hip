@@ -42,7 +42,7 @@ int check_common(int K, int N, const double *h_alpha, const double *h_beta, Node
 // Sizes of a cache; *shift: log2 of the page.
 int check_cache(int64_t B, int64_t M, int64_t P, int page, int *shift) {
     if (B < 0 || M < 1 || P < 1 || page < 1 || (page & (page - 1)) != 0) return APPROXIFER_ERR_BAD_CACHE;
-    if (page > APPROXIFER_MAX_PAGE || B > APPROXIFER_MAX_SEQUENCES || P > 0x7fffffffLL || M > 0x7fffffffLL / page)
+    if (page > APPROXIFER_MAX_PAGE || B > APPROXIFER_MAX_SEQUENCES || P > APPROXIFER_MAX_PAGES || M > 0x7fffffffLL / page)
         return APPROXIFER_ERR_LIMIT;
     *shift = __builtin_ctz(static_cast<unsigned>(page));
     return APPROXIFER_OK;
@@ -411,7 +411,7 @@ int approxifer_cache_compact(int32_t *d_table, const int32_t *d_lens, int32_t *d
 }
 
 size_t approxifer_cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P) {
-    if (B < 0 || B_out < 0 || P < 1 || B > APPROXIFER_MAX_SEQUENCES || B_out > APPROXIFER_MAX_SEQUENCES || P > 0x7fffffffLL) return 0;
+    if (B < 0 || B_out < 0 || P < 1 || B > APPROXIFER_MAX_SEQUENCES || B_out > APPROXIFER_MAX_SEQUENCES || P > APPROXIFER_MAX_PAGES) return 0;
     return approxifer::cache_workspace_bytes(B, B_out, P);
 }
 

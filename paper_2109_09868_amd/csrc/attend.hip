@@ -33,7 +33,7 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     g.pairs = static_cast<int>(pairs);
     g.blocks = static_cast<int>(blocks);
     g.rows = static_cast<int>(max_rows * group < 16 ? max_rows * group : 16);
-    if (parts < 2) {
+    if (parts < 2 || blocks == 0) {
         g.parts = 1;
         g.chunk = 0x7fffffff;
         return g;

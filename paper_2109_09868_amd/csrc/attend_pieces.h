@@ -31,6 +31,11 @@ __device__ __forceinline__ v16f multiply<F32>(v4i a, v4i b, v16f d) {
     return d;
 }
 
+// Weights relative to a running maximum are kept as 2^kLift times themselves, below 2^15: their sum is, too, and what is small against
+// the largest keeps the bits that half precision loses below 2^-14 (many such weights together count).
+template <class E>
+constexpr float kLift = std::is_same<E, F16>::value ? 7.0f : 0.0f;
+
 // Eight floats rounded to 16 bits.
 template <class E>
 __device__ __forceinline__ v4i rounded8(const float *p) {

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                     for (int k = 0; k < 16; ++k) out[n][k] *= f;
                 top = most;
             }
-            const float base = top == -INFINITY ? 0.0f : top * scale;
+            const float base = top == -INFINITY ? 0.0f : top * scale - kLift<E>;
             float sum = 0.0f;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
@@ -400,7 +400,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         const float inverse = !alone ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
         const int n = wave * 32 + row32;
         if (!alone && half == 0) {
-            partial[S::kRows * c.Dh + n] = top == -INFINITY ? top : top * scale;
+            partial[S::kRows * c.Dh + n] = top == -INFINITY ? top : top * scale - kLift<E>;
             partial[S::kRows * c.Dh + S::kRows + n] = total;
         }
         V *y = static_cast<V *>(c.out) + ((rows.start + token) * c.Hq + head) * c.Dh;

@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
                 for (int k = 0; k < 4; ++k) out[n][k] *= f;
             top = most;
         }
-        const float base = top == -INFINITY ? 0.0f : top * scale;
+        const float base = top == -INFINITY ? 0.0f : top * scale - kLift<E>;
 #pragma unroll
         for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
@@ -217,12 +217,11 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         }
     }
 
-    if constexpr (S::kSize == 2) {                            // infinities among the values: element by element
+    // infinities among the values: element by element.  (A hidden key's place in the product is taken by one that is seen, with weight 0.)
 #pragma unroll
-        for (int o = 0; o < kOut; ++o)
+    for (int o = 0; o < kOut; ++o)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) odd |= !(fabsf(out[o][k]) <= 3.402823466e38f);
-    }
+        for (int k = 0; k < 4; ++k) odd |= !(fabsf(out[o][k]) <= 3.402823466e38f);
 
     // the waves meet: one maximum per row, sums relative to it
     total = quarters_sum(total);
@@ -278,7 +277,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         } else {
             *reinterpret_cast<v4f *>(partial + r * c.Dh + d) = sum;
             if (d == 0) {
-                partial[16 * c.Dh + r] = m == -INFINITY ? m : m * scale;
+                partial[16 * c.Dh + r] = m == -INFINITY ? m : m * scale - kLift<E>;
                 partial[16 * c.Dh + 16 + r] = l;
             }
         }
@@ -312,6 +311,7 @@ hipError_t launch_tokens(const AttendCall &c, const TokenGrid &g, float *workspa
     typedef TokenShape<E, DP> S;
     const int64_t work = static_cast<int64_t>(g.pairs) * g.parts * g.blocks;
     const int64_t blocks = work + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
+    if (blocks == 0) return hipSuccess;                       // max_rows is 0: nothing but statuses is written
     hipError_t e = launch_kernel(attend_tokens_kernel<E, DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
     if (e == hipSuccess && g.parts > 1) {
         const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * g.rows;

@@ -137,6 +137,66 @@ def test_what_a_row_sees_does_reach_it(binding, dtype, new):
 
 
 @pytest.mark.parametrize("dtype", list(ref.DTYPES.values()), ids=list(ref.DTYPES))
+@pytest.mark.parametrize("length", [1, 33, 150])
+def test_the_last_value_of_a_row_may_be_infinite(binding, dtype, length):
+    # lengths that end inside a tile: places behind the last take nothing of it
+    c = ref.cache(6, dtype, [length], [1], 1, 64, 16)
+    j = length - 1
+    c["v_pool"][int(c["table"][0, j // 16]), 0, j % 16, 9] = math.inf
+    q = torch.randn((1, 2, 64), generator=torch.Generator().manual_seed(1)).to(dtype)
+    out, _ = _call(binding, c, q)
+    assert torch.all(out[:, :, 9] == math.inf) and int(out.isfinite().sum()) == 2 * 63
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_many_small_weights_of_half_precision_count(binding, new):
+    # 6000 keys of a weight that is next to 2^-26 of the first one's: half precision has no numbers there.  Weights are kept as
+    # 2^7 times themselves, so that each is off by 2^-32 of the largest at most, and by half a step.
+    c = ref.cache(0, torch.float16, [6000], [new], 1, 64, 16)
+    c["k_pool"].zero_()
+    p = int(c["table"][0, 0])
+    c["k_pool"][p, 0, 0, 0] = 4.5
+    c["v_pool"][:] = 1.0
+    c["v_pool"][p, 0, 0] = 0.0
+    q = torch.zeros((new, 4, 64), dtype=torch.float16)
+    q[:, :, 0] = 4.0
+    out, _ = _call(binding, c, q, scale=1.0)
+    n = torch.arange(6000 - new, 6000, dtype=torch.float64)
+    small = math.exp(-18.0)
+    want = n * small / (1 + n * small)
+    bound = n * 2.0 ** -32 + want * (2 * ref.half_step(torch.float16) + (6000 + 64 + 36 * 64) * ref.U32)
+    assert torch.all((out.double() - want[:, None, None]).abs() <= bound[:, None, None])
+
+
+@pytest.mark.parametrize("status", [True, False])
+def test_bounds_of_zero(binding, status):
+    c = ref.cache(0, torch.float16, [40, 7000], [1, 1], 2, 64, 16)
+    kp, vp, table, lens, starts = ref.on(DEV, c)
+    lib, q, out = binding.load(), torch.zeros((2, 4, 64), dtype=torch.float16, device=DEV), torch.full((2, 4, 64), -3.0, device=DEV).half()
+    st, ws = torch.full((2,), -1, dtype=torch.int32, device=DEV), torch.empty((1 << 22,), dtype=torch.uint8, device=DEV)
+    for T, rows in ((2, 0), (0, 0), (0, 1)):
+        seq = binding._Sequences(table.data_ptr(), lens.data_ptr(), starts.data_ptr(), T, 2, table.shape[1], kp.shape[0], 16)
+        rc = lib.approxifer_attend(seq, 4, 2, 64, binding.F16, q.data_ptr(), 256, kp.data_ptr(), vp.data_ptr(), out.data_ptr(), rows, 7000,
+                                   0, 0, 0.125, st.data_ptr() if status else None, ws.data_ptr(), ws.numel(), None)
+        assert rc == 0
+    torch.cuda.synchronize()
+    assert torch.all(out == -3.0) and st.tolist() == ([1, 1] if status else [-1, -1])
+
+
+def test_what_a_call_on_a_stream_allocates_belongs_to_it(binding):
+    c = ref.cache(0, torch.bfloat16, [7000], [1], 2, 64, 16)
+    kp, vp, table, lens, starts = ref.on(DEV, c)
+    q = torch.randn((1, 8, 64), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    want, _ = _call(binding, c, q)
+    x, side = q.to(DEV), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (side, side.cuda_stream):
+        out, status = binding.approxifer_attend(x, kp, vp, table, lens, starts, 1, 7000, stream=stream)
+        side.synchronize()
+        assert status.tolist() == [0] and torch.equal(out.cpu(), want)
+
+
+@pytest.mark.parametrize("dtype", list(ref.DTYPES.values()), ids=list(ref.DTYPES))
 @pytest.mark.parametrize("new", [3, 70])
 def test_rows_that_see_nothing_are_zero(binding, dtype, new):
     # more new tokens than the sequence has: the first rows have no place

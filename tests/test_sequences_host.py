@@ -135,6 +135,13 @@ def test_rotary_frequencies(lib):
     assert lib.approxifer_rotary_frequencies(4, 1e4, None) == -1
 
 
+def test_pages_are_counted_in_31_bits(lib):
+    # kernels walk over pages some thousands at a time, past the last one
+    assert _attend(lib, _seq(P=(1 << 30) + 1)) == -3 and _append(lib, _seq(P=(1 << 30) + 1)) == -3
+    assert lib.approxifer_cache_reserve(FAKE, FAKE, FAKE, FAKE, None, 2, 3, (1 << 30) + 1, 16, None) == -3
+    assert binding.approxifer_cache_workspace_bytes(2, 3, (1 << 30) + 1) == 0 < binding.approxifer_cache_workspace_bytes(2, 3, 1 << 30)
+
+
 def test_new_codes_have_texts_of_their_own(lib):
     texts = {binding.strerror(code) for code in range(0, -13, -1)}
     assert len(texts) == 13 and not any("unknown" in t for t in texts)
