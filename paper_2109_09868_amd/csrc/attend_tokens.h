@@ -37,9 +37,9 @@ struct TokenGrid {
     __device__ __forceinline__ int chunk_of(int steps) const { return parts == 1 ? 0x7fffffff : max(chunk, (steps + parts - 1) / parts); }
 };
 
-template <class E, int DP>
-__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(AttendCall c, TokenGrid g,
-                                                                                                          float *workspace) {
+// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(AttendCall c, TokenGrid g, float *workspace) {
     typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
     constexpr int kKeys = S::kKeys, kOut = DP / 16;
@@ -85,34 +85,46 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     const V *const k_pool = static_cast<const V *>(c.k_pool), *const v_pool = static_cast<const V *>(c.v_pool);
     char *const vt = lds + wave * S::kBytes;
 
+    const int Dh = kWhole ? DP : c.Dh;
     v4i k_next[S::kBlocks][S::kSteps], v_next[S::kLoads];
     const auto page_at = [&](int it) { return table[keys.seen(keys.begin_of(min(it, end - 1)) + (lane & (kKeys - 1))) >> shift]; };
-    int page_next = begin < end ? page_at(begin + wave) : 0;
+    int page_next = begin < end ? page_at(begin + wave) : 0, page = 0;
     unsigned long long bad_next = 0;
-    const auto load = [&](int it) {
+    // Element `at` of a key of the tile at j0.  Blocks of 16 keys lie in one page unless pages are small: the address is then the wave's
+    // plus an offset of the lane's that never changes.  What nobody sees is not used, but it may be read.
+    const auto address = [&](const V *pool, int j0, int block, int key, int at) {
+        if constexpr (kSmall) {
+            const int p = __shfl(page, block * 16 + key);
+            return pool + ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (keys.seen(j0 + block * 16 + key) & slots)) * Dh + at;
+        } else {
+            const int p = __builtin_amdgcn_readlane(page, block * 16);
+            return pool + ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + ((j0 + block * 16) & slots)) * Dh + (key * Dh + at);
+        }
+    };
+    // Loads return in order: a tile's pages are asked for before the keys of the tile before it, and its keys before that tile's values are
+    // waited for, so that half a tile at least is on its way at any time.
+    const auto load_keys = [&](int it) {
         const bool off = page_next < 0 || page_next >= c.seq.P;
         bad_next = __ballot(off);
-        const int page = off ? 0 : page_next, j0 = keys.begin_of(it);
-        const auto row_of = [&](int key) {
-            const int p = __shfl(page, key);
-            return ((static_cast<int64_t>(p) * c.Hkv + h) * (slots + 1) + (keys.seen(j0 + key) & slots)) * c.Dh;
-        };
+        page = off ? 0 : page_next;
+        page_next = page_at(it + S::kWaves);
+        const int j0 = keys.begin_of(it);
 #pragma unroll
-        for (int b = 0; b < S::kBlocks; ++b) {
-            const V *x = k_pool + row_of(b * 16 + row16);
+        for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
             for (int s = 0; s < S::kSteps; ++s) {
                 const int d = (4 * s + quarter) * S::kPerPiece;
-                k_next[b][s] = DP == c.Dh || d < c.Dh ? *reinterpret_cast<const v4i *>(x + d) : v4i{0, 0, 0, 0};
+                k_next[b][s] = *reinterpret_cast<const v4i *>(address(k_pool, j0, b, row16, kWhole || d < Dh ? d : 0));
             }
-        }
+    };
+    const auto load_values = [&](int it) {
+        const int j0 = keys.begin_of(it);
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
-            const int index = n * kWave + lane, key = index / S::kPieces, d = index % S::kPieces * S::kPerPiece;
-            const V *x = v_pool + row_of(key) + d;
-            v_next[n] = DP == c.Dh || d < c.Dh ? *reinterpret_cast<const v4i *>(x) : v4i{0, 0, 0, 0};
+            const int index = n * kWave + lane, d = index % S::kPieces * S::kPerPiece;
+            v_next[n] = *reinterpret_cast<const v4i *>(
+                address(v_pool, j0, n * 4 / S::kPieces, index / S::kPieces % 16, kWhole || d < Dh ? d : 0));
         }
-        page_next = page_at(it + S::kWaves);
     };
 
     v4f out[kOut];
@@ -120,8 +132,11 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     for (int n = 0; n < kOut; ++n) out[n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     float top = -INFINITY, total = 0.0f;
     bool odd = false;
-    if (begin + wave < end) load(begin + wave);
-    for (int it = begin + wave; it < end; it += S::kWaves) {
+    if (begin + wave < end) {
+        load_keys(begin + wave);
+        load_values(begin + wave);
+    }
+    const auto step = [&](int it, auto more) {
         const int j0 = keys.begin_of(it);
         const unsigned long long bad = bad_next;
         const bool whole = j0 + kKeys - 1 <= p0 && (c.window == 0 || j0 > p1 - c.window || j0 + kKeys <= c.sinks);
@@ -130,7 +145,18 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         for (int b = 0; b < S::kBlocks; ++b) {
             s[b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int n = 0; n < S::kSteps; ++n) s[b] = multiply16<E>(k_next[b][n], q[n], s[b]);
+            for (int n = 0; n < S::kSteps; ++n) {
+                if (!kWhole && (4 * n + quarter) * S::kPerPiece >= Dh) k_next[b][n] = v4i{0, 0, 0, 0};  // behind the head
+                s[b] = multiply16<E>(k_next[b][n], q[n], s[b]);
+            }
+        }
+        if constexpr (more) load_keys(it + S::kWaves);
+        if (!kSmall && !whole) {                              // seen by nobody: whatever the page holds there
+#pragma unroll
+            for (int n = 0; n < S::kLoads; ++n) {
+                const int j = j0 + (n * kWave + lane) / S::kPieces;
+                if (keys.seen(j) != j) v_next[n] = v4i{0, 0, 0, 0};
+            }
         }
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
@@ -141,7 +167,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) odd |= not_finite<E>(v_next[n]);
         }
-        if (it + S::kWaves < end) load(it + S::kWaves);
+        if constexpr (more) load_values(it + S::kWaves);
         const bool masked = !whole || bad != 0;
         if (masked) {
             const int reach = place - j0 - 4 * quarter, start = c.sinks - j0 - 4 * quarter;
@@ -215,7 +241,11 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
                         out[o] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, s[b][k], out[o], 0, 0, 0);
                     }
         }
-    }
+    };
+    // the last tile on its own: a load that may or may not be on its way would have to be waited for as if it were not
+    int it = begin + wave;
+    for (; it + S::kWaves < end; it += S::kWaves) step(it, std::true_type{});
+    if (it < end) step(it, std::false_type{});
 
     // infinities among the values: element by element.  (A hidden key's place in the product is taken by one that is seen, with weight 0.)
 #pragma unroll
@@ -306,13 +336,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall c, TokenGri
                             n, (keys.steps + chunk - 1) / chunk);
 }
 
-template <class E, int DP>
+template <class E, int DP, bool kWhole, bool kSmall>
 hipError_t launch_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
     typedef TokenShape<E, DP> S;
     const int64_t work = static_cast<int64_t>(g.pairs) * g.parts * g.blocks;
     const int64_t blocks = work + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
     if (blocks == 0) return hipSuccess;                       // max_rows is 0: nothing but statuses is written
-    hipError_t e = launch_kernel(attend_tokens_kernel<E, DP>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
+    hipError_t e = launch_kernel(attend_tokens_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
     if (e == hipSuccess && g.parts > 1) {
         const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * g.rows;
         const bool many = g.parts > 8;
@@ -323,13 +353,20 @@ hipError_t launch_tokens(const AttendCall &c, const TokenGrid &g, float *workspa
     return e;
 }
 
+template <class E, bool kSmall>
+hipError_t launch_tokens_of(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
+    if (c.Dh == 64) return launch_tokens<E, 64, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 128) return launch_tokens<E, 128, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 256) return launch_tokens<E, 256, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 64) return launch_tokens<E, 64, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 96) return launch_tokens<E, 96, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 128) return launch_tokens<E, 128, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 192) return launch_tokens<E, 192, false, kSmall>(c, g, workspace, stream);
+    return launch_tokens<E, 256, false, kSmall>(c, g, workspace, stream);
+}
 template <class E>
 hipError_t launch_tokens_of(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
-    if (c.Dh <= 64) return launch_tokens<E, 64>(c, g, workspace, stream);
-    if (c.Dh <= 96) return launch_tokens<E, 96>(c, g, workspace, stream);
-    if (c.Dh <= 128) return launch_tokens<E, 128>(c, g, workspace, stream);
-    if (c.Dh <= 192) return launch_tokens<E, 192>(c, g, workspace, stream);
-    return launch_tokens<E, 256>(c, g, workspace, stream);
+    return c.seq.page_shift >= 4 ? launch_tokens_of<E, false>(c, g, workspace, stream) : launch_tokens_of<E, true>(c, g, workspace, stream);
 }
 
 hipError_t launch_tokens_f32(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
