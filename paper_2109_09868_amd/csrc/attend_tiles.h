@@ -11,6 +11,10 @@
 //
 // Keys and values go through LDS, the next tile's on their way while this one is computed: straight there where heads and pages are whole
 // (else by registers), two tiles of each and one barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
+//
+// Bound by the matrix cores and the vector units, one after the other, at the clock that power leaves: two prompts of 4099 and 7001 tokens (32 heads of
+// 128 on 8, bf16) 641 to 665 us on different cards, 950 TFLOP/s; 12001 tokens of 24 heads of 64 in a window of 2048 (fp16) 198 us, 700 TFLOP/s; 192
+// texts of 128 tokens, 12 heads of 64 in 32 bits, 102 us, 47 TFLOP/s and 3.0 TB/s, which wait for their loads.
 #pragma once
 
 #include "attend_join.h"
@@ -40,7 +44,7 @@ struct TileShape {
     static constexpr int kPieces = DP * kSize / 16;           // of a row
     static constexpr int kStride = pow2_at_least(kPieces);    // pieces between rows in LDS
     // 32 keys a tile where 64 take too much LDS or too many registers, and for short 32-bit heads, where three workgroups share a CU so
-    // (192 sequences of 128 tokens, 12 heads of 64: 110 us, 125 with 64 keys and two workgroups)
+    // (192 sequences of 128 tokens, 12 heads of 64: 110 us when this was chosen, 125 with 64 keys and two workgroups)
     static constexpr bool kShort = kSize == 4 && DP == 64;
     static constexpr int kKeys = kStride * 16 > 512 || DP > 128 || kShort ? 32 : 64;
     static constexpr int kWaves = 4;
@@ -453,7 +457,9 @@ hipError_t launch_tiles(const AttendCall &c, const TileGrid &g, float *workspace
     hipError_t e = launch_kernel(attend_tiles_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(S::kThreads), 0,
                                  stream, c, g, workspace);
     if (e == hipSuccess && g.parts > 1) {
-        const bool many = g.parts > 8;
+        // four waves for a row of many parts, as far as they are there: rows many 77 us with one and 87 with four (128 tokens of 32 heads, 20000
+        // keys), rows few 36 and 25 (8 tokens of 8 heads, 60000 keys)
+        const bool many = g.parts > 8 && c.seq.T * c.Hq <= 1024;
         const int64_t all = heads * S::kRows;
         e = launch_kernel(many ? attend_join_tiles_kernel<E, DP, 4> : attend_join_tiles_kernel<E, DP, 1>,
                           dim3(static_cast<unsigned>(many ? all : (all + 3) / 4)), dim3(256), 0, stream, c, g,
