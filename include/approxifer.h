@@ -342,7 +342,7 @@ int approxifer_wait_mask(const float *d_arrival, uint8_t *d_mask, int32_t *d_cou
  *   APPROXIFER_SEQUENCE_NO_PAGES, APPROXIFER_SEQUENCE_SHARED_PAGE   see the calls that take pages
  *
  * Sizes: page a power of two up to 4096; Dh a multiple of 8 up to 256; Hq a multiple of Hkv, Hq <= 1024; T up to 2^24, B up
- * to 2^20, T Hq up to 2^30, B Hkv up to 2^22, P up to 2^30, M page below 2^31 (pools may be larger than that), M and P at least 1.
+ * to 2^20, T Hq up to 2^30, B Hkv up to 2^22, P and M page up to 2^30 (pools may be larger than that), M and P at least 1.
  * APPROXIFER_ERR_BAD_CACHE, or APPROXIFER_ERR_LIMIT for sizes that are merely too large.
  */
 #define APPROXIFER_F32 0
@@ -361,6 +361,7 @@ int approxifer_wait_mask(const float *d_arrival, uint8_t *d_mask, int32_t *d_cou
 #define APPROXIFER_MAX_ROWS (1 << 24)
 #define APPROXIFER_MAX_SEQUENCES (1 << 20)
 #define APPROXIFER_MAX_PAGES (1 << 30)
+#define APPROXIFER_MAX_TOKENS (1 << 30)
 
 typedef struct approxifer_sequences {   /* host memory, read before the call returns */
     const int32_t *d_table;             /* [B][M] device */

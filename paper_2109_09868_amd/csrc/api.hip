@@ -42,7 +42,7 @@ int check_common(int K, int N, const double *h_alpha, const double *h_beta, Node
 // Sizes of a cache; *shift: log2 of the page.
 int check_cache(int64_t B, int64_t M, int64_t P, int page, int *shift) {
     if (B < 0 || M < 1 || P < 1 || page < 1 || (page & (page - 1)) != 0) return APPROXIFER_ERR_BAD_CACHE;
-    if (page > APPROXIFER_MAX_PAGE || B > APPROXIFER_MAX_SEQUENCES || P > APPROXIFER_MAX_PAGES || M > 0x7fffffffLL / page)
+    if (page > APPROXIFER_MAX_PAGE || B > APPROXIFER_MAX_SEQUENCES || P > APPROXIFER_MAX_PAGES || M > APPROXIFER_MAX_TOKENS / page)
         return APPROXIFER_ERR_LIMIT;
     *shift = __builtin_ctz(static_cast<unsigned>(page));
     return APPROXIFER_OK;
@@ -360,7 +360,9 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
         dtype > APPROXIFER_BF16 || max_rows < 1 || max_len < 1 || window < 0 || sinks < 0 || T * Hq > (1LL << 30) ||
         B * Hkv > (1LL << 22))
         return 0;
-    return approxifer::attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
+    const int64_t most = APPROXIFER_MAX_TOKENS;               // no sequence is longer
+    return approxifer::attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len < most ? max_len : most, window < most ? window : 0,
+                                              sinks < most ? sinks : most);
 }
 
 int approxifer_cache_reserve(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, const int32_t *d_add, int32_t *d_status, int64_t B,

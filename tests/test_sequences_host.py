@@ -142,6 +142,21 @@ def test_pages_are_counted_in_31_bits(lib):
     assert binding.approxifer_cache_workspace_bytes(2, 3, (1 << 30) + 1) == 0 < binding.approxifer_cache_workspace_bytes(2, 3, 1 << 30)
 
 
+def test_places_are_counted_in_31_bits(lib):
+    # places are compared with those of a whole tile, or window, further on
+    assert _attend(lib, _seq(M=(1 << 26) + 1)) == -3 and _attend(lib, _seq(M=(1 << 30) + 1, page=1)) == -3
+    assert _append(lib, _seq(M=(1 << 30) + 1, page=1)) == -3
+
+
+def test_bounds_beyond_any_sequence_ask_for_no_more(lib):
+    import torch
+    need = binding.approxifer_attend_workspace_bytes
+    huge = 2 ** 63 - 1
+    assert need(4, 2, 4, 2, 64, torch.float16, 1, huge) == need(4, 2, 4, 2, 64, torch.float16, 1, 1 << 30) > 0
+    assert need(4, 2, 4, 2, 64, torch.float16, huge, huge, huge, huge) == need(4, 2, 4, 2, 64, torch.float16, 4, 1 << 30)
+    assert need(400, 2, 4, 2, 64, torch.float32, 200, 9000, 500, huge) == need(400, 2, 4, 2, 64, torch.float32, 200, 9000, 500, 1 << 30)
+
+
 def test_new_codes_have_texts_of_their_own(lib):
     texts = {binding.strerror(code) for code in range(0, -13, -1)}
     assert len(texts) == 13 and not any("unknown" in t for t in texts)
