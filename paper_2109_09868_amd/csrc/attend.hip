@@ -14,6 +14,10 @@ int token_rows(int dtype) { return dtype == APPROXIFER_F32 ? 64 : 16; }
 // Workgroups that it is given if keys are cut: two on every CU, in one round.  With 256 / 512 / 768 / 1024 / 2048 three sequences of up to
 // 131072 keys take 258 / 244 / 257 / 257 / 255 us.
 constexpr int64_t kTokenGroups = 512;
+// Where that leaves more than a seventh of the places empty, as many as make three rounds, if each still has 24 tiles: 264 heads of sequences
+// of 4000 keys (bf16, 128) 108 us in six parts each and 136 in one, 288 (32 bits, 64) 116 and 144; with 1000 keys 40 us either way, and
+// 384 windows of 1024 keys 44 us whole, 53 in two parts.
+constexpr int64_t kTokenRounds = 3, kTokenChunk = 24;
 
 // How the tokens kernel cuts the keys of a call into parts, given what workspace there is.
 TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
@@ -27,6 +31,12 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     }
     int64_t parts = kTokenGroups / (pairs * blocks > 0 ? pairs * blocks : 1);
     parts = parts < (tiles + 7) / 8 ? parts : (tiles + 7) / 8;           // two tiles a wave at least
+    const int64_t groups = pairs * blocks * (parts > 1 ? parts : 1), places = (groups + kTokenGroups - 1) / kTokenGroups * kTokenGroups;
+    if (groups * 7 < places * 6) {
+        int64_t more = (kTokenRounds * kTokenGroups + pairs * blocks - 1) / (pairs * blocks > 0 ? pairs * blocks : 1);
+        more = more < tiles / kTokenChunk ? more : tiles / kTokenChunk;
+        parts = parts > more ? parts : more;
+    }
     const int64_t room = static_cast<int64_t>(workspace_bytes) / (pairs * blocks * part_floats(16, Dh) * 4 + 1);
     parts = parts < room ? parts : room;
     TokenGrid g;
