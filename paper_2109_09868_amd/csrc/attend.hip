@@ -1,4 +1,6 @@
 // Attention over a cache in pages: which kernel a call takes, and how its keys are cut.
+#include <cmath>
+
 #include "attend_tiles.h"
 #include "attend_tokens.h"
 
@@ -53,11 +55,25 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     return g;
 }
 
-// Workgroups that the tiles kernel is given if keys are cut, again two on every CU, and fewest tiles of 64 keys in a part.  With 512 / 768 /
-// 1024: 16 tokens of 4 sequences of up to 40000 keys 106 / 136 / 118 us, 64 of 60000 keys 107 / 101 / 118, 512 of 60000 612 / 635 / 579.
-constexpr int64_t kTileGroups = 512, kTileChunk = 8;
+// Into how many parts the tiles kernel cuts the keys of `heads` tiles of rows and cache heads.  A part takes `tile_us` a tile of 64 keys, all of
+// them at once as long as the GPU has room; the parts of a row are written and read again at 4.5 bytes a ps, and joined by a launch of
+// about 6 us more.  So sqrt(tiles tile_us / us a part) of them are the least time, if that is less than without any.  Whole / two or three / more
+// parts: 1000 tokens of 32 heads on 8 (bf16, 128) 30 us / 46 in two, 16 tokens of 4 sequences of up to 40000 keys 932 / 106 in sixteen; in 32 bits four
+// prompts of 500 (8 heads of 128) 80 / 60 / 71, one of 1000 (4 heads on one) 49 in four, 35 in eight.
+int64_t tile_parts(int64_t rows, int64_t heads, int64_t tiles, int Dh, int dtype) {
+    const bool wide = dtype == APPROXIFER_F32;
+    const int64_t places = Dh > 128 || (wide && Dh > 64) ? 256 : wide ? 768 : 512;       // workgroups at a time
+    int64_t most = places / (heads > 0 ? heads : 1);
+    most = most < tiles / 2 ? most : tiles / 2;
+    if (most < 2) return 1;
+    const double tile_us = Dh * (!wide ? 0.0086 : Dh > 64 ? 0.0625 : 0.053);
+    const double part_us = static_cast<double>(rows) * Dh * 8.0 / 4.5e6;
+    int64_t parts = static_cast<int64_t>(std::sqrt(tiles * tile_us / part_us) + 0.5);
+    parts = parts < most ? parts : most;
+    return parts < 2 || tiles * tile_us / parts + parts * part_us + 6.0 > tiles * tile_us ? 1 : parts;
+}
 
-TileGrid tile_grid(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
+TileGrid tile_grid(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
                    size_t workspace_bytes) {
     const int64_t group = Hq / Hkv;
     TileGrid g;
@@ -70,8 +86,7 @@ TileGrid tile_grid(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int64_t max_ro
     }
     // half of the tiles that only make up a sequence's number can be empty
     const int64_t heads = (g.single ? B : T * group / kTileRows + (B + 1) / 2) * Hkv;
-    int64_t parts = kTileGroups / (heads > 0 ? heads : 1);
-    parts = parts < tiles / kTileChunk ? parts : tiles / kTileChunk;
+    int64_t parts = tile_parts(T * Hq, heads, tiles, Dh, dtype);
     const int64_t room = static_cast<int64_t>(workspace_bytes) / (g.slots * Hkv * part_floats(kTileRows, Dh) * 4 + 1);
     parts = parts < room ? parts : room;
     g.parts = static_cast<int>(parts < 2 ? 1 : parts);
@@ -86,7 +101,7 @@ size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int
     constexpr size_t kAll = static_cast<size_t>(1) << 60;
     max_rows = max_rows < T ? max_rows : T;
     if (max_rows * (Hq / Hkv) > token_rows(dtype)) {
-        const TileGrid g = tile_grid(T, B, Hq, Hkv, Dh, max_rows, max_len, window, sinks, kAll);
+        const TileGrid g = tile_grid(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll);
         return g.parts < 2 ? 0 : static_cast<size_t>(g.slots) * Hkv * g.parts * part_floats(kTileRows, Dh) * 4;
     }
     const TokenGrid g = token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll);
@@ -97,7 +112,8 @@ int launch_attend(const AttendCall &c, void *workspace, size_t workspace_bytes, 
     const int dtype = c.dtype;
     float *const w = static_cast<float *>(workspace);
     if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) > token_rows(dtype)) {
-        const TileGrid g = tile_grid(c.seq.T, c.seq.B, c.Hq, c.Hkv, c.Dh, c.max_rows, c.max_len, c.window, c.sinks, workspace_bytes);
+        const TileGrid g = tile_grid(c.seq.T, c.seq.B, c.Hq, c.Hkv, c.Dh, dtype, c.max_rows, c.max_len, c.window, c.sinks,
+                                     workspace_bytes);
         return launch_status(dtype == APPROXIFER_F32   ? launch_tiles_f32(c, g, w, stream)
                              : dtype == APPROXIFER_F16 ? launch_tiles_f16(c, g, w, stream)
                                                        : launch_tiles_bf16(c, g, w, stream));
