@@ -18,8 +18,10 @@ class SequenceCache:
     """Keys and values of up to `max_sequences` sequences in `layers` layers: `pages` pages of `page` tokens each, at most
     `max_pages` pages a sequence.
 
-    table, lens and refs always describe the sequences as they stand; status is what the last call said of each.  fork()
-    changes how many sequences there are.
+    table, lens and refs always describe the sequences as they stand; status is what the last call said of each, refused what the last
+    reserve() or fork() said.  A sequence that was refused room has no place for the new tokens that come with the others':
+    append() writes nothing of them to the pages and attend() answers zeros, until it is reserved again.  fork() changes how many
+    sequences there are.
     """
 
     def __init__(self, layers, heads, kv_heads, head_dim, max_sequences, max_pages, pages, device, page=16, dtype=None, window=0, sinks=0,
@@ -38,6 +40,9 @@ class SequenceCache:
         self._lens = [torch.zeros((max_sequences,), dtype=i32, device=device) for _ in range(2)]
         self._refs = [torch.zeros((pages,), dtype=i32, device=device) for _ in range(2)]
         self._status = torch.zeros((max_sequences,), dtype=i32, device=device)
+        self._refused = torch.zeros((max_sequences,), dtype=i32, device=device)
+        # lengths as append() and attend() see them: 0 for those that were refused, whose new tokens then have no place
+        self._roomy = torch.zeros((max_sequences,), dtype=i32, device=device)
         self.moved = torch.empty((pages,), dtype=i32, device=device)
         self.live = torch.empty((1,), dtype=i32, device=device)
         self._now = 0
@@ -61,6 +66,17 @@ class SequenceCache:
     def status(self):
         return self._status[:self.sequences]
 
+    @property
+    def refused(self):
+        return self._refused[:self.sequences]
+
+    def _settle(self, lost=None):
+        """After a call that gives room: who was refused (or is lost already), and whom the others' calls therefore pass by."""
+        import torch
+        self.refused.copy_(self.status if lost is None else torch.where(lost == 0, self.status, lost))
+        torch.mul(self.lens, self.refused == 0, out=self._roomy[:self.sequences])
+        return self.refused
+
     def begin(self, sequences):
         """`sequences` empty sequences; whatever was there is dropped."""
         if not 0 <= sequences <= self.max_sequences:
@@ -68,31 +84,38 @@ class SequenceCache:
         self.sequences = sequences
         self.lens.zero_()
         self.refs.zero_()
+        self.status.zero_()
+        self._settle()
 
-    def reserve(self, add):
-        """Room for add[b] more tokens (an int32 device tensor, or a number for all) of every sequence."""
+    def reserve(self, add, lost=None):
+        """Room for add[b] more tokens (an int32 device tensor, or a number for all) of every sequence but those where lost (an int32
+        device tensor of statuses, or None) is not 0: they get none, and stay refused with that status.  Returns refused."""
         import torch
         if not isinstance(add, torch.Tensor):
             add = torch.full((self.sequences,), int(add), dtype=torch.int32, device=self.device)
+        if lost is not None:
+            add = add * (lost == 0)
         binding.approxifer_cache_reserve(self.table, self.lens, self.refs, add, self.page, status=self.status)
-        return self.status
+        return self._settle(lost)
 
     def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
         """The new tokens' heads, normed and rotated; keys and values go to their pages.  Returns the queries."""
         import torch
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        binding.approxifer_append(q, k, v, self.pools[layer, 0], self.pools[layer, 1], self.table, self.lens, starts, self.freq,
+        binding.approxifer_append(q, k, v, self.pools[layer, 0], self.pools[layer, 1], self.table,
+                                  self._roomy[:self.sequences], starts, self.freq,
                                   q_weight=q_weight, k_weight=k_weight, positions=positions, axis=axis, q_out=out, status=self.status)
         return out
 
     def attend(self, layer, q, starts, max_rows, max_len):
         """What the new tokens read in their sequences: [T, heads, head_dim]."""
-        out, _ = binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self.lens, starts, max_rows,
-                                           max_len, window=self.window, sinks=self.sinks, status=self.status)
+        out, _ = binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self._roomy[:self.sequences], starts,
+                                           max_rows, max_len, window=self.window, sinks=self.sinks, status=self.status)
         return out
 
     def fork(self, parents, keep=None):
-        """Sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens: lists or int32 device tensors."""
+        """Sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens: lists or int32 device tensors.
+        Returns refused: a sequence for which there was no page is empty."""
         import torch
         parents, keep = (x if x is None or isinstance(x, torch.Tensor) else torch.tensor(x, dtype=torch.int32, device=self.device)
                          for x in (parents, keep))
@@ -104,7 +127,7 @@ class SequenceCache:
                                       table_out=self._tables[new][:n], lens_out=self._lens[new][:n], refs_out=self._refs[new],
                                       status=self._status[:n], workspace=self._workspace)
         self._now, self.sequences = new, n
-        return self.status
+        return self._settle()
 
     def compact(self):
         """Moves live pages together; afterwards pages live[0] and up are free."""
@@ -154,12 +177,26 @@ class CodedSequences:
     tokens of all queries [G, K, n, width], encodes them, lets every worker's sequence read its coded tokens, and decodes
     the fastest N - S workers' predictions for the last token.  nodes: (alpha, beta) instead of the library's; with the
     same K nodes twice the code is the identity, and every query is one worker's.
+
+    lost [G, N] int32 holds the first status other than 0 that the cache has had for each worker's sequence: one that got no page,
+    or no place in its table, misses tokens from then on.  Such a worker counts as one that never answers, so a group can
+    spare S of them; a group that has lost more gets APPROXIFER_GROUP_BAD_MASK from the decoder, and values of 0.
     """
 
     def __init__(self, model, cache, G, K, N, S, sign_mode=binding.SIGN_SURVIVOR_RANK, nodes=None):
         self.model, self.cache, self.G, self.K, self.N, self.S, self.sign_mode = model, cache, G, K, N, S, sign_mode
         self.alpha, self.beta = nodes or binding.approxifer_chebyshev_nodes(K, N)
         self.length = 0
+        self._lost = None
+
+    @property
+    def lost(self):
+        return self._lost.view(self.G, self.N)
+
+    def _lose(self, statuses):
+        """Keeps the first status other than 0 of every sequence."""
+        import torch
+        self._lost = torch.where(self._lost == 0, statuses, self._lost)
 
     def _starts(self, sequences, n):
         import torch
@@ -169,9 +206,10 @@ class CodedSequences:
         """prompt [n, width].  Berrut's weights sum to one: a token that all queries share is its own coded token."""
         n = prompt.shape[0]
         self.cache.begin(1)
-        self.cache.reserve(n)
+        self._lost = self.cache.reserve(n).clone()
         self.model.read(self.cache, prompt, self._starts(1, n), n, n)
-        self.cache.fork([0] * (self.G * self.N))
+        self._lose(self.cache.status)
+        self._lose(self.cache.fork([0] * (self.G * self.N)))  # what the prompt's sequence missed, all of them miss
         self.length = n
 
     def step(self, tokens, arrival):
@@ -179,17 +217,21 @@ class CodedSequences:
         G, K, N = self.G, self.K, self.N
         n, width = tokens.shape[2], tokens.shape[3]
         coded = binding.approxifer_encode(tokens.reshape(G, K, n * width), self.alpha, self.beta)
-        self.cache.reserve(n)
+        self._lost = self.cache.reserve(n, self._lost).clone()
         self.length += n
         preds = self.model.read(self.cache, coded.view(G * N * n, width), self._starts(G * N, n), n, self.length)
+        self._lose(self.cache.status)
         last = preds.view(G, N, n, -1)[:, :, -1].contiguous()
-        mask, _ = binding.approxifer_wait_mask(arrival, N - self.S)
+        mask, _ = binding.approxifer_wait_mask(arrival.masked_fill(self.lost != 0, float("inf")), N - self.S)
         return binding.approxifer_decode(last, mask, self.alpha, self.beta, self.S, self.sign_mode)
 
     def finish(self, groups):
         """Drops all groups but those listed, in their order, and closes up the pages that this leaves free."""
-        parents = [g * self.N + i for g in groups for i in range(self.N)]
-        self.cache.fork(parents)
+        import torch
+        parents = torch.tensor([g * self.N + i for g in groups for i in range(self.N)], dtype=torch.int32, device=self.cache.device)
+        forked = self.cache.fork(parents)
+        self._lost = self._lost[parents.long()]
+        self._lose(forked)
         self.G = len(groups)
         return self.cache.compact()
 
@@ -241,8 +283,9 @@ def main():
             out.append(coded.step(x, arrival)[0])
         torch.cuda.synchronize()
         rest = (time.perf_counter() - t - first) / max(args.steps, 1)
+        bad = int((coded.lost != 0).sum())
         live = int(coded.finish(list(range(0, G, 2))))
-        return out, first, rest, live, int(cache.status.abs().sum())
+        return out, first, rest, live, bad + int((coded.lost != 0).sum())
 
     serve(N, S)
     got, first, rest, live, bad = serve(N, S)
