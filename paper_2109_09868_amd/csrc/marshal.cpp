@@ -358,7 +358,7 @@ PyObject *append(PyObject *const *a, Py_ssize_t n) {
     if (a[10] != Py_None && (qw = shaped(a[10], c.type, c.Dh)) == nullptr) Py_RETURN_NONE;
     if (a[11] != Py_None && (kw = shaped(a[11], c.type, c.Dh)) == nullptr) Py_RETURN_NONE;
     double eps = 0.0;
-    if (!real(a[12], eps)) Py_RETURN_NONE;
+    if (!real(a[12], eps) || !PyBool_Check(a[15])) Py_RETURN_NONE;    // other truth values are the binding's to read
     int axes = 1;
     if (a[13] != Py_None) {
         const at::Tensor *p = plain(a[13], kI32);

@@ -180,3 +180,8 @@ def test_graph_replays_and_other_streams(binding):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.all((out.cpu().double() - want[0]).abs() <= want[1]) and status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("interleaved", [True, 1, np.True_, np.int64(3), False, 0, np.False_, None], ids=repr)
+def test_what_counts_as_interleaved(binding, interleaved):
+    _run(binding, torch.bfloat16, [20, 3], [20, 1], 4, 2, 64, 16, 32, interleaved=interleaved)
