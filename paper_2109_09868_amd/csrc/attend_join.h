@@ -86,15 +86,15 @@ __device__ __forceinline__ void join_row(const AttendCall &c, const Rows &rows, 
 }
 
 // One wave: `row` of a sequence and cache head h over tiles begin..end-1, element by element, as a part of R rows of which it is the n-th, or
-// the result where there is but one part.  scratch: 320 floats of LDS.
+// the result where there is but one part.  scratch: 256 floats of LDS.
 template <class E, int kKeys>
 __device__ void attend_part(const AttendCall &c, const Rows &rows, int64_t row, int h, float *scratch, const KeyTiles<kKeys> &keys, int begin,
                             int end, bool alone, float *partial, int R, int n) {
     typedef typename E::Value V;
     const int group = c.Hq / c.Hkv, i = static_cast<int>(row / group), head = h * group + static_cast<int>(row % group);
     const int main_from = max(begin, keys.sink_tiles), lane = lane_id();
-    const RowSum y = attend_row<E>(c, rows, i, head, scratch, scratch + APPROXIFER_MAX_HEAD_DIM, begin * kKeys,
-                                   min(end, keys.sink_tiles) * kKeys, main_from < end ? keys.begin_of(main_from) : 0,
+    const RowSum y = attend_row<E>(c, rows, i, head, scratch, begin * kKeys, min(end, keys.sink_tiles) * kKeys,
+                                   main_from < end ? keys.begin_of(main_from) : 0,
                                    main_from < end ? keys.begin_of(end - 1) + kKeys : 0);
     V *const out = static_cast<V *>(c.out) + ((rows.start + i) * c.Hq + head) * c.Dh;
     const float inverse = y.total == 0.0f ? 0.0f : 1.0f / y.total;

@@ -1,6 +1,6 @@
 // Attention of one row to what its sequence holds, straight from the definition: one wave, float32, a key per lane for the
-// scores and a dimension per lane for the sum.  The tiled kernels fall back on it where a tile cannot be computed as a
-// product: a value that is not finite and that some of the tile's rows must not see.
+// scores and a dimension per lane for the sum.  The tiled kernels fall back on it where a row cannot be computed as a
+// product: a value that is not finite times a weight of 0.
 #pragma once
 
 #include "sequences.h"
@@ -33,16 +33,17 @@ struct KeyTiles {
     __device__ __forceinline__ int seen(int j) const { return j > last ? last : j < from && j >= sinks_end ? from : j; }
 };
 
-// One row over the places [a0, a1) and [b0, b1), as far as it sees them.  q: [256] and p: [64] floats of LDS of this wave.  Lane l
-// has dimensions l, l + 64, .. of `out`, not yet divided by `total`; both relative to exp(top).
+// One row over the places [a0, a1) and [b0, b1), as far as it sees them.  q: [256] floats of LDS of this wave.  Lane l has
+// dimensions l, l + 64, .. of `out`, not yet divided by `total`; both relative to exp(top).  Every key's value row takes a load of its
+// own, kAhead of them on their way.
 struct RowSum {
     float out[APPROXIFER_MAX_HEAD_DIM / kWave], top, total;
 };
 template <class E>
-__device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head, float *q, float *p, int a0, int a1, int b0,
-                             int b1) {
+__device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head, float *q, int a0, int a1, int b0, int b1) {
     typedef typename E::Value V;
-    constexpr int kPerLane = APPROXIFER_MAX_HEAD_DIM / kWave;
+    typedef V VP __attribute__((ext_vector_type(16 / sizeof(V))));
+    constexpr int kPerLane = APPROXIFER_MAX_HEAD_DIM / kWave, kPiece = 16 / sizeof(V), kAhead = 4;
     const int lane = lane_id(), h = head / (c.Hq / c.Hkv), size = 1 << c.seq.page_shift;
     const int64_t t = r.start + i;
     const V *x = static_cast<const V *>(c.q) + t * c.q_stride + static_cast<int64_t>(head) * c.Dh;
@@ -55,18 +56,23 @@ __device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head
     for (int part = 0; part < 2; ++part) {
         const int from = part ? b0 : a0, to = min(part ? b1 : a1, see.place + 1);
         for (int j0 = from; j0 < to; j0 += kWave) {
-            const int j = j0 + lane, count = min(to - j0, kWave);
+            const int j = j0 + lane;
             const bool mine = j < to && see.sees(j);
             float s = -INFINITY;
+            int page = -1;
             if (mine) {
-                const int page = page_of(c.seq, r.b, j);
+                page = page_of(c.seq, r.b, j);
                 if (page < 0) {
                     s = NAN;
                 } else {
                     const V *k = static_cast<const V *>(c.k_pool) +
                                  ((static_cast<int64_t>(page) * c.Hkv + h) * size + (j & (size - 1))) * c.Dh;
                     s = 0.0f;
-                    for (int d = 0; d < c.Dh; ++d) s += q[d] * E::load(k[d]);
+                    for (int d = 0; d < c.Dh; d += kPiece) {
+                        const VP x = *reinterpret_cast<const VP *>(k + d);
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e) s += q[d + e] * E::load(x[e]);
+                    }
                 }
             }
             float m = s;
@@ -77,21 +83,26 @@ __device__ RowSum attend_row(const AttendCall &c, const Rows &r, int i, int head
             for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
             y.total = y.total * shrink + sum;
             y.top = next;
-            p[lane] = w;
-            __builtin_amdgcn_wave_barrier();
-            __threadfence_block();
             for (int k = 0; k < kPerLane; ++k) y.out[k] *= shrink;
-            for (int n = 0; n < count; ++n) {
-                if (!see.sees(j0 + n)) continue;
-                const int page = page_of(c.seq, r.b, j0 + n);
-                if (page < 0) continue;
-                const V *v = static_cast<const V *>(c.v_pool) +
-                             ((static_cast<int64_t>(page) * c.Hkv + h) * size + ((j0 + n) & (size - 1))) * c.Dh;
-                for (int k = 0; k < kPerLane; ++k)
-                    if (lane + k * kWave < c.Dh) y.out[k] += p[n] * E::load(v[lane + k * kWave]);
+            for (unsigned long long left = __ballot(page >= 0); left != 0;) {
+                const int count = min(__popcll(left), kAhead);
+                float weight[kAhead], x[kAhead][kPerLane];
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a) {
+                    const int n = __ffsll(left) - 1;          // behind the last one: that again, not used
+                    if (a + 1 < count) left &= left - 1;
+                    weight[a] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(w), n));
+                    const V *v = static_cast<const V *>(c.v_pool) +
+                                 ((static_cast<int64_t>(__builtin_amdgcn_readlane(page, n)) * c.Hkv + h) * size + ((j0 + n) & (size - 1))) * c.Dh;
+#pragma unroll
+                    for (int k = 0; k < kPerLane; ++k) x[a][k] = lane + k * kWave < c.Dh ? E::load(v[lane + k * kWave]) : 0.0f;
+                }
+                left &= left - 1;
+#pragma unroll
+                for (int a = 0; a < kAhead; ++a)
+#pragma unroll
+                    for (int k = 0; k < kPerLane; ++k) y.out[k] += a < count ? weight[a] * x[a][k] : 0.0f;
             }
-            __builtin_amdgcn_wave_barrier();
-            __threadfence_block();
         }
     }
     return y;

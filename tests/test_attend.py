@@ -305,3 +305,25 @@ def test_same_bits_every_time_on_any_stream_and_in_graphs(binding, lens, new):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out.cpu(), first) and status.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("dtype", list(ref.DTYPES.values()), ids=list(ref.DTYPES))
+@pytest.mark.parametrize("length,new", [(300, 1), (300, 70), (300, 300), (9000, 70)])
+@pytest.mark.parametrize("gap", [12.0, 30.0, 80.0])
+def test_an_infinity_of_a_small_weight_reaches_the_rows_that_see_it(binding, dtype, length, new, gap):
+    # every key's score is 0 but that of one at place 20, which is `gap` below: in half precision its weight rounds to 0, and 0 times an
+    # infinity would be no number
+    c = ref.cache(6, dtype, [length], [new], 1, 64, 16)
+    c["k_pool"].zero_()
+    p = int(c["table"][0, 1])
+    c["k_pool"][p, 0, 4, 0] = -gap / 4
+    q = torch.zeros((new, 2, 64), dtype=dtype)
+    q[:, :, 0] = 4.0
+    want, bound = ref.attend(c, q, scale=1.0)
+    c["v_pool"][p, 0, 4, 5], c["v_pool"][p, 0, 4, 6] = math.inf, -math.inf
+    out, status = _call(binding, c, q, scale=1.0)
+    sees = torch.arange(length - new, length) >= 20
+    assert status == [0]
+    assert torch.all(out[sees][:, :, 5] == math.inf) and torch.all(out[sees][:, :, 6] == -math.inf)
+    off, rest = (out.double() - want).abs(), [d for d in range(64) if d not in (5, 6)]
+    assert torch.all(off[~sees] <= bound[~sees]) and torch.all(off[:, :, rest] <= bound[:, :, rest])
