@@ -12,7 +12,12 @@ namespace {
 // the better ones for them.  8 tokens by 4 heads (32 rows) of 8 sequences of up to 40000 keys: 284 us here, 186 there; 32-bit products cost
 // more than memory does, whichever kernel forms them, and the tiles kernel's 128 rows are mostly empty: 16 tokens (64 rows) of up to 6000
 // keys 108 us here, 121 there.
-int token_rows(int dtype) { return dtype == APPROXIFER_F32 ? 64 : 16; }
+// Neither kernel's calls reach 2^32 threads, which a launch cannot have: the tiles kernel's because T Hq / 128 + B Hkv workgroups are enough,
+// and calls that would take more than 2^24 blocks of 16 rows go there.
+bool few_rows(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype) {
+    const int64_t rows = max_rows * (Hq / Hkv), blocks = (rows + 15) / 16;
+    return rows <= (dtype == APPROXIFER_F32 ? 64 : 16) && B * Hkv * blocks + (B + 3) / 4 < 1 << 24;
+}
 // Workgroups that it is given if keys are cut: two on every CU, in one round.  With 256 / 512 / 768 / 1024 / 2048 three sequences of up to
 // 131072 keys take 258 / 244 / 257 / 257 / 255 us.
 constexpr int64_t kTokenGroups = 512;
@@ -100,7 +105,7 @@ size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int
                               int64_t window, int64_t sinks) {
     constexpr size_t kAll = static_cast<size_t>(1) << 60;
     max_rows = max_rows < T ? max_rows : T;
-    if (max_rows * (Hq / Hkv) > token_rows(dtype)) {
+    if (!few_rows(B, Hq, Hkv, max_rows, dtype)) {
         const TileGrid g = tile_grid(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll);
         return g.parts < 2 ? 0 : static_cast<size_t>(g.slots) * Hkv * g.parts * part_floats(kTileRows, Dh) * 4;
     }
@@ -111,7 +116,7 @@ size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int
 int launch_attend(const AttendCall &c, void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const int dtype = c.dtype;
     float *const w = static_cast<float *>(workspace);
-    if (static_cast<int64_t>(c.max_rows) * (c.Hq / c.Hkv) > token_rows(dtype)) {
+    if (!few_rows(c.seq.B, c.Hq, c.Hkv, c.max_rows, dtype)) {
         const TileGrid g = tile_grid(c.seq.T, c.seq.B, c.Hq, c.Hkv, c.Dh, dtype, c.max_rows, c.max_len, c.window, c.sinks,
                                      workspace_bytes);
         return launch_status(dtype == APPROXIFER_F32   ? launch_tiles_f32(c, g, w, stream)
