@@ -417,7 +417,7 @@ int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
  *           must not overlap d_q
  *   max_rows, max_len   bounds of the sequences' numbers of new tokens and lengths: a sequence beyond one is
  *           APPROXIFER_SEQUENCE_BAD.  The work is laid out for them, so close bounds are faster.
- *   window >= 0, sinks >= 0, scale finite
+ *   window >= 0, sinks >= 0, |scale| <= 2^126 (it is used in float32)
  *   d_workspace, workspace_bytes   scratch of the caller's, 16-byte aligned, or NULL / 0, as for
  *           approxifer_decode_byzantine(): long sequences with few rows are split over the GPU, and the parts meet there.
  *           approxifer_attend_workspace_bytes() gives the size with which the call is fastest; with less it is split

@@ -323,7 +323,7 @@ int approxifer_attend(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
     approxifer::AttendCall c;
     int rc = check_sequences(h_seq, Hq, Hkv, Dh, dtype, &c.seq);
     if (rc != APPROXIFER_OK) return rc;
-    if (max_rows < 0 || max_len < 0 || window < 0 || sinks < 0 || !std::isfinite(scale)) return APPROXIFER_ERR_BAD_SHAPE;
+    if (max_rows < 0 || max_len < 0 || window < 0 || sinks < 0 || !(std::fabs(scale) <= 0x1p126)) return APPROXIFER_ERR_BAD_SHAPE;
     if (c.seq.B == 0 && c.seq.T > 0) return APPROXIFER_ERR_BAD_CACHE;
     if (c.seq.B == 0) return APPROXIFER_OK;
     if (c.seq.table == nullptr || c.seq.lens == nullptr || c.seq.starts == nullptr) return APPROXIFER_ERR_NULL_POINTER;

@@ -189,3 +189,11 @@ def test_the_binding_refuses_what_is_no_device_tensor(lib):
         binding.approxifer_cache_fork(pool, table, n[:1], torch.zeros((3,), dtype=torch.int32), n)
     with pytest.raises(TypeError):
         binding.approxifer_cache_compact(pool, table, n[:1], torch.zeros((3,), dtype=torch.int32))
+
+
+def test_scales_that_float32_does_not_hold(lib):
+    # the kernels multiply by scale log2(e) in float32
+    for scale in (1e300, -1e300, 3.4e38, -2.0 ** 127):
+        assert _attend(lib, scale=scale) == -2, scale
+    for scale in (2.0 ** 126, -2.0 ** 126, 1e-300, 0.0):
+        assert _attend(lib, _seq(B=0, T=0), scale=scale) == 0, scale
