@@ -423,8 +423,9 @@ int approxifer_append(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
  *           approxifer_attend_workspace_bytes() gives the size with which the call is fastest; with less it is split
  *           less, and as correct.
  * Rows that see a place in a bad page are NaN.  Scores, softmax and sums are float32; for 16-bit types the weights are
- * rounded before they multiply the values, for many rows to the type, for few (up to 16 of a sequence and head of the
- * cache) to twice its length.  Each output is rounded once.
+ * rounded before they multiply the values, for many rows to the type (which adds about a third to the error that the
+ * output's own rounding makes), for few (up to 16 of a sequence and head of the cache) to twice its length.  Each output
+ * is rounded once.
  * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE, ERR_BAD_CACHE, ERR_LIMIT, ERR_BAD_DTYPE, ERR_ALIGNMENT or ERR_LAUNCH; the
  * call may consist of two launches.
  */

@@ -13,8 +13,9 @@
 // (else by registers), two tiles of each and one barrier a tile.  Rows of LDS are permuted in pieces of 16 bytes so that both kinds of reads spread over all banks.
 //
 // Bound by the matrix cores and the vector units, one after the other, at the clock that power leaves: two prompts of 4099 and 7001 tokens (32 heads of
-// 128 on 8, bf16) 641 to 665 us on different cards, 950 TFLOP/s; 12001 tokens of 24 heads of 64 in a window of 2048 (fp16) 198 us, 700 TFLOP/s; 192
-// texts of 128 tokens, 12 heads of 64 in 32 bits, 102 us, 47 TFLOP/s and 3.0 TB/s, which wait for their loads.
+// 128 on 8, bf16) 636 to 704 us by card, 981 to 886 TFLOP/s; 12001 tokens of 24 heads of 64 in a window of 2048 (fp16) 193 to 209 us, 715 to 661
+// TFLOP/s; 192 texts of 128 tokens, 12 heads of 64 in 32 bits, 100 to 103 us, 48 TFLOP/s and 3.0 TB/s: their four waves have 1, 2, 3 and 4 tiles
+// and meet after each, and wait for their first loads.
 #pragma once
 
 #include "attend_join.h"
@@ -326,6 +327,9 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                 }
             total += sum;
             if constexpr (S::kSize == 2) {
+                // weights in one piece of their type, at 2.1e-3 (bf16) and 2.7e-4 (fp16) of the outputs' norm from 64 bits; in two pieces, as the
+                // few-rows kernel has them, 1.6e-3 and 2.0e-4, as the result's own rounding, but the two prompts of bf16 take 884 us
+                // instead of 671 and the window of fp16 265 instead of 198
                 const int i = lane & 15, quad = lane >> 4 & 1;
 #pragma unroll
                 for (int n = 0; n < kKeys / 16; ++n) {
