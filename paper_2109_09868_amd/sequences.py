@@ -10,6 +10,8 @@ caller's hosted model (projections are torch's products, weights are drawn from 
 """
 from __future__ import annotations
 
+import math
+
 import numpy as np
 
 from . import binding
@@ -40,78 +42,85 @@ class SequenceCache:
         self._tables = [torch.full((max_sequences, max_pages), -1, dtype=i32, device=device) for _ in range(2)]
         self._lens = [torch.zeros((max_sequences,), dtype=i32, device=device) for _ in range(2)]
         self._refs = [torch.zeros((pages,), dtype=i32, device=device) for _ in range(2)]
-        self._status = torch.zeros((max_sequences,), dtype=i32, device=device)
-        self._refused = torch.zeros((max_sequences,), dtype=i32, device=device)
-        # lengths as append() and attend() see them: 0 for those that were refused, whose new tokens then have no place
-        self._roomy = torch.zeros((max_sequences,), dtype=i32, device=device)
+        # whole: where refused is 0; _seen: lengths as append() and attend() see them, 0 for those that were refused, whose new tokens then
+        # have no place; _asked: what reserve() asks for
+        self._each = {name: torch.zeros((max_sequences,), dtype=torch.bool if name == "whole" else i32, device=device)
+                      for name in ("status", "refused", "whole", "_seen", "_asked")}
         self.moved = torch.empty((pages,), dtype=i32, device=device)
         self.live = torch.empty((1,), dtype=i32, device=device)
-        self._now = 0
-        self.sequences = 0
+        self._show(0, 0)
         need = binding.approxifer_cache_workspace_bytes(max_sequences, max_sequences, pages)
         self._workspace = torch.empty((need,), dtype=torch.uint8, device=device)
 
-    @property
-    def table(self):
-        return self._tables[self._now][:self.sequences]
+    def _show(self, now, n):
+        """The first n sequences of the set `now` are the ones that there are."""
+        self._now, self.sequences = now, n
+        self.table, self.lens, self.refs = self._tables[now][:n], self._lens[now][:n], self._refs[now]
+        for name, t in self._each.items():
+            setattr(self, name, t[:n])
 
-    @property
-    def lens(self):
-        return self._lens[self._now][:self.sequences]
-
-    @property
-    def refs(self):
-        return self._refs[self._now]
-
-    @property
-    def status(self):
-        return self._status[:self.sequences]
-
-    @property
-    def refused(self):
-        return self._refused[:self.sequences]
-
-    def _settle(self, lost=None):
-        """After a call that gives room: who was refused (or is lost already), and whom the others' calls therefore pass by."""
+    def _settle(self):
+        """Whom the calls for new tokens pass by, after refused has changed."""
         import torch
-        self.refused.copy_(self.status if lost is None else torch.where(lost == 0, self.status, lost))
-        torch.mul(self.lens, self.refused == 0, out=self._roomy[:self.sequences])
+        torch.eq(self.refused, 0, out=self.whole)
+        torch.mul(self.lens, self.whole, out=self._seen)
         return self.refused
 
     def begin(self, sequences):
         """`sequences` empty sequences; whatever was there is dropped."""
         if not 0 <= sequences <= self.max_sequences:
             raise ValueError("at most %d sequences" % self.max_sequences)
-        self.sequences = sequences
+        self._show(self._now, sequences)
         self.lens.zero_()
         self.refs.zero_()
         self.status.zero_()
+        self.refused.zero_()
         self._settle()
 
     def reserve(self, add, lost=None):
         """Room for add[b] more tokens (an int32 device tensor, or a number for all) of every sequence but those where lost (an int32
-        device tensor of statuses, or None) is not 0: they get none, and stay refused with that status.  Returns refused."""
+        device tensor of statuses: refused itself, to go on without those; or None) is not 0: they get none, and stay refused with that
+        status.  Returns refused."""
         import torch
-        if not isinstance(add, torch.Tensor):
-            add = torch.full((self.sequences,), int(add), dtype=torch.int32, device=self.device)
-        if lost is not None:
-            add = add * (lost == 0)
+        number = None if isinstance(add, torch.Tensor) else min(int(add), 2 ** 31 - 1)
+        if lost is None:
+            add = self._asked.fill_(number) if number is not None else add
+        else:
+            if lost is not self.refused:
+                self.refused.copy_(lost)
+            torch.eq(self.refused, 0, out=self.whole)
+            add = torch.mul(self.whole, number, out=self._asked) if number is not None else add * self.whole
         binding.approxifer_cache_reserve(self.table, self.lens, self.refs, add, self.page, status=self.status)
-        return self._settle(lost)
+        if lost is None:
+            self.refused.copy_(self.status)
+        else:
+            self.refused.add_(self.status)                    # 0 for those that are lost: they have asked for nothing
+        return self._settle()
+
+    def lose(self):
+        """Sequences of whose tokens the last append() or attend() told something else than 0 are refused from now on."""
+        import torch
+        self.refused.add_(self.status)                        # 0 for those that are refused already: their calls saw no places
+        torch.eq(self.refused, 0, out=self.whole)
 
     def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
         """The new tokens' heads, normed and rotated; keys and values go to their pages.  Returns the queries."""
         import torch
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         binding.approxifer_append(q, k, v, self.pools[layer, 0], self.pools[layer, 1], self.table,
-                                  self._roomy[:self.sequences], starts, self.freq,
-                                  q_weight=q_weight, k_weight=k_weight, positions=positions, axis=axis, q_out=out, status=self.status)
+                                  self._seen, starts, self.freq, q_weight=q_weight, k_weight=k_weight, positions=positions, axis=axis,
+                                  q_out=out, status=self.status)
         return out
 
     def attend(self, layer, q, starts, max_rows, max_len):
         """What the new tokens read in their sequences: [T, heads, head_dim]."""
-        out, _ = binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self._roomy[:self.sequences], starts,
-                                           max_rows, max_len, window=self.window, sinks=self.sinks, status=self.status)
+        import torch
+        out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        need = binding.approxifer_attend_workspace_bytes(q.shape[0], self.sequences, self.heads, self.kv_heads, self.head_dim, self.dtype,
+                                                         max_rows, max_len, self.window, self.sinks)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else binding.NO_WORKSPACE
+        binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self._seen, starts, max_rows, max_len,
+                                  window=self.window, sinks=self.sinks, out=out, status=self.status, workspace=workspace)
         return out
 
     def fork(self, parents, keep=None):
@@ -126,8 +135,9 @@ class SequenceCache:
         new = 1 - self._now
         binding.approxifer_cache_fork(self.pools, self.table, self.lens, self.refs, parents, keep=keep,
                                       table_out=self._tables[new][:n], lens_out=self._lens[new][:n], refs_out=self._refs[new],
-                                      status=self._status[:n], workspace=self._workspace)
-        self._now, self.sequences = new, n
+                                      status=self._each["status"][:n], workspace=self._workspace)
+        self._show(new, n)
+        self.refused.copy_(self.status)
         return self._settle()
 
     def compact(self):
@@ -188,16 +198,19 @@ class CodedSequences:
         self.model, self.cache, self.G, self.K, self.N, self.S, self.sign_mode = model, cache, G, K, N, S, sign_mode
         self.alpha, self.beta = nodes or binding.approxifer_chebyshev_nodes(K, N)
         self.length = 0
-        self._lost = None
 
     @property
     def lost(self):
-        return self._lost.view(self.G, self.N)
+        return self.cache.refused.view(self.G, self.N)
 
-    def _lose(self, statuses):
-        """Keeps the first status other than 0 of every sequence."""
+    def _fork(self, parents):
+        """What a parent has missed, its children miss too."""
         import torch
-        self._lost = torch.where(self._lost == 0, statuses, self._lost)
+        parents = torch.tensor(parents, dtype=torch.int32, device=self.cache.device)
+        lost = self.cache.refused[parents.long()]
+        refused = self.cache.fork(parents)
+        refused.copy_(torch.where(lost == 0, refused, lost))
+        self.cache._settle()
 
     def _starts(self, sequences, n):
         import torch
@@ -207,32 +220,29 @@ class CodedSequences:
         """prompt [n, width].  Berrut's weights sum to one: a token that all queries share is its own coded token."""
         n = prompt.shape[0]
         self.cache.begin(1)
-        self._lost = self.cache.reserve(n).clone()
+        self.cache.reserve(n)
         self.model.read(self.cache, prompt, self._starts(1, n), n, n)
-        self._lose(self.cache.status)
-        self._lose(self.cache.fork([0] * (self.G * self.N)))  # what the prompt's sequence missed, all of them miss
+        self.cache.lose()
+        self._fork([0] * (self.G * self.N))
         self.length = n
 
     def step(self, tokens, arrival):
         """tokens [G, K, n, width] float32; arrival [G, N] response times.  Returns (values [G, K, classes], status [G])."""
+        import torch
         G, K, N = self.G, self.K, self.N
         n, width = tokens.shape[2], tokens.shape[3]
         coded = binding.approxifer_encode(tokens.reshape(G, K, n * width), self.alpha, self.beta)
-        self._lost = self.cache.reserve(n, self._lost).clone()
+        self.cache.reserve(n, lost=self.cache.refused)
         self.length += n
         preds = self.model.read(self.cache, coded.view(G * N * n, width), self._starts(G * N, n), n, self.length)
-        self._lose(self.cache.status)
+        self.cache.lose()
         last = preds.view(G, N, n, -1)[:, :, -1].contiguous()
-        mask, _ = binding.approxifer_wait_mask(arrival.masked_fill(self.lost != 0, float("inf")), N - self.S)
+        mask, _ = binding.approxifer_wait_mask(torch.where(self.cache.whole.view(G, N), arrival, math.inf), N - self.S)
         return binding.approxifer_decode(last, mask, self.alpha, self.beta, self.S, self.sign_mode)
 
     def finish(self, groups):
         """Drops all groups but those listed, in their order, and closes up the pages that this leaves free."""
-        import torch
-        parents = torch.tensor([g * self.N + i for g in groups for i in range(self.N)], dtype=torch.int32, device=self.cache.device)
-        forked = self.cache.fork(parents)
-        self._lost = self._lost[parents.long()]
-        self._lose(forked)
+        self._fork([g * self.N + i for g in groups for i in range(self.N)])
         self.G = len(groups)
         return self.cache.compact()
 
