@@ -4,9 +4,9 @@
         -> coded tokens appended and attended to, one or many at a time -> predictions, decoded by the serving loop's calls
         -> sequences that ended are dropped, pages close up
 
-Every step on the cache is one call of the C ABI.  Pools, tables and the page calls' workspace are allocated once, the new tokens' queries
-and outputs and attention's scratch with every call.  SequenceModel is a stand-in for the
-caller's hosted model (projections are torch's products, weights are drawn from a seed); there is no CPU path here.
+Every step on the cache is one call of the C ABI, and a few of torch's on the sequences' statuses.  Pools, tables and the page calls'
+workspace are allocated once, the new tokens' queries and outputs and attention's scratch with every call.  SequenceModel is a stand-in
+for the caller's hosted model (projections are torch's products, weights are drawn from a seed); there is no CPU path here.
 """
 from __future__ import annotations
 
