@@ -488,6 +488,34 @@ int approxifer_cache_compact(int32_t *d_table, const int32_t *d_lens, int32_t *d
  * that they refuse.  Host arithmetic only. */
 size_t approxifer_cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P);
 
+/*
+ * Eviction: every sequence of more than `budget` tokens keeps that many.  Its `first` first and `recent` last tokens stay, and of
+ * those between them the ones with the largest masses (approxifer_attend_mass() adds them up; equal ones: the lower place; NaN is
+ * less than any number).  What stays keeps its order and closes up: the token that was at the i-th kept place is at place i, in all
+ * pools.  Keys keep the rotation that they were appended with, so new tokens' positions are then the caller's to give.
+ * Sequences of at most `budget` tokens stay as they are.
+ *   d_mass      [B][mass_stride] float32, one for each place; of a sequence that is cut they close up too, and the places that it
+ *               gives up get 0.  mass_stride >= 0; a sequence longer than that is bad.
+ *   d_kept      [B][budget] int32, written: the places that are kept, ascending, then -1 (all of them -1 where the status is not OK)
+ *   d_pools     [planes][P][heads][page][row_bytes], 16-byte aligned, row_bytes a multiple of 16 up to 1024; may be NULL with
+ *               planes = 0.  Only places below `budget` are written, and of these none before the first page that changes.
+ * Pages that a sequence holds alone are written in place.  One that has other holders too, and of which a token moves (or that is the
+ * last one and not full), is left to them, and a free page takes its place: lowest index first, in the order of the sequences, as
+ * they were free when the call began.  Pages behind the budget are given back, and their table entries become -1.
+ *   1 <= budget <= 2^30, first >= 0, recent >= 0, first + recent <= budget
+ *   d_status    [B]: APPROXIFER_SEQUENCE_BAD (length outside 0 .. M page, or beyond mass_stride), APPROXIFER_SEQUENCE_BAD_PAGE (it is
+ *               to be cut, and a page of it is not in 0 .. P - 1, or has no holder), APPROXIFER_SEQUENCE_NO_PAGES (the free pages end
+ *               before this sequence; later ones that want any end so too): the sequence stays as it is
+ *   d_workspace at least approxifer_cache_evict_workspace_bytes(B, budget, P, page) bytes, 16-byte aligned
+ * Returns OK, ERR_NULL_POINTER, ERR_BAD_SHAPE (planes, heads, row_bytes, mass_stride, budget, first, recent), ERR_BAD_CACHE, ERR_LIMIT,
+ * ERR_ALIGNMENT, ERR_WORKSPACE or ERR_LAUNCH; the call consists of several launches.
+ */
+int approxifer_cache_evict(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, float *d_mass, int64_t mass_stride, int32_t *d_kept,
+                           int32_t *d_status, void *d_pools, int64_t planes, int64_t heads, int64_t row_bytes, int64_t B, int64_t M,
+                           int64_t P, int page, int64_t budget, int64_t first, int64_t recent, void *d_workspace, size_t workspace_bytes,
+                           void *stream);
+size_t approxifer_cache_evict_workspace_bytes(int64_t B, int64_t budget, int64_t P, int page);
+
 /* Text for a return code; never NULL.  The string is static. */
 const char *approxifer_strerror(int code);
 

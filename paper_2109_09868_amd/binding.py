@@ -51,6 +51,8 @@ EXPORTS = (
     "approxifer_cache_fork",
     "approxifer_cache_compact",
     "approxifer_cache_workspace_bytes",
+    "approxifer_cache_evict",
+    "approxifer_cache_evict_workspace_bytes",
 )
 
 
@@ -139,6 +141,10 @@ def load() -> ctypes.CDLL:
     lib.approxifer_cache_compact.argtypes = [vp] * 6 + [q] * 5 + [i, vp, z, vp]
     lib.approxifer_cache_workspace_bytes.restype = z
     lib.approxifer_cache_workspace_bytes.argtypes = [q, q, q]
+    lib.approxifer_cache_evict.restype = i
+    lib.approxifer_cache_evict.argtypes = [vp, vp, vp, vp, q, vp, vp, vp] + [q] * 6 + [i, q, q, q, vp, z, vp]
+    lib.approxifer_cache_evict_workspace_bytes.restype = z
+    lib.approxifer_cache_evict_workspace_bytes.argtypes = [q, q, q, i]
     _lib = lib
     return lib
 
@@ -202,7 +208,7 @@ def _marshal():
         module, handle = _marshal_module(), None
         if module is not None:
             names = ("encode", "decode", "decode_top1", "decode_byzantine", "decode_byzantine_homogeneous", "pad_last_group",
-                     "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact")
+                     "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact", "cache_evict")
             handle = module.bind(*(ctypes.cast(getattr(lib, "approxifer_" + n), ctypes.c_void_p).value for n in names))
         _ordinary = (lib, module, handle)
     return _ordinary[1], _ordinary[2]
@@ -744,3 +750,41 @@ def approxifer_cache_compact(pools, table, lens, refs, moved=None, live=None, wo
         _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(moved, i32, (P,)), _dev(live, i32, (1,)), at, planes,
         page_bytes, B, M, P, page, ws_ptr, ws_bytes, _stream_handle(stream)))
     return moved, live
+
+
+def approxifer_cache_evict_workspace_bytes(B: int, budget: int, P: int, page: int) -> int:
+    """Bytes of scratch memory that approxifer_cache_evict needs."""
+    return int(load().approxifer_cache_evict_workspace_bytes(int(B), int(budget), int(P), int(page)))
+
+
+def approxifer_cache_evict(pools, table, lens, refs, mass, budget, first=0, recent=0, kept=None, status=None, workspace=None,
+                           stream=None):
+    """Cuts every sequence of more than `budget` tokens to that many, in place: its `first` first and `recent` last ones and those of the
+    largest mass between them, in their order.  pools [.., P, Hkv, page, Dh] hold all layers' keys and values; table [B, M], lens
+    [B], refs [P] int32, mass [B, L] float32.  Returns (kept [B, budget] int32: the places that stay, then -1; status [B] int32)."""
+    if kept is not None and status is not None and workspace is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.cache_evict(lib, pools, table, lens, refs, mass, budget, first, recent, kept, status,
+                                                           workspace)):
+            return kept, status
+    import torch
+    i32 = torch.int32
+    B, M = table.shape
+    P, budget = refs.numel(), int(budget)
+    at, planes, _, page = _planes(pools, P)
+    if not isinstance(mass, torch.Tensor) or mass.dim() != 2:
+        raise TypeError("mass is a tensor [B, L]")
+    with _on(stream):
+        if kept is None:
+            kept = torch.empty((B, max(budget, 0)), dtype=i32, device=table.device)
+        if status is None:
+            status = torch.full((B,), -1, dtype=i32, device=table.device)
+        if workspace is None:
+            workspace = torch.empty((approxifer_cache_evict_workspace_bytes(B, budget, P, page),), dtype=torch.uint8, device=table.device)
+    ws_ptr, ws_bytes = _scratch(workspace)
+    _check(_entry().approxifer_cache_evict(
+        _dev(table, i32), _dev(lens, i32, (B,)), _dev(refs, i32), _dev(mass, torch.float32, (B, mass.shape[1])), mass.shape[1],
+        _dev(kept, i32, (B, max(budget, 0))), _dev(status, i32, (B,)), at, planes, pools.shape[-3],
+        pools.shape[-1] * pools.element_size(), B, M, P, page, budget, int(first), int(recent), ws_ptr, ws_bytes,
+        _stream_handle(stream)))
+    return kept, status

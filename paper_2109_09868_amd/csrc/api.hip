@@ -82,7 +82,7 @@ int check_pools(const void *d_pools, int64_t planes, int64_t page_bytes, int64_t
 
 extern "C" {
 
-int approxifer_version(void) { return 400; }   // 0.4.0: sequences in pages
+int approxifer_version(void) { return 500; }   // 0.5.0: shared prefixes, attention that adds up its weights, eviction
 
 const char *approxifer_strerror(int code) {
     switch (code) {
@@ -415,6 +415,36 @@ int approxifer_cache_compact(int32_t *d_table, const int32_t *d_lens, int32_t *d
 size_t approxifer_cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P) {
     if (B < 0 || B_out < 0 || P < 1 || B > APPROXIFER_MAX_SEQUENCES || B_out > APPROXIFER_MAX_SEQUENCES || P > APPROXIFER_MAX_PAGES) return 0;
     return approxifer::cache_workspace_bytes(B, B_out, P);
+}
+
+int approxifer_cache_evict(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, float *d_mass, int64_t mass_stride, int32_t *d_kept,
+                           int32_t *d_status, void *d_pools, int64_t planes, int64_t heads, int64_t row_bytes, int64_t B, int64_t M,
+                           int64_t P, int page, int64_t budget, int64_t first, int64_t recent, void *d_workspace, size_t workspace_bytes,
+                           void *stream) {
+    int shift = 0;
+    int rc = check_cache(B, M, P, page, &shift);
+    if (rc != APPROXIFER_OK) return rc;
+    if (heads < 0 || row_bytes < 0 || mass_stride < 0 || budget < 1 || first < 0 || recent < 0 || first > budget || recent > budget - first)
+        return APPROXIFER_ERR_BAD_SHAPE;
+    if (heads > APPROXIFER_MAX_HEADS || row_bytes > 4 * APPROXIFER_MAX_HEAD_DIM || budget > APPROXIFER_MAX_TOKENS) return APPROXIFER_ERR_LIMIT;
+    if (heads == 0 || row_bytes == 0) planes = planes < 0 ? planes : 0;       // pools of nothing
+    if ((rc = check_pools(d_pools, planes, heads * page * row_bytes, P)) != APPROXIFER_OK) return rc;
+    if (planes > 0 && row_bytes % 16 != 0) return APPROXIFER_ERR_ALIGNMENT;
+    if (B == 0) return APPROXIFER_OK;
+    if (d_table == nullptr || d_lens == nullptr || d_refs == nullptr || d_mass == nullptr || d_kept == nullptr)
+        return APPROXIFER_ERR_NULL_POINTER;
+    if (d_workspace == nullptr || workspace_bytes < approxifer::evict_workspace_bytes(B, budget, P, shift)) return APPROXIFER_ERR_WORKSPACE;
+    if (!aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
+    return approxifer::launch_cache_evict(d_table, d_lens, d_refs, d_mass, mass_stride, d_kept, d_status, d_pools, planes, heads, row_bytes,
+                                          static_cast<int>(B), static_cast<int>(M), static_cast<int>(P), shift, static_cast<int>(budget),
+                                          static_cast<int>(first), static_cast<int>(recent), d_workspace,
+                                          static_cast<hipStream_t>(stream));
+}
+
+size_t approxifer_cache_evict_workspace_bytes(int64_t B, int64_t budget, int64_t P, int page) {
+    int shift = 0;
+    if (check_cache(B, 1, P, page, &shift) != APPROXIFER_OK || B < 1 || budget < 1 || budget > APPROXIFER_MAX_TOKENS) return 0;
+    return approxifer::evict_workspace_bytes(B, budget, P, shift);
 }
 
 }  // extern "C"

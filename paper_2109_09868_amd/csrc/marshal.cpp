@@ -30,6 +30,7 @@ struct Library {
     decltype(&approxifer_cache_reserve) cache_reserve;
     decltype(&approxifer_cache_fork) cache_fork;
     decltype(&approxifer_cache_compact) cache_compact;
+    decltype(&approxifer_cache_evict) cache_evict;
 };
 
 // The handle of a loaded library: its entry points, by address, in the order above.
@@ -54,7 +55,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
         reinterpret_cast<decltype(Library::top1)>(p[6]),           reinterpret_cast<decltype(Library::wait_mask)>(p[7]),
         reinterpret_cast<decltype(Library::append)>(p[8]),         reinterpret_cast<decltype(Library::attend)>(p[9]),
         reinterpret_cast<decltype(Library::cache_reserve)>(p[10]), reinterpret_cast<decltype(Library::cache_fork)>(p[11]),
-        reinterpret_cast<decltype(Library::cache_compact)>(p[12])};
+        reinterpret_cast<decltype(Library::cache_compact)>(p[12]), reinterpret_cast<decltype(Library::cache_evict)>(p[13])};
     PyObject *c = PyCapsule_New(lib, kCapsule, [](PyObject *o) { delete static_cast<Library *>(PyCapsule_GetPointer(o, kCapsule)); });
     if (c == nullptr) delete lib;
     return c;
@@ -438,7 +439,7 @@ PyObject *cache_reserve(PyObject *const *a, Py_ssize_t n) {
 
 // Pools [.., P, Hkv, page, Dh] of any type, table, lens, refs and workspace.
 struct Pages {
-    int64_t B = 0, M = 0, P = 0, planes = 0, page_bytes = 0;
+    int64_t B = 0, M = 0, P = 0, planes = 0, page_bytes = 0, heads = 0;
     int page = 0;
     void *pools = nullptr, *table = nullptr, *lens = nullptr, *refs = nullptr, *ws = nullptr;
     size_t ws_bytes = 0;
@@ -453,6 +454,7 @@ struct Pages {
         P = ref->numel();
         if (pool->size(-4) != P) return;
         page = static_cast<int>(pool->size(-2));
+        heads = pool->size(-3);
         page_bytes = pool->size(-1) * pool->size(-2) * pool->size(-3) * static_cast<int64_t>(pool->element_size());
         planes = pool->numel() / (pool->size(-1) * pool->size(-2) * pool->size(-3) * P);
         pools = pool->data_ptr();
@@ -498,6 +500,26 @@ PyObject *cache_compact(PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (library, pools, table, lens, refs, mass, budget, first, recent, kept, status, workspace)
+PyObject *cache_evict(PyObject *const *a, Py_ssize_t n) {
+    const Library *lib = n == 12 ? library(a[0]) : nullptr;
+    if (lib == nullptr) return nullptr;
+    const Pages c(a[1], a[2], a[3], a[4], a[11]);
+    const at::Tensor *m = plain(a[5], kF32);
+    int64_t budget, first, recent;
+    if (!c.ok || m == nullptr || m->dim() != 2 || m->size(0) != c.B || !integer64(a[6], budget) || !integer64(a[7], first) ||
+        !integer64(a[8], recent))
+        Py_RETURN_NONE;
+    const int64_t stride = m->size(1);
+    void *mass = m->data_ptr(), *kept = shaped(a[9], kI32, c.B, budget), *status = shaped(a[10], kI32, c.B);
+    if (mass == nullptr || kept == nullptr || status == nullptr) Py_RETURN_NONE;
+    return status_of([&](void *s) {
+        return lib->cache_evict(ints(c.table), ints(c.lens), ints(c.refs), static_cast<float *>(mass), stride, ints(kept), ints(status),
+                                c.pools, c.planes, c.heads, c.page_bytes / (c.heads * c.page), c.B, c.M, c.P, c.page, budget, first, recent,
+                                c.ws, c.ws_bytes, s);
+    });
+}
+
 // No C++ exception leaves the module: what torch throws makes the call one for the binding's own checks.
 template <PyObject *(*F)(PyObject *const *, Py_ssize_t)>
 PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -519,6 +541,7 @@ PyMethodDef methods[] = {
     APPROXIFER_METHOD(byzantine), APPROXIFER_METHOD(pad_last_group), APPROXIFER_METHOD(top1),
     APPROXIFER_METHOD(wait_mask), APPROXIFER_METHOD(append),         APPROXIFER_METHOD(attend),
     APPROXIFER_METHOD(cache_reserve), APPROXIFER_METHOD(cache_fork), APPROXIFER_METHOD(cache_compact),
+    APPROXIFER_METHOD(cache_evict),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -115,5 +115,9 @@ int launch_cache_compact(int32_t *table, const int32_t *lens, int32_t *refs, int
                          int64_t planes, int64_t page_bytes, int B, int M, int P, int page_shift, void *workspace,
                          hipStream_t stream);
 size_t cache_workspace_bytes(int64_t B, int64_t B_out, int64_t P);
+int launch_cache_evict(int32_t *table, int32_t *lens, int32_t *refs, float *mass, int64_t mass_stride, int32_t *kept, int32_t *status,
+                       void *pools, int64_t planes, int64_t heads, int64_t row_bytes, int B, int M, int P, int page_shift, int budget,
+                       int first, int recent, void *workspace, hipStream_t stream);
+size_t evict_workspace_bytes(int64_t B, int64_t budget, int64_t P, int page_shift);
 
 }  // namespace approxifer

@@ -227,3 +227,52 @@ def compact(table, lens, refs, page):
                 if 0 <= row[j] < P and moved[row[j]] >= 0:
                     row[j] = moved[row[j]]
     return table, after, moved, live, moves
+
+
+def evict(table, lens, refs, mass, budget, first, recent, page):
+    """(table, lens, refs, mass, kept, status, moves): lists in, lists out; moves: for every sequence that is cut, [((page, slot) it comes
+    from, (page, slot) it goes to), ..] of the tokens in the pages that change."""
+    B, M, P = len(table), len(table[0]) if table else 0, len(refs)
+    table, lens, mass, held = [list(r) for r in table], list(lens), [list(r) for r in mass], list(refs)
+    refs, kept, status, moves = list(refs), [], [], []
+    free = [p for p in range(P) if held[p] == 0]
+    wanted = 0
+    for b in range(B):
+        l = lens[b]
+        row = [-1] * budget
+        kept.append(row)
+        if not 0 <= l <= M * page or l > len(mass[b]):
+            status.append(1)
+            continue
+        if l <= budget:
+            row[:l] = range(l)
+            status.append(0)
+            continue
+        if any(not 0 <= p < P or held[p] < 1 for p in table[b][:-(-l // page)]):
+            status.append(2)
+            continue
+        value = [-math.inf if math.isnan(x) else x for x in mass[b]]
+        inner = sorted(range(first, l - recent), key=lambda j: (math.isnan(mass[b][j]), -value[j], j))
+        stays = [*range(first), *sorted(inner[:budget - first - recent]), *range(l - recent, l)]
+        shifted = [i for i in range(budget) if stays[i] != i]
+        after = -(-budget // page)
+        low = min(shifted[0] // page if shifted else after, budget // page)
+        wants = [j for j in range(low, after) if held[table[b][j]] > 1]
+        wanted += len(wants)
+        if wants and wanted > len(free):
+            status.append(3)
+            continue
+        status.append(0)
+        row[:] = stays
+        old = list(table[b])
+        for n, j in enumerate(wants):
+            refs[old[j]] -= 1
+            table[b][j] = free[wanted - len(wants) + n]
+            refs[table[b][j]] = 1
+        for j in range(after, -(-l // page)):
+            refs[old[j]] -= 1
+            table[b][j] = -1
+        moves += [((old[stays[i] // page], stays[i] % page), (table[b][i // page], i % page)) for i in range(low * page, budget)]
+        mass[b][:l] = [mass[b][j] for j in stays] + [0.0] * (l - budget)
+        lens[b] = budget
+    return table, lens, refs, mass, kept, status, moves
