@@ -437,6 +437,28 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
                                          int64_t max_len, int64_t window, int64_t sinks);
 
 /*
+ * approxifer_attend(), which also adds up the weights that it gives: for every place j of sequence b
+ *     d_mass[b][j] += sum over the rows of b and the Hq query heads of softmax_j(scale q . k_j),
+ * the measure by which approxifer_cache_evict() chooses.  Places that no row sees get nothing added; a call for each layer adds the
+ * layers up.  Where a row is NaN, so is the mass of all that it sees.
+ *
+ *   d_mass      [B][mass_stride] float32; places of a sequence's length and behind it are left as they are.  A sequence longer than
+ *               mass_stride is APPROXIFER_SEQUENCE_BAD, as one beyond max_len is.
+ *   d_workspace 16-byte aligned, at least 8 T Hq bytes rounded up to 256.  approxifer_attend_mass_workspace_bytes() gives the size with
+ *               which the call is fastest; with less its work is split less.
+ * Others as approxifer_attend().  Weights and their sums are float32; a key's weights are added in an order that the sizes and the
+ * workspace fix, so the same call gives the same bits.
+ * Returns what approxifer_attend() does, or ERR_WORKSPACE; ERR_BAD_SHAPE for a negative mass_stride, ERR_ALIGNMENT for a d_mass that is not
+ * at a multiple of 4.  The call consists of up to four launches.
+ */
+int approxifer_attend_mass(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype,
+                           const void *d_q, int64_t q_stride, const void *d_k_pool, const void *d_v_pool, void *d_out,
+                           float *d_mass, int64_t mass_stride, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
+                           double scale, int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream);
+size_t approxifer_attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows,
+                                              int64_t max_len, int64_t window, int64_t sinks);
+
+/*
  * Room for d_add[b] >= 0 more tokens of every sequence: lens[b] += add[b], and the pages this takes are the free ones of
  * lowest index, given out in the order of the sequences; their refs become 1.  All in place.
  *   APPROXIFER_SEQUENCE_SHARED_PAGE   the sequence's last page is not full and has another holder: fork the sequence first

@@ -51,6 +51,8 @@ EXPORTS = (
     "approxifer_cache_fork",
     "approxifer_cache_compact",
     "approxifer_cache_workspace_bytes",
+    "approxifer_attend_mass",
+    "approxifer_attend_mass_workspace_bytes",
     "approxifer_cache_evict",
     "approxifer_cache_evict_workspace_bytes",
 )
@@ -141,6 +143,10 @@ def load() -> ctypes.CDLL:
     lib.approxifer_cache_compact.argtypes = [vp] * 6 + [q] * 5 + [i, vp, z, vp]
     lib.approxifer_cache_workspace_bytes.restype = z
     lib.approxifer_cache_workspace_bytes.argtypes = [q, q, q]
+    lib.approxifer_attend_mass.restype = i
+    lib.approxifer_attend_mass.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, vp, q, q, q, q, q, f, vp, vp, z, vp]
+    lib.approxifer_attend_mass_workspace_bytes.restype = z
+    lib.approxifer_attend_mass_workspace_bytes.argtypes = lib.approxifer_attend_workspace_bytes.argtypes
     lib.approxifer_cache_evict.restype = i
     lib.approxifer_cache_evict.argtypes = [vp, vp, vp, vp, q, vp, vp, vp] + [q] * 6 + [i, q, q, q, vp, z, vp]
     lib.approxifer_cache_evict_workspace_bytes.restype = z
@@ -208,7 +214,8 @@ def _marshal():
         module, handle = _marshal_module(), None
         if module is not None:
             names = ("encode", "decode", "decode_top1", "decode_byzantine", "decode_byzantine_homogeneous", "pad_last_group",
-                     "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact", "cache_evict")
+                     "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact", "cache_evict",
+                     "attend_mass")
             handle = module.bind(*(ctypes.cast(getattr(lib, "approxifer_" + n), ctypes.c_void_p).value for n in names))
         _ordinary = (lib, module, handle)
     return _ordinary[1], _ordinary[2]
@@ -653,6 +660,48 @@ def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len,
         ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kp, vp, _dev(out, dtype, (T, Hq, Dh)), int(max_rows), int(max_len),
         int(window), int(sinks), Dh ** -0.5 if scale is None else float(scale), _dev(status, torch.int32, (table.shape[0],)), ws_ptr,
         ws_bytes, _stream_handle(stream)))
+    return out, status
+
+
+def approxifer_attend_mass_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window=0, sinks=0) -> int:
+    """Bytes of scratch memory with which approxifer_attend_mass is fastest; dtype a torch dtype."""
+    return int(load().approxifer_attend_mass_workspace_bytes(int(T), int(B), int(Hq), int(Hkv), int(Dh), _dtype_code(dtype), int(max_rows),
+                                                             int(max_len), int(window), int(sinks)))
+
+
+def approxifer_attend_mass(q, k_pool, v_pool, table, lens, starts, mass, max_rows, max_len, window=0, sinks=0, scale=None, out=None,
+                           status=None, workspace=None, stream=None):
+    """approxifer_attend, which adds the weights that it gives every place of a sequence to mass [B, L] float32, L at least the sequences'
+    length.  workspace: of approxifer_attend_mass_workspace_bytes(), or None.  Returns (out [T, Hq, Dh], status [B] int32)."""
+    if out is not None and status is not None and workspace is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.attend_mass(lib, q, k_pool, v_pool, table, lens, starts, mass, max_rows, max_len, window,
+                                                           sinks, scale, out, status, None if workspace is NO_WORKSPACE else workspace)):
+            return out, status
+    import torch
+    dtype = k_pool.dtype
+    code = _dtype_code(dtype)
+    T, Hq, Dh = q.shape
+    Hkv = k_pool.shape[1]
+    B = table.shape[0]
+    kp, vp = _pools(k_pool, v_pool, dtype, None, Dh)
+    qp, q_stride = _rows(q, dtype)
+    if not isinstance(mass, torch.Tensor) or mass.dim() != 2:
+        raise TypeError("mass is a tensor [B, L]")
+    with _on(stream):
+        if out is None:
+            out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+        if status is None:
+            status = torch.full((B,), -1, dtype=torch.int32, device=q.device)
+        if workspace is None:
+            need = approxifer_attend_mass_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else NO_WORKSPACE
+    ws_ptr, ws_bytes = _scratch(workspace)
+    seq = _sequences(table, lens, starts, T, k_pool)
+    _check(_entry().approxifer_attend_mass(
+        ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kp, vp, _dev(out, dtype, (T, Hq, Dh)),
+        _dev(mass, torch.float32, (B, mass.shape[1])), mass.shape[1], int(max_rows), int(max_len), int(window), int(sinks),
+        Dh ** -0.5 if scale is None else float(scale), _dev(status, torch.int32, (B,)), ws_ptr, ws_bytes, _stream_handle(stream)))
     return out, status
 
 

@@ -70,6 +70,54 @@ int check_rows(const void *p, int64_t stride, int64_t values, int dtype) {
     return aligned(p, dtype == APPROXIFER_F32 ? 4 : 2) ? APPROXIFER_OK : APPROXIFER_ERR_ALIGNMENT;
 }
 
+// A call of approxifer_attend() or of one that does the same and more: its checks, in the order in which they decide, and its
+// description.  empty: nothing is left to do.
+int check_attend(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride, const void *d_k_pool,
+                 const void *d_v_pool, void *d_out, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks, double scale,
+                 int32_t *d_status, void *d_workspace, approxifer::AttendCall *call, bool *empty) {
+    approxifer::AttendCall &c = *call;
+    int rc = check_sequences(h_seq, Hq, Hkv, Dh, dtype, &c.seq);
+    if (rc != APPROXIFER_OK) return rc;
+    if (max_rows < 0 || max_len < 0 || window < 0 || sinks < 0 || !(std::fabs(scale) <= 0x1p126)) return APPROXIFER_ERR_BAD_SHAPE;
+    if (c.seq.B == 0 && c.seq.T > 0) return APPROXIFER_ERR_BAD_CACHE;
+    *empty = c.seq.B == 0 || (c.seq.T == 0 && d_status == nullptr);
+    if (c.seq.B == 0) return APPROXIFER_OK;
+    if (c.seq.table == nullptr || c.seq.lens == nullptr || c.seq.starts == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+    if (*empty) return APPROXIFER_OK;
+    if (c.seq.T > 0) {
+        if (d_q == nullptr || d_k_pool == nullptr || d_v_pool == nullptr || d_out == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+        if ((rc = check_rows(d_q, q_stride, static_cast<int64_t>(Hq) * Dh, dtype)) != APPROXIFER_OK) return rc;
+        if (!aligned(d_out, 16) || !aligned(d_k_pool, 16) || !aligned(d_v_pool, 16)) return APPROXIFER_ERR_ALIGNMENT;
+        if (d_workspace != nullptr && !aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
+    }
+    const int64_t most = h_seq->M * h_seq->page;              // no sequence is longer, no window reaches further
+    c.Hq = Hq;
+    c.Hkv = Hkv;
+    c.Dh = Dh;
+    c.dtype = dtype;
+    c.q = d_q;
+    c.q_stride = q_stride;
+    c.k_pool = d_k_pool;
+    c.v_pool = d_v_pool;
+    c.out = d_out;
+    c.status = d_status;
+    c.max_rows = static_cast<int>(max_rows < c.seq.T ? max_rows : c.seq.T);
+    c.max_len = static_cast<int>(max_len < most ? max_len : most);
+    c.window = static_cast<int>(window < most ? window : 0);
+    c.sinks = c.window == 0 ? 0 : static_cast<int>(sinks < most ? sinks : most);
+    c.scale = static_cast<float>(scale);
+    return APPROXIFER_OK;
+}
+
+// Sizes of attention that a call would take: what the size of its workspace is asked for.
+bool attend_sizes_taken(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window,
+                        int64_t sinks) {
+    return T >= 1 && T <= APPROXIFER_MAX_ROWS && B >= 1 && B <= APPROXIFER_MAX_SEQUENCES && Hkv >= 1 && Hq >= 1 && Hq % Hkv == 0 &&
+           Hq <= APPROXIFER_MAX_HEADS && Dh >= 1 && Dh % 8 == 0 && Dh <= APPROXIFER_MAX_HEAD_DIM && dtype >= APPROXIFER_F32 &&
+           dtype <= APPROXIFER_BF16 && max_rows >= 1 && max_len >= 1 && window >= 0 && sinks >= 0 && T * Hq <= (1LL << 30) &&
+           B * Hkv <= (1LL << 22);
+}
+
 int check_pools(const void *d_pools, int64_t planes, int64_t page_bytes, int64_t P) {
     if (planes < 0 || page_bytes < 0) return APPROXIFER_ERR_BAD_SHAPE;
     if (planes == 0 || page_bytes == 0) return APPROXIFER_OK;
@@ -321,48 +369,46 @@ int approxifer_attend(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh
                       const void *d_k_pool, const void *d_v_pool, void *d_out, int64_t max_rows, int64_t max_len, int64_t window,
                       int64_t sinks, double scale, int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream) {
     approxifer::AttendCall c;
-    int rc = check_sequences(h_seq, Hq, Hkv, Dh, dtype, &c.seq);
-    if (rc != APPROXIFER_OK) return rc;
-    if (max_rows < 0 || max_len < 0 || window < 0 || sinks < 0 || !(std::fabs(scale) <= 0x1p126)) return APPROXIFER_ERR_BAD_SHAPE;
-    if (c.seq.B == 0 && c.seq.T > 0) return APPROXIFER_ERR_BAD_CACHE;
-    if (c.seq.B == 0) return APPROXIFER_OK;
-    if (c.seq.table == nullptr || c.seq.lens == nullptr || c.seq.starts == nullptr) return APPROXIFER_ERR_NULL_POINTER;
-    if (c.seq.T == 0 && d_status == nullptr) return APPROXIFER_OK;
-    if (c.seq.T > 0) {
-        if (d_q == nullptr || d_k_pool == nullptr || d_v_pool == nullptr || d_out == nullptr) return APPROXIFER_ERR_NULL_POINTER;
-        if ((rc = check_rows(d_q, q_stride, static_cast<int64_t>(Hq) * Dh, dtype)) != APPROXIFER_OK) return rc;
-        if (!aligned(d_out, 16) || !aligned(d_k_pool, 16) || !aligned(d_v_pool, 16)) return APPROXIFER_ERR_ALIGNMENT;
-        if (d_workspace != nullptr && !aligned(d_workspace, 16)) return APPROXIFER_ERR_ALIGNMENT;
-    }
-    const int64_t most = h_seq->M * h_seq->page;              // no sequence is longer, no window reaches further
-    c.Hq = Hq;
-    c.Hkv = Hkv;
-    c.Dh = Dh;
-    c.dtype = dtype;
-    c.q = d_q;
-    c.q_stride = q_stride;
-    c.k_pool = d_k_pool;
-    c.v_pool = d_v_pool;
-    c.out = d_out;
-    c.status = d_status;
-    c.max_rows = static_cast<int>(max_rows < c.seq.T ? max_rows : c.seq.T);
-    c.max_len = static_cast<int>(max_len < most ? max_len : most);
-    c.window = static_cast<int>(window < most ? window : 0);
-    c.sinks = c.window == 0 ? 0 : static_cast<int>(sinks < most ? sinks : most);
-    c.scale = static_cast<float>(scale);
+    bool empty = false;
+    const int rc = check_attend(h_seq, Hq, Hkv, Dh, dtype, d_q, q_stride, d_k_pool, d_v_pool, d_out, max_rows, max_len, window, sinks,
+                                scale, d_status, d_workspace, &c, &empty);
+    if (rc != APPROXIFER_OK || empty) return rc;
     return approxifer::launch_attend(c, d_workspace, d_workspace != nullptr ? workspace_bytes : 0, static_cast<hipStream_t>(stream));
 }
 
 size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                                          int64_t window, int64_t sinks) {
-    if (T < 1 || T > APPROXIFER_MAX_ROWS || B < 1 || B > APPROXIFER_MAX_SEQUENCES || Hkv < 1 || Hq < 1 || Hq % Hkv != 0 ||
-        Hq > APPROXIFER_MAX_HEADS || Dh < 1 || Dh % 8 != 0 || Dh > APPROXIFER_MAX_HEAD_DIM || dtype < APPROXIFER_F32 ||
-        dtype > APPROXIFER_BF16 || max_rows < 1 || max_len < 1 || window < 0 || sinks < 0 || T * Hq > (1LL << 30) ||
-        B * Hkv > (1LL << 22))
-        return 0;
+    if (!attend_sizes_taken(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)) return 0;
     const int64_t most = APPROXIFER_MAX_TOKENS;               // no sequence is longer
     return approxifer::attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len < most ? max_len : most, window < most ? window : 0,
                                               sinks < most ? sinks : most);
+}
+
+int approxifer_attend_mass(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,
+                           const void *d_k_pool, const void *d_v_pool, void *d_out, float *d_mass, int64_t mass_stride, int64_t max_rows,
+                           int64_t max_len, int64_t window, int64_t sinks, double scale, int32_t *d_status, void *d_workspace,
+                           size_t workspace_bytes, void *stream) {
+    approxifer::AttendCall c;
+    bool empty = false;
+    if (mass_stride < 0) return APPROXIFER_ERR_BAD_SHAPE;
+    const int rc = check_attend(h_seq, Hq, Hkv, Dh, dtype, d_q, q_stride, d_k_pool, d_v_pool, d_out, max_rows,
+                                max_len < mass_stride ? max_len : mass_stride, window, sinks, scale, d_status, d_workspace, &c, &empty);
+    if (rc != APPROXIFER_OK || empty) return rc;
+    if (c.seq.T > 0) {
+        if (d_mass == nullptr) return APPROXIFER_ERR_NULL_POINTER;
+        if (!aligned(d_mass, 4)) return APPROXIFER_ERR_ALIGNMENT;
+        if (d_workspace == nullptr || workspace_bytes < approxifer::attend_mass_least_bytes(c.seq.T, Hq)) return APPROXIFER_ERR_WORKSPACE;
+    }
+    return approxifer::launch_attend_mass(c, d_mass, mass_stride, d_workspace, d_workspace != nullptr ? workspace_bytes : 0,
+                                          static_cast<hipStream_t>(stream));
+}
+
+size_t approxifer_attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                                              int64_t window, int64_t sinks) {
+    if (!attend_sizes_taken(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks)) return 0;
+    const int64_t most = APPROXIFER_MAX_TOKENS;
+    return approxifer::attend_mass_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len < most ? max_len : most,
+                                                   window < most ? window : 0, sinks < most ? sinks : most);
 }
 
 int approxifer_cache_reserve(int32_t *d_table, int32_t *d_lens, int32_t *d_refs, const int32_t *d_add, int32_t *d_status, int64_t B,

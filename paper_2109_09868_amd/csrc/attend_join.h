@@ -58,6 +58,7 @@ __device__ __forceinline__ void join_row(const AttendCall &c, const Rows &rows, 
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k)
             if (lane + k * kWave < c.Dh) y[lane + k * kWave] = E::store(out[k] * inverse);
+        if (c.stats != nullptr && lane == 0) RowStats(top, total).store(c, t, h * group + static_cast<int>(row % group));
         return;
     }
 #pragma unroll
@@ -77,6 +78,7 @@ __device__ __forceinline__ void join_row(const AttendCall &c, const Rows &rows, 
         sum += tops[w] == -INFINITY ? totals[w] : f[w] * totals[w];
     }
     const float inverse = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (c.stats != nullptr && threadIdx.x == 0) RowStats(all, sum).store(c, t, h * group + static_cast<int>(row % group));
     for (int d = threadIdx.x; d < c.Dh; d += 256) {
         float x = 0.0f;
 #pragma unroll

@@ -386,6 +386,8 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
 
     float *const partial = workspace + (index * static_cast<int64_t>(g.parts) + part) * part_floats(S::kRows, c.Dh);
     total = half_sum(total);
+    if (c.stats != nullptr && alone && half == 0 && first + wave * 32 + row32 < row_count)
+        RowStats(top == -INFINITY ? top : top * scale - kLift<E>, total).store(c, rows.start + token, head);
     // A weight of 0 (hidden, or rounded to it) times an infinity is NaN, and so is all that a hidden NaN touches: the product cannot hide it.
     // Rows with such sums are computed again, element by element; those whose weights are no numbers are NaN as they have to be.  (A prompt of 2048
     // tokens, 8 heads of 128 on 2, bf16: 0.08 to 0.1 ms, with an infinity that all rows see too; with a NaN in their place, where all rows are

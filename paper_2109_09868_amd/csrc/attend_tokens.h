@@ -278,6 +278,17 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     const bool alone = keys.steps <= chunk;
     const int64_t slot = (static_cast<int64_t>(pair) * g.blocks + block) * g.parts + part;
     float *const partial = workspace + slot * part_floats(S::kRows, c.Dh);
+    if (c.stats != nullptr && alone && threadIdx.x < S::kRows && first + threadIdx.x < row_count) {
+        const int r = threadIdx.x;
+        float m = tops[0][r], l = 0.0f;
+#pragma unroll
+        for (int w = 1; w < S::kWaves; ++w) m = fmaxf(m, tops[w][r]);
+#pragma unroll
+        for (int w = 0; w < S::kWaves; ++w)
+            l += tops[w][r] == -INFINITY ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f((tops[w][r] - m) * scale);
+        const int64_t at = first + r;
+        RowStats(m == -INFINITY ? m : m * scale - kLift<E>, l).store(c, rows.start + at / group, h * group + static_cast<int>(at % group));
+    }
     if (dirty != 0) {                                         // rows that must not see what the product cannot hide
         __syncthreads();
         float *const scratch = reinterpret_cast<float *>(vt);

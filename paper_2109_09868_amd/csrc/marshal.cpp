@@ -31,6 +31,7 @@ struct Library {
     decltype(&approxifer_cache_fork) cache_fork;
     decltype(&approxifer_cache_compact) cache_compact;
     decltype(&approxifer_cache_evict) cache_evict;
+    decltype(&approxifer_attend_mass) attend_mass;
 };
 
 // The handle of a loaded library: its entry points, by address, in the order above.
@@ -55,7 +56,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
         reinterpret_cast<decltype(Library::top1)>(p[6]),           reinterpret_cast<decltype(Library::wait_mask)>(p[7]),
         reinterpret_cast<decltype(Library::append)>(p[8]),         reinterpret_cast<decltype(Library::attend)>(p[9]),
         reinterpret_cast<decltype(Library::cache_reserve)>(p[10]), reinterpret_cast<decltype(Library::cache_fork)>(p[11]),
-        reinterpret_cast<decltype(Library::cache_compact)>(p[12]), reinterpret_cast<decltype(Library::cache_evict)>(p[13])};
+        reinterpret_cast<decltype(Library::cache_compact)>(p[12]), reinterpret_cast<decltype(Library::cache_evict)>(p[13]),
+        reinterpret_cast<decltype(Library::attend_mass)>(p[14])};
     PyObject *c = PyCapsule_New(lib, kCapsule, [](PyObject *o) { delete static_cast<Library *>(PyCapsule_GetPointer(o, kCapsule)); });
     if (c == nullptr) delete lib;
     return c;
@@ -421,6 +423,34 @@ PyObject *attend(PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (library, q, k_pool, v_pool, table, lens, starts, mass, max_rows, max_len, window, sinks, scale or None, out, status, workspace or None)
+PyObject *attend_mass(PyObject *const *a, Py_ssize_t n) {
+    const Library *lib = n == 16 ? library(a[0]) : nullptr;
+    if (lib == nullptr) return nullptr;
+    Cache c(a[2], a[3], a[4], a[5], a[6]);
+    if (!c.ok) Py_RETURN_NONE;
+    const TokenRows q(a[1], c.type);
+    const at::Tensor *m = plain(a[7], kF32), *w = a[15] == Py_None ? nullptr : plain(a[15], kU8);
+    int64_t rows, length, window, sinks;
+    if (q.data == nullptr || q.Dh != c.Dh || q.heads > APPROXIFER_MAX_HEADS || !integer64(a[8], rows) || !integer64(a[9], length) ||
+        !integer64(a[10], window) || !integer64(a[11], sinks) || m == nullptr || m->dim() != 2 || m->size(0) != c.seq.B ||
+        (a[15] != Py_None && w == nullptr))
+        Py_RETURN_NONE;
+    double scale = 1.0 / std::sqrt(static_cast<double>(c.Dh));
+    if (a[12] != Py_None && !real(a[12], scale)) Py_RETURN_NONE;
+    void *out = shaped(a[13], c.type, q.T, q.heads, q.Dh), *status = shaped(a[14], kI32, c.seq.B), *mass = m->data_ptr();
+    if (out == nullptr || status == nullptr || mass == nullptr) Py_RETURN_NONE;
+    const int64_t stride = m->size(1);
+    void *ws = w != nullptr ? w->data_ptr() : nullptr;
+    const size_t ws_bytes = w != nullptr ? static_cast<size_t>(w->numel()) : 0;
+    c.seq.T = q.T;
+    return status_of([&](void *s) {
+        return lib->attend_mass(&c.seq, static_cast<int>(q.heads), c.Hkv, c.Dh, c.dtype, q.data, q.stride, c.k, c.v, out,
+                                static_cast<float *>(mass), stride, rows, length, window, sinks, scale, static_cast<int32_t *>(status), ws,
+                                ws_bytes, s);
+    });
+}
+
 int32_t *ints(void *p) { return static_cast<int32_t *>(p); }
 
 // (library, table, lens, refs, add, page, status)
@@ -541,7 +571,7 @@ PyMethodDef methods[] = {
     APPROXIFER_METHOD(byzantine), APPROXIFER_METHOD(pad_last_group), APPROXIFER_METHOD(top1),
     APPROXIFER_METHOD(wait_mask), APPROXIFER_METHOD(append),         APPROXIFER_METHOD(attend),
     APPROXIFER_METHOD(cache_reserve), APPROXIFER_METHOD(cache_fork), APPROXIFER_METHOD(cache_compact),
-    APPROXIFER_METHOD(cache_evict),
+    APPROXIFER_METHOD(cache_evict),   APPROXIFER_METHOD(attend_mass),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -100,8 +100,24 @@ struct AttendCall {
     int32_t *status;
     int max_rows, max_len, window, sinks;                     // window: 0 no limit
     float scale;
+    float *stats = nullptr;                                   // [T][Hq][2], or null: of every row what RowStats says
+};
+// Of a row that attention has settled: what its weights are relative to (of c S, base 2), and the inverse of their sum.
+struct RowStats {
+    float base, inverse;
+    __device__ __forceinline__ RowStats(float top, float total)
+        : base(top == -INFINITY ? 0.0f : top), inverse(total == 0.0f ? 0.0f : 1.0f / total) {}
+    __device__ __forceinline__ void store(const AttendCall &c, int64_t t, int head) const {
+        float *const at = c.stats + 2 * (t * c.Hq + head);
+        at[0] = base;
+        at[1] = inverse;
+    }
 };
 int launch_attend(const AttendCall &c, void *workspace, size_t workspace_bytes, hipStream_t stream);
+int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *workspace, size_t workspace_bytes, hipStream_t stream);
+size_t attend_mass_least_bytes(int64_t T, int Hq);
+size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                                   int64_t window, int64_t sinks);
 size_t attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                               int64_t window, int64_t sinks);
 

@@ -90,6 +90,35 @@ def attend(c, q, window=0, sinks=0, scale=None):
     return out, bound
 
 
+def mass(c, q, window=0, sinks=0, scale=None):
+    """(sums float64 [B, longest], bound): the weights that every place is given, and how far float32 may be off.  With u = 2^-24: scores
+    are formed twice, by (Dh + 8) u scale sum |q k| off each time, once in a weight and once in its row's total, which is n weights
+    added, (n + 64) u; the exponent's argument is rounded where it is up to 1.5 scores' range wide, 4 u of that in all; the N weights of
+    a place are added one after the other at worst, (N + 16) u.  A weight below 2^-126 may be 0."""
+    T, Hq, Dh = q.shape
+    scale = Dh ** -0.5 if scale is None else scale
+    longest = max(int(c["lens"].max()), 1)
+    sums, bound = torch.zeros((len(c["lens"]), longest), dtype=torch.float64), torch.zeros((len(c["lens"]), longest), dtype=torch.float64)
+    for b in range(len(c["lens"])):
+        k = held(c, "k_pool", b)
+        length, t0, t1 = int(c["lens"][b]), int(c["starts"][b]), int(c["starts"][b + 1])
+        for t in range(t0, t1):
+            place = length - (t1 - t)
+            if place < 0:
+                continue
+            seen = visible(place, length, window, sinks)
+            n = int(seen.sum())
+            for h in range(Hq):
+                kk, x = k[h * k.shape[0] // Hq][seen], q[t, h].double()
+                s = kk @ x * scale
+                w = torch.softmax(s, 0)
+                off = 4.0 * (Dh + 8) * U32 * abs(scale) * float((kk.abs() @ x.abs()).max())
+                off += 2.0 * (n + 64) * U32 + 4.0 * U32 * 1.5 * float(s.max() - s.min()) + ((t1 - t0) * Hq + 16) * U32
+                sums[b, :length][seen] += w
+                bound[b, :length][seen] += off * w + 2.0 ** -126
+    return sums, bound
+
+
 def append(c, q, k, v, freq, q_weight=None, k_weight=None, eps=1e-6, positions=None, axis=None, interleaved=False):
     """(q_out, its bound, k_pool, its bound, v_pool): float64; pools where nothing is written keep their values, bound 0.  A
     norm's sum, root and two products are off by (Dh + 16) u at most, cosine and sine of an angle reduced in float64 by 8 u, the

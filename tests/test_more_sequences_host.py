@@ -44,3 +44,50 @@ def test_evict_refusals(lib):
     assert _evict(lib, B=0, table=None, lens=None, mass=None, kept=None, ws=None) == 0
     for none in ((0, 20, 5, 16), (2, 0, 5, 16), (2, 20, 0, 16), (2, 20, 5, 12), (2, 1 << 31, 5, 16)):
         assert binding.approxifer_cache_evict_workspace_bytes(*none) == 0
+
+
+def _seq(T=4, B=2, M=3, P=5, page=16, table=4096, lens=4096, starts=4096):
+    return binding._Sequences(table, lens, starts, T, B, M, P, page)
+
+
+def _mass(lib, seq=None, Hq=4, Hkv=2, Dh=64, dtype=0, q=FAKE, qs=256, kp=FAKE, vp=FAKE, out=FAKE, mass=FAKE, stride=48, rows=1, length=48,
+          window=0, sinks=0, scale=1.0, status=FAKE, ws=FAKE, ws_bytes=256):
+    s = ctypes.byref(seq if seq is not None else _seq()) if seq is not False else None
+    return lib.approxifer_attend_mass(s, Hq, Hkv, Dh, dtype, q, qs, kp, vp, out, mass, stride, rows, length, window, sinks, scale, status, ws,
+                                      ws_bytes, None)
+
+
+def _sizes_are_refused(lib, call):
+    for bad in (dict(T=-1), dict(B=-1), dict(M=0), dict(P=0), dict(page=0), dict(page=24), dict(page=-16)):
+        assert call(lib, _seq(**bad)) == -11, bad
+    for bad in (dict(T=(1 << 24) + 1), dict(B=(1 << 20) + 1), dict(P=1 << 31), dict(M=1 << 28), dict(page=8192)):
+        assert call(lib, _seq(**bad)) == -3, bad
+    for bad in (dict(Hq=0), dict(Hkv=0), dict(Hq=3), dict(Dh=0), dict(Dh=-8), dict(Dh=60)):
+        assert call(lib, **bad) == -11, bad
+    assert call(lib, Hq=2048, qs=2048 * 64) == -3 and call(lib, Dh=264, qs=4 * 264) == -3
+    for dtype in (-1, 3, 7):
+        assert call(lib, dtype=dtype) == -9
+    assert call(lib, False) == -1
+    for missing in ("table", "lens", "starts"):
+        assert call(lib, _seq(**{missing: None})) == -1
+    assert call(lib, _seq(B=0)) == -11
+    assert call(lib, _seq(B=0, T=0, table=None, lens=None, starts=None)) == 0
+    assert call(lib, _seq(T=0), status=None) == 0
+    for missing in ("q", "kp", "vp", "out"):
+        assert call(lib, **{missing: None}) == -1
+    for bad in (dict(rows=-1), dict(length=-1), dict(window=-1), dict(sinks=-1), dict(scale=float("nan")), dict(scale=float("inf")),
+                dict(qs=255)):
+        assert call(lib, **bad) == -2, bad
+    for odd in ("q", "kp", "vp", "out", "ws"):
+        assert call(lib, **{odd: ODD}) == -10
+
+
+def test_attend_mass_refusals(lib):
+    _sizes_are_refused(lib, _mass)
+    assert _mass(lib, mass=None) == -1 and _mass(lib, mass=ODD) == -10 and _mass(lib, stride=-1) == -2
+    assert _mass(lib, ws=None) == -12 and _mass(lib, ws_bytes=255) == -12
+    import torch
+    need = binding.approxifer_attend_mass_workspace_bytes
+    for args in ((0, 2, 4, 2, 64), (4, 0, 4, 2, 64), (4, 2, 3, 2, 64), (4, 2, 4, 2, 60), (4, 2, 4, 2, 264)):
+        assert need(*args, torch.float16, 1, 100) == 0
+    assert need(4, 2, 4, 2, 64, torch.float16, 1, 100) >= 256
