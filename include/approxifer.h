@@ -437,6 +437,31 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
                                          int64_t max_len, int64_t window, int64_t sinks);
 
 /*
+ * approxifer_attend() for sequences that begin alike, as forks of one prompt do: what a group of them has in common is read once for all of
+ * its rows, not once for every sequence.
+ *
+ *   d_groups    [C + 1] int32, must not fall: sequences d_groups[c] .. d_groups[c + 1] - 1 are group c.  Others are in none.
+ *   d_shared    [C] int32: the first d_shared[c] places of all sequences of group c, as far as they have them, hold the same keys and
+ *               values, in the same pages or in copies (approxifer_cache_fork() shares the full ones and copies the last).  From whose
+ *               pages they are read is the call's choice.
+ *   max_shared  bound of d_shared.  Sequences of a group that reaches outside 0 .. B, or whose d_shared is not in 0 .. max_shared, are
+ *               attended to as if they shared nothing.
+ *   d_workspace as for approxifer_attend(), of approxifer_attend_shared_workspace_bytes(); without one, or with too small a one, and
+ *               where sharing would cost more than it gives, the call is approxifer_attend()
+ * Where d_groups falls, any row may be unwritten or wrong.  A page that is not in 0 .. P - 1 of the sequence that a group's places are read from
+ * makes the rows of the others that see it NaN too, and their statuses APPROXIFER_SEQUENCE_BAD_PAGE.
+ * Others, and what is returned, as approxifer_attend(), with ERR_BAD_SHAPE also for a negative C or max_shared and ERR_LIMIT for a C beyond
+ * 2^20; the call consists of up to three launches.
+ */
+int approxifer_attend_shared(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype,
+                             const void *d_q, int64_t q_stride, const void *d_k_pool, const void *d_v_pool, void *d_out,
+                             const int32_t *d_groups, const int32_t *d_shared, int64_t C, int64_t max_rows, int64_t max_len,
+                             int64_t max_shared, int64_t window, int64_t sinks, double scale, int32_t *d_status, void *d_workspace,
+                             size_t workspace_bytes, void *stream);
+size_t approxifer_attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows,
+                                                int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks);
+
+/*
  * approxifer_attend(), which also adds up the weights that it gives: for every place j of sequence b
  *     d_mass[b][j] += sum over the rows of b and the Hq query heads of softmax_j(scale q . k_j),
  * the measure by which approxifer_cache_evict() chooses.  Places that no row sees get nothing added; a call for each layer adds the

@@ -51,6 +51,8 @@ EXPORTS = (
     "approxifer_cache_fork",
     "approxifer_cache_compact",
     "approxifer_cache_workspace_bytes",
+    "approxifer_attend_shared",
+    "approxifer_attend_shared_workspace_bytes",
     "approxifer_attend_mass",
     "approxifer_attend_mass_workspace_bytes",
     "approxifer_cache_evict",
@@ -143,6 +145,10 @@ def load() -> ctypes.CDLL:
     lib.approxifer_cache_compact.argtypes = [vp] * 6 + [q] * 5 + [i, vp, z, vp]
     lib.approxifer_cache_workspace_bytes.restype = z
     lib.approxifer_cache_workspace_bytes.argtypes = [q, q, q]
+    lib.approxifer_attend_shared.restype = i
+    lib.approxifer_attend_shared.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, vp, vp, q, q, q, q, q, q, f, vp, vp, z, vp]
+    lib.approxifer_attend_shared_workspace_bytes.restype = z
+    lib.approxifer_attend_shared_workspace_bytes.argtypes = [q, q, q, i, i, i, i, q, q, q, q, q]
     lib.approxifer_attend_mass.restype = i
     lib.approxifer_attend_mass.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, vp, q, q, q, q, q, f, vp, vp, z, vp]
     lib.approxifer_attend_mass_workspace_bytes.restype = z
@@ -215,7 +221,7 @@ def _marshal():
         if module is not None:
             names = ("encode", "decode", "decode_top1", "decode_byzantine", "decode_byzantine_homogeneous", "pad_last_group",
                      "top1", "wait_mask", "append", "attend", "cache_reserve", "cache_fork", "cache_compact", "cache_evict",
-                     "attend_mass")
+                     "attend_mass", "attend_shared")
             handle = module.bind(*(ctypes.cast(getattr(lib, "approxifer_" + n), ctypes.c_void_p).value for n in names))
         _ordinary = (lib, module, handle)
     return _ordinary[1], _ordinary[2]
@@ -659,6 +665,50 @@ def approxifer_attend(q, k_pool, v_pool, table, lens, starts, max_rows, max_len,
     _check(_entry().approxifer_attend(
         ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kp, vp, _dev(out, dtype, (T, Hq, Dh)), int(max_rows), int(max_len),
         int(window), int(sinks), Dh ** -0.5 if scale is None else float(scale), _dev(status, torch.int32, (table.shape[0],)), ws_ptr,
+        ws_bytes, _stream_handle(stream)))
+    return out, status
+
+
+def approxifer_attend_shared_workspace_bytes(T, B, C, Hq, Hkv, Dh, dtype, max_rows, max_len, max_shared, window=0, sinks=0) -> int:
+    """Bytes of scratch memory with which approxifer_attend_shared is fastest (0: none); dtype a torch dtype."""
+    return int(load().approxifer_attend_shared_workspace_bytes(int(T), int(B), int(C), int(Hq), int(Hkv), int(Dh), _dtype_code(dtype),
+                                                               int(max_rows), int(max_len), int(max_shared), int(window), int(sinks)))
+
+
+def approxifer_attend_shared(q, k_pool, v_pool, table, lens, starts, groups, shared, max_rows, max_len, max_shared, window=0, sinks=0,
+                             scale=None, out=None, status=None, workspace=None, stream=None):
+    """approxifer_attend for sequences that begin alike: sequences groups[c] .. groups[c + 1] - 1 have their first shared[c] places in common
+    (groups [C + 1], shared [C] int32; max_shared bounds the latter), and what they have in common is read once for all of them.
+    Returns (out [T, Hq, Dh], status [B] int32)."""
+    if out is not None and status is not None and workspace is not None and stream is None:
+        native, lib = _marshal()
+        if native is not None and _done(native.attend_shared(lib, q, k_pool, v_pool, table, lens, starts, groups, shared, max_rows, max_len,
+                                                             max_shared, window, sinks, scale, out, status,
+                                                             None if workspace is NO_WORKSPACE else workspace)):
+            return out, status
+    import torch
+    dtype = k_pool.dtype
+    code = _dtype_code(dtype)
+    T, Hq, Dh = q.shape
+    Hkv = k_pool.shape[1]
+    B = table.shape[0]
+    kp, vp = _pools(k_pool, v_pool, dtype, None, Dh)
+    qp, q_stride = _rows(q, dtype)
+    C = shared.numel()
+    gp, sp = _dev(groups, torch.int32, (C + 1,)), _dev(shared, torch.int32, (C,))
+    with _on(stream):
+        if out is None:
+            out = torch.empty((T, Hq, Dh), dtype=dtype, device=q.device)
+        if status is None:
+            status = torch.full((B,), -1, dtype=torch.int32, device=q.device)
+        if workspace is None:
+            need = approxifer_attend_shared_workspace_bytes(T, B, C, Hq, Hkv, Dh, dtype, max_rows, max_len, max_shared, window, sinks)
+            workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else NO_WORKSPACE
+    ws_ptr, ws_bytes = _scratch(workspace)
+    seq = _sequences(table, lens, starts, T, k_pool)
+    _check(_entry().approxifer_attend_shared(
+        ctypes.byref(seq), Hq, Hkv, Dh, code, qp, q_stride, kp, vp, _dev(out, dtype, (T, Hq, Dh)), gp, sp, C, int(max_rows), int(max_len),
+        int(max_shared), int(window), int(sinks), Dh ** -0.5 if scale is None else float(scale), _dev(status, torch.int32, (B,)), ws_ptr,
         ws_bytes, _stream_handle(stream)))
     return out, status
 

@@ -14,7 +14,8 @@ SOURCES = ["api.hip", "encode.hip", "decode.hip", "byzantine.hip", "byzantine_pa
            "byzantine_pairs_small.hip", "byzantine_null_pairs_small.hip", "append.hip", "attend.hip",
            "attend_tiles_f32.hip", "attend_tiles_f16.hip", "attend_tiles_bf16.hip",
            "attend_tokens_f32.hip", "attend_tokens_f16.hip", "attend_tokens_bf16.hip", "pages.hip", "evict.hip",
-           "attend_mass.hip", "attend_mass_f32.hip", "attend_mass_f16.hip", "attend_mass_bf16.hip"]
+           "attend_mass.hip", "attend_mass_f32.hip", "attend_mass_f16.hip", "attend_mass_bf16.hip",
+           "attend_shared.hip", "attend_shared_f32.hip", "attend_shared_f16.hip", "attend_shared_bf16.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

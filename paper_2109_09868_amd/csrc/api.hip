@@ -384,6 +384,32 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
                                               sinks < most ? sinks : most);
 }
 
+int approxifer_attend_shared(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,
+                             const void *d_k_pool, const void *d_v_pool, void *d_out, const int32_t *d_groups, const int32_t *d_shared,
+                             int64_t C, int64_t max_rows, int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks, double scale,
+                             int32_t *d_status, void *d_workspace, size_t workspace_bytes, void *stream) {
+    approxifer::AttendCall c;
+    bool empty = false;
+    if (C < 0 || max_shared < 0) return APPROXIFER_ERR_BAD_SHAPE;
+    if (C > APPROXIFER_MAX_SEQUENCES) return APPROXIFER_ERR_LIMIT;
+    const int rc = check_attend(h_seq, Hq, Hkv, Dh, dtype, d_q, q_stride, d_k_pool, d_v_pool, d_out, max_rows, max_len, window, sinks,
+                                scale, d_status, d_workspace, &c, &empty);
+    if (rc != APPROXIFER_OK || empty) return rc;
+    if (C > 0 && c.seq.T > 0 && (d_groups == nullptr || d_shared == nullptr)) return APPROXIFER_ERR_NULL_POINTER;
+    return approxifer::launch_attend_shared(c, d_groups, d_shared, C, max_shared < c.max_len ? max_shared : c.max_len, d_workspace,
+                                            d_workspace != nullptr ? workspace_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
+size_t approxifer_attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows,
+                                                int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks) {
+    if (!attend_sizes_taken(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks) || C < 0 || C > APPROXIFER_MAX_SEQUENCES ||
+        max_shared < 0)
+        return 0;
+    const int64_t most = APPROXIFER_MAX_TOKENS, length = max_len < most ? max_len : most;
+    return approxifer::attend_shared_workspace_bytes(T, B, C, Hq, Hkv, Dh, dtype, max_rows, length, max_shared < length ? max_shared : length,
+                                                     window < most ? window : 0, sinks < most ? sinks : most);
+}
+
 int approxifer_attend_mass(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,
                            const void *d_k_pool, const void *d_v_pool, void *d_out, float *d_mass, int64_t mass_stride, int64_t max_rows,
                            int64_t max_len, int64_t window, int64_t sinks, double scale, int32_t *d_status, void *d_workspace,

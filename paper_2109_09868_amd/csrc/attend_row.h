@@ -17,20 +17,30 @@ struct Visible {
     __device__ __forceinline__ bool sees(int j) const { return j <= place && (j >= from || j < sinks_end); }
 };
 
-// The keys that rows at places p0..p1 see, in tiles of kKeys: those of the first tokens, then those of the window.
-template <int kKeys>
+// The keys that rows at places p0..p1 see, in tiles of kKeys: those of the first tokens, then those of the window.  kRange: of these
+// the ones at `low` up to `high` - 1.
+template <int kKeys, bool kRange = false>
 struct KeyTiles {
-    int last, from, sinks_end, sink_tiles, main_tile, steps;
-    __device__ __forceinline__ KeyTiles(int window, int sinks, int p0, int p1) : last(p1) {
+    int last, from, sinks_end, sink_tiles, main_tile, steps, low;
+    __device__ __forceinline__ KeyTiles(int window, int sinks, int p0, int p1, int begin = 0, int high = 0x7fffffff)
+        : last(kRange ? min(p1, high - 1) : p1), low(kRange ? begin : 0) {
         from = window > 0 ? max(p0 - window + 1, 0) : 0;
-        sinks_end = min(sinks, from);
-        sink_tiles = (sinks_end + kKeys - 1) / kKeys;
-        main_tile = max(from / kKeys, sink_tiles);
-        steps = p1 < 0 ? 0 : sink_tiles + max(p1 / kKeys + 1 - main_tile, 0);
+        if (kRange) from = max(from, low);
+        sinks_end = kRange ? max(min(min(sinks, from), last + 1), low) : min(sinks, from);
+        const int sinks_tile = (sinks_end + kKeys - 1) / kKeys;
+        sink_tiles = !kRange ? sinks_tile : sinks_end > low ? sinks_tile - low / kKeys : 0;
+        main_tile = !kRange || sink_tiles > 0 ? max(from / kKeys, sinks_tile) : from / kKeys;
+        steps = last < low ? 0 : sink_tiles + (kRange && from > last ? 0 : max(last / kKeys + 1 - main_tile, 0));
     }
-    __device__ __forceinline__ int begin_of(int it) const { return (it < sink_tiles ? it : main_tile + it - sink_tiles) * kKeys; }
+    __device__ __forceinline__ int begin_of(int it) const {
+        return (it < sink_tiles ? (kRange ? low / kKeys + it : it) : main_tile + it - sink_tiles) * kKeys;
+    }
     // the key itself, or one that some row sees where none sees this one: what nobody sees is not read
-    __device__ __forceinline__ int seen(int j) const { return j > last ? last : j < from && j >= sinks_end ? from : j; }
+    __device__ __forceinline__ int seen(int j) const {
+        if (kRange && j < low) j = low;
+        if (kRange && from > last) return min(j, sinks_end - 1);
+        return j > last ? last : j < from && j >= sinks_end ? from : j;
+    }
 };
 
 // One row over the places [a0, a1) and [b0, b1), as far as it sees them.  q: [256] floats of LDS of this wave.  Lane l has

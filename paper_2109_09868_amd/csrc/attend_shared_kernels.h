@@ -1,0 +1,66 @@
+// The attention kernels for groups of sequences that begin alike, and their launches.
+#pragma once
+
+#include "attend_tiles.h"
+#include "attend_tokens.h"
+
+namespace approxifer {
+
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_shared_tiles_kernel(AttendCall c, SharedCall shared) {
+    attend_tiles<E, DP, kWhole, kSmall, true>(c, TileGrid{}, nullptr, shared);
+}
+
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_shared_tokens_kernel(AttendCall c, SharedCall shared) {
+    attend_tokens<E, DP, kWhole, kSmall, true>(c, TokenGrid{}, nullptr, shared);
+}
+
+// F<E, DP, kWhole, kSmall>::run() for a call's head: as many instances as the kernels for single sequences have.
+template <template <class, int, bool, bool> class F, class E, bool kSmall>
+hipError_t shared_instance(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    if (c.Dh == 64) return F<E, 64, true, kSmall>::run(c, shared, stream);
+    if (c.Dh == 128) return F<E, 128, true, kSmall>::run(c, shared, stream);
+    if (c.Dh == 256) return F<E, 256, true, kSmall>::run(c, shared, stream);
+    if (c.Dh < 64) return F<E, 64, false, kSmall>::run(c, shared, stream);
+    if (c.Dh <= 96) return F<E, 96, false, kSmall>::run(c, shared, stream);
+    if (c.Dh < 128) return F<E, 128, false, kSmall>::run(c, shared, stream);
+    if (c.Dh <= 192) return F<E, 192, false, kSmall>::run(c, shared, stream);
+    return F<E, 256, false, kSmall>::run(c, shared, stream);
+}
+
+inline unsigned shared_blocks(const AttendCall &c, const SharedCall &shared) {
+    return static_cast<unsigned>((shared.common_slots * shared.common_parts + shared.own_slots * shared.own_parts) * c.Hkv);
+}
+template <class E, int DP, bool kWhole, bool kSmall>
+struct SharedTiles {
+    static hipError_t run(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+        return launch_kernel(attend_shared_tiles_kernel<E, DP, kWhole, kSmall>, dim3(shared_blocks(c, shared)), dim3(256), 0, stream, c, shared);
+    }
+};
+template <class E, int DP, bool kWhole, bool kSmall>
+struct SharedTokens {
+    static hipError_t run(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+        return launch_kernel(attend_shared_tokens_kernel<E, DP, kWhole, kSmall>, dim3(shared_blocks(c, shared)), dim3(256), 0, stream, c, shared);
+    }
+};
+
+template <class E>
+hipError_t launch_shared_tiles_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    return c.seq.page_shift >= 4 ? shared_instance<SharedTiles, E, false>(c, shared, stream) : shared_instance<SharedTiles, E, true>(c, shared, stream);
+}
+template <class E>
+hipError_t launch_shared_tokens_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    return c.seq.page_shift >= 4 ? shared_instance<SharedTokens, E, false>(c, shared, stream)
+                                 : shared_instance<SharedTokens, E, true>(c, shared, stream);
+}
+template <class E>
+hipError_t launch_shared_join_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    const int64_t blocks = (c.seq.T * c.Hq + 3) / 4 + (c.status != nullptr ? (c.seq.B + 3) / 4 : 0);
+    const dim3 grid(static_cast<unsigned>(blocks));
+    if (c.Dh <= 64) return launch_kernel(attend_shared_join_kernel<E, 64>, grid, dim3(256), 0, stream, c, shared);
+    if (c.Dh <= 128) return launch_kernel(attend_shared_join_kernel<E, 128>, grid, dim3(256), 0, stream, c, shared);
+    return launch_kernel(attend_shared_join_kernel<E, 256>, grid, dim3(256), 0, stream, c, shared);
+}
+
+}  // namespace approxifer

@@ -18,7 +18,7 @@
 // and meet after each, and wait for their first loads.
 #pragma once
 
-#include "attend_join.h"
+#include "attend_shared.h"
 
 namespace approxifer {
 
@@ -79,9 +79,10 @@ __device__ __forceinline__ int slot_owner(const Sequences &s, int64_t slot, int 
     return lo;
 }
 
-// kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.
-template <class E, int DP, bool kWhole, bool kSmall>
-__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, TileGrid g, float *workspace) {
+// kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.  kShared: rows are those of a group of sequences, or of one,
+// and keys the ones that the group has in common, or the others; g is then not used, and sums always meet in the workspace.
+template <class E, int DP, bool kWhole, bool kSmall, bool kShared>
+__device__ __forceinline__ void attend_tiles(const AttendCall &c, const TileGrid &g, float *workspace, const SharedCall &shared) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
     constexpr bool kDirect = kWhole && !kSmall && S::kStride == S::kPieces;
@@ -89,35 +90,58 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     constexpr int kVec = S::kSize == 2 ? 1 : kOut % 4 == 0 ? 4 : kOut % 2 == 0 ? 2 : 1;
     __shared__ __align__(16) char lds[S::kLds];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
-    const int64_t heads = g.slots * c.Hkv, work = heads * g.parts;
-    if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
-        const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
-        if (b >= c.seq.B) return;
-        const int st = attend_status(c, static_cast<int>(b));
-        if (lane == 0) c.status[b] = st;
-        return;
-    }
-    const int part = static_cast<int>(blockIdx.x / heads), index = static_cast<int>(blockIdx.x % heads);
-    const int h = index % c.Hkv, group = c.Hq / c.Hkv;
-    const int64_t slot = g.slots - 1 - index / c.Hkv;
+    const int group = c.Hq / c.Hkv;
+    int part, index = 0, h, b;
     int64_t tile = 0;
-    const int b = g.single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
-    const Rows rows = rows_of(c.seq, b);
-    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = tile * S::kRows;
-    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || tile < 0 || first >= row_count) return;
+    SharedUnit unit;
+    if constexpr (kShared) {
+        unit = shared_unit(c, shared, blockIdx.x, S::kRows);
+        if (unit.rows == 0) return;
+        part = unit.part;
+        h = unit.h;
+        b = unit.b;
+        tile = unit.block;
+    } else {
+        const int64_t heads = g.slots * c.Hkv, work = heads * g.parts;
+        if (blockIdx.x >= work) {                             // the last workgroups: statuses, a wave for each
+            const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
+            if (b >= c.seq.B) return;
+            const int st = attend_status(c, static_cast<int>(b));
+            if (lane == 0) c.status[b] = st;
+            return;
+        }
+        part = static_cast<int>(blockIdx.x / heads);
+        index = static_cast<int>(blockIdx.x % heads);
+        h = index % c.Hkv;
+        const int64_t slot = g.slots - 1 - index / c.Hkv;
+        b = g.single ? static_cast<int>(slot) : slot_owner(c.seq, slot, group, S::kRows, &tile);
+    }
+    Rows rows;
+    if constexpr (!kShared) rows = rows_of(c.seq, b);
+    const int64_t row_count = kShared ? unit.rows : static_cast<int64_t>(rows.n) * group, first = tile * S::kRows;
+    if (!kShared && (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || tile < 0 || first >= row_count)) return;
 
     // this lane's row; lanes behind the last row repeat it
     const int64_t row = min(first + wave * 32 + row32, row_count - 1);
     const int token = static_cast<int>(row / group), head = h * group + static_cast<int>(row % group);
-    const int place = rows.place(token);
-    const int p0 = rows.place(static_cast<int>(first / group));
-    const int p1 = rows.place(static_cast<int>(min(first + S::kRows - 1, row_count - 1) / group));
-    const int w0 = __builtin_amdgcn_readfirstlane(place);
-    const int w1 = __builtin_amdgcn_readlane(place, 31);
+    const int64_t start = kShared ? unit.start : rows.start;
+    int place, p0, p1, w0, w1;                                // places: this row's, and the least and largest of the tile and of the wave
+    if constexpr (kShared) {
+        place = shared_place(c, unit, start + token);
+        unit.places_of(place, S::kWaves, reinterpret_cast<int *>(lds), &p0, &p1, &w0, &w1);
+    } else {
+        place = rows.place(token);
+        p0 = rows.place(static_cast<int>(first / group));
+        p1 = rows.place(static_cast<int>(min(first + S::kRows - 1, row_count - 1) / group));
+        w0 = __builtin_amdgcn_readfirstlane(place);
+        w1 = __builtin_amdgcn_readlane(place, 31);
+    }
+    const int end = kShared ? unit.end : 0x7fffffff, low = kShared ? unit.low : 0;         // of the keys that there are here
+    const int near = kShared ? min(place, end - 1) : place;   // the last that this row sees of them
 
     v4i q[kSteps];
     {
-        const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
+        const V *x = static_cast<const V *>(c.q) + (start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
         const bool whole = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
         const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
         const int Dh = c.scale == 0.0f ? 0 : kWhole ? DP : c.Dh;  // scale 0: scores of 0 at scale 1
@@ -126,13 +150,13 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     }
     const float scale = c.scale == 0.0f ? 1.0f : fabsf(c.scale) * 1.44269504088896340736f;
 
-    const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
-    const int chunk = g.chunk_of<kKeys>(keys.steps);
+    const KeyTiles<kKeys, kShared> keys(c.window, c.sinks, p0, p1, low, end);
+    const int chunk = kShared ? unit.chunk_of<kKeys>(keys.steps) : g.chunk_of<kKeys>(keys.steps);
     const int begin = part * chunk, steps = min(keys.steps, begin + chunk);       // this part's tiles: begin .. steps - 1
-    if (begin >= steps && part > 0) return;
-    const bool alone = keys.steps <= chunk;
+    if (!kShared && begin >= steps && part > 0) return;
+    const bool alone = !kShared && keys.steps <= chunk;
     const auto begin_of = [&](int it) { return keys.begin_of(it); };
-    const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
+    const int32_t *table = c.seq.table + static_cast<int64_t>(b) * c.seq.M;
     const int shift = c.seq.page_shift, in_page = (1 << shift) - 1;
     const auto page_at = [&](int it) {                        // of key `lane` of the tile
         return table[keys.seen(begin_of(min(it, steps - 1)) + (lane & (kKeys - 1))) >> shift];
@@ -196,6 +220,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         page_next = page_at(it + 1);
     };
     const auto whole_tile = [&](int j0, int a, int b) {       // every row from place a to place b sees every key
+        if (kShared && (j0 < low || j0 + kKeys > end)) return false;
         return j0 + kKeys - 1 <= a && (c.window == 0 || j0 > b - c.window || j0 + kKeys <= c.sinks);
     };
     const auto put = [&](int it) {                            // from the registers into LDS
@@ -254,7 +279,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
             else load(it + 1);
         }
         const char *const kt = lds + (it & 1) * 2 * S::kBytes, *const vt = kt + S::kBytes;
-        const bool none = j0 > w1 || (c.window > 0 && j0 + kKeys - 1 <= w0 - c.window && j0 >= c.sinks);
+        const bool none = j0 > (kShared ? min(w1, end - 1) : w1) || (c.window > 0 && j0 + kKeys - 1 <= w0 - c.window && j0 >= c.sinks);
         if (!none) {
             v16f s[kBlocks];
 #pragma unroll
@@ -275,7 +300,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
             __builtin_amdgcn_sched_group_barrier(kMfma, S::kAhead * (S::kSize == 4 ? 4 : 1), 0);
             // what is hidden from a row: keys behind it, keys before its window; and keys of bad pages are no numbers.  Few tiles need any
             // of it, and hardly one needs all.
-            const int reach = place - j0 - 4 * half;
+            const int reach = near - j0 - 4 * half;
             if (bad_now != 0) {
                 const unsigned long long off = bad_now >> (4 * half);
 #pragma unroll
@@ -284,14 +309,21 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                     for (int k = 0; k < 16; ++k)
                         if (off >> (b * 32 + 8 * (k / 4) + k % 4) & 1) s[b][k] = NAN;
             }
-            if (j0 + kKeys - 1 > w0) {
+            if (kShared && j0 < low) {
+                const int ahead = low - j0 - 4 * half;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[b][k] = b * 32 + 8 * (k / 4) + k % 4 >= ahead ? s[b][k] : -INFINITY;
+            }
+            if (j0 + kKeys - 1 > (kShared ? min(w0, end - 1) : w0)) {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
                     for (int k = 0; k < 16; ++k) s[b][k] = b * 32 + 8 * (k / 4) + k % 4 <= reach ? s[b][k] : -INFINITY;
             }
             if (c.window != 0 && j0 <= w1 - c.window && j0 + kKeys > c.sinks) {
-                const int start = c.sinks - j0 - 4 * half, back = reach - c.window;
+                const int start = c.sinks - j0 - 4 * half, back = (kShared ? place - j0 - 4 * half : reach) - c.window;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -384,10 +416,10 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
         __syncthreads();
     }
 
-    float *const partial = workspace + (index * static_cast<int64_t>(g.parts) + part) * part_floats(S::kRows, c.Dh);
+    float *const partial = kShared ? nullptr : workspace + (index * static_cast<int64_t>(g.parts) + part) * part_floats(S::kRows, c.Dh);
     total = half_sum(total);
-    if (c.stats != nullptr && alone && half == 0 && first + wave * 32 + row32 < row_count)
-        RowStats(top == -INFINITY ? top : top * scale - kLift<E>, total).store(c, rows.start + token, head);
+    if (!kShared && c.stats != nullptr && alone && half == 0 && first + wave * 32 + row32 < row_count)
+        RowStats(top == -INFINITY ? top : top * scale - kLift<E>, total).store(c, start + token, head);
     // A weight of 0 (hidden, or rounded to it) times an infinity is NaN, and so is all that a hidden NaN touches: the product cannot hide it.
     // Rows with such sums are computed again, element by element; those whose weights are no numbers are NaN as they have to be.  (A prompt of 2048
     // tokens, 8 heads of 128 on 2, bf16: 0.08 to 0.1 ms, with an infinity that all rows see too; with a NaN in their place, where all rows are
@@ -402,11 +434,18 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
     if (first + wave * 32 + row32 < row_count && (odd_rows >> row32 & 1) == 0) {
         const float inverse = !alone ? 1.0f : total == 0.0f ? 0.0f : 1.0f / total;
         const int n = wave * 32 + row32;
+        const int64_t at = (start + token) * c.Hq + head;
+        float *sums = kShared ? shared.sums(c, unit.sum_part, at) : partial + n * c.Dh;
         if (!alone && half == 0) {
-            partial[S::kRows * c.Dh + n] = top == -INFINITY ? top : top * scale - kLift<E>;
-            partial[S::kRows * c.Dh + S::kRows + n] = total;
+            const float most = top == -INFINITY ? top : top * scale - kLift<E>;
+            if constexpr (kShared) {
+                shared.settle(c, unit.sum_part, at, most, total);
+            } else {
+                partial[S::kRows * c.Dh + n] = most;
+                partial[S::kRows * c.Dh + S::kRows + n] = total;
+            }
         }
-        V *y = static_cast<V *>(c.out) + ((rows.start + token) * c.Hq + head) * c.Dh;
+        V *y = static_cast<V *>(c.out) + at * c.Dh;
 #pragma unroll
         for (int o = 0; o < kOut; o += kVec)
 #pragma unroll
@@ -417,14 +456,21 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles
                     const auto value = [&](int n) { return out[o + (4 * j + n) % kVec][4 * k + (4 * j + n) / kVec] * inverse; };
                     if (!kWhole && d >= c.Dh) continue;
                     if (alone) store4<E>(y + d, value(0), value(1), value(2), value(3));
-                    else *reinterpret_cast<v4f *>(partial + n * c.Dh + d) = v4f{value(0), value(1), value(2), value(3)};
+                    else *reinterpret_cast<v4f *>(sums + d) = v4f{value(0), value(1), value(2), value(3)};
                 }
     }
     float *const scratch = reinterpret_cast<float *>(lds) + wave * APPROXIFER_MAX_HEAD_DIM;      // the tiles are done with
     for (unsigned left = odd_rows; left != 0; left &= left - 1) {
         const int n = wave * 32 + __builtin_ctz(left);
-        if (first + n < row_count) attend_part<E>(c, rows, first + n, h, scratch, keys, begin, steps, alone, partial, S::kRows, n);
+        if (first + n >= row_count) continue;
+        if constexpr (kShared) shared_part<E>(c, shared, unit, first + n, scratch, keys, begin, steps);
+        else attend_part<E>(c, rows, first + n, h, scratch, keys, begin, steps, alone, partial, S::kRows, n);
     }
+}
+
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, TileGrid g, float *workspace) {
+    attend_tiles<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{});
 }
 
 template <class E, int DP, int kWaves>

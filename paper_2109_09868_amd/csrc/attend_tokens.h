@@ -10,7 +10,7 @@
 // 4.5 TB/s; 24 of up to 129 keys (12 heads of 64, 32 bits) 11 us, of which the bytes are 3.
 #pragma once
 
-#include "attend_join.h"
+#include "attend_shared.h"
 
 namespace approxifer {
 
@@ -39,9 +39,9 @@ struct TokenGrid {
     __device__ __forceinline__ int chunk_of(int steps) const { return parts == 1 ? 0x7fffffff : max(chunk, (steps + parts - 1) / parts); }
 };
 
-// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.
-template <class E, int DP, bool kWhole, bool kSmall>
-__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(AttendCall c, TokenGrid g, float *workspace) {
+// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.  kShared: as in attend_tiles().
+template <class E, int DP, bool kWhole, bool kSmall, bool kShared>
+__device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, const SharedCall &shared) {
     typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
     constexpr int kKeys = S::kKeys, kOut = DP / 16;
@@ -49,40 +49,66 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     __shared__ float tops[S::kWaves][16], totals[S::kWaves][16];
     __shared__ int dirty;
     const int lane = lane_id(), wave = wave_id(), quarter = lane >> 4, row16 = lane & 15;
-    const int64_t units = static_cast<int64_t>(g.pairs) * g.parts, work = units * g.blocks;
-    if (blockIdx.x >= work) {                                 // the last workgroups: statuses, a wave for each
-        const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
-        if (b >= c.seq.B) return;
-        const int st = attend_status(c, static_cast<int>(b));
-        if (lane == 0) c.status[b] = st;
-        return;
+    const int group = c.Hq / c.Hkv;
+    int part, h, b, pair = 0, block = 0;
+    SharedUnit unit;
+    if constexpr (kShared) {
+        unit = shared_unit(c, shared, blockIdx.x, S::kRows);
+        if (unit.rows == 0) return;
+        part = unit.part;
+        h = unit.h;
+        b = unit.b;
+        block = static_cast<int>(unit.block);
+    } else {
+        const int64_t units = static_cast<int64_t>(g.pairs) * g.parts, work = units * g.blocks;
+        if (blockIdx.x >= work) {                             // the last workgroups: statuses, a wave for each
+            const int64_t b = (blockIdx.x - work) * S::kWaves + wave;
+            if (b >= c.seq.B) return;
+            const int st = attend_status(c, static_cast<int>(b));
+            if (lane == 0) c.status[b] = st;
+            return;
+        }
+        const int unit = static_cast<int>(blockIdx.x % units);
+        block = static_cast<int>(blockIdx.x / units);
+        pair = unit % g.pairs;
+        part = unit / g.pairs;
+        h = pair % c.Hkv;
+        b = pair / c.Hkv;
     }
-    const int unit = static_cast<int>(blockIdx.x % units), block = static_cast<int>(blockIdx.x / units);
-    const int pair = unit % g.pairs, part = unit / g.pairs;
-    const int h = pair % c.Hkv, group = c.Hq / c.Hkv;
-    const Rows rows = rows_of(c.seq, pair / c.Hkv);
-    const int64_t row_count = static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(block) * S::kRows;
-    if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || first >= row_count) return;
+    Rows rows;
+    if constexpr (!kShared) rows = rows_of(c.seq, b);
+    const int64_t row_count = kShared ? unit.rows : static_cast<int64_t>(rows.n) * group, first = static_cast<int64_t>(block) * S::kRows;
+    if (!kShared && (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || first >= row_count)) return;
 
     const int64_t row = min(first + row16, row_count - 1);
     const int token = static_cast<int>(row / group), head = h * group + static_cast<int>(row % group);
-    const int place = rows.place(token);
-    const int p0 = __builtin_amdgcn_readfirstlane(place), p1 = __builtin_amdgcn_readlane(place, 15);
-    const KeyTiles<kKeys> keys(c.window, c.sinks, p0, p1);
-    const int chunk = g.chunk_of(keys.steps), begin = part * chunk, end = min(keys.steps, begin + chunk);
-    if (begin >= end && part > 0) return;                     // the parts that there are end before this one
+    const int64_t start = kShared ? unit.start : rows.start;
+    int place, p0, p1;                                        // places: this row's, and the least and largest of the block
+    if constexpr (kShared) {
+        place = shared_place(c, unit, start + token);
+        unit.places_of(place, &p0, &p1);
+    } else {
+        place = rows.place(token);
+        p0 = __builtin_amdgcn_readfirstlane(place);
+        p1 = __builtin_amdgcn_readlane(place, 15);
+    }
+    const int high = kShared ? unit.end : 0x7fffffff, low = kShared ? unit.low : 0;        // of the keys that there are here
+    const KeyTiles<kKeys, kShared> keys(c.window, c.sinks, p0, p1, low, high);
+    const int chunk = kShared ? unit.chunk_of<kKeys>(keys.steps) : g.chunk_of(keys.steps), begin = part * chunk,
+              end = min(keys.steps, begin + chunk);
+    if (!kShared && begin >= end && part > 0) return;         // the parts that there are end before this one
     if (threadIdx.x == 0) dirty = 0;
 
     v4i q[S::kSteps];
     {
-        const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
+        const V *x = static_cast<const V *>(c.q) + (start + token) * c.q_stride + static_cast<int64_t>(head) * c.Dh;
         const bool whole = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
         const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) q[s] = query_piece<E>(x, (4 * s + quarter) * S::kPerPiece, c.Dh, whole, flip);
     }
     const float scale = fabsf(c.scale) * 1.44269504088896340736f;
-    const int32_t *table = c.seq.table + static_cast<int64_t>(rows.b) * c.seq.M;
+    const int32_t *table = c.seq.table + static_cast<int64_t>(b) * c.seq.M;
     const int shift = c.seq.page_shift, slots = (1 << shift) - 1;
     const V *const k_pool = static_cast<const V *>(c.k_pool), *const v_pool = static_cast<const V *>(c.v_pool);
     char *const vt = lds + wave * S::kBytes;
@@ -141,7 +167,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
     const auto step = [&](int it, auto more) {
         const int j0 = keys.begin_of(it);
         const unsigned long long bad = bad_next;
-        const bool whole = j0 + kKeys - 1 <= p0 && (c.window == 0 || j0 > p1 - c.window || j0 + kKeys <= c.sinks);
+        const bool whole = (!kShared || (j0 >= low && j0 + kKeys <= high)) && j0 + kKeys - 1 <= p0 && (c.window == 0 || j0 > p1 - c.window || j0 + kKeys <= c.sinks);
         v4f s[S::kBlocks];
 #pragma unroll
         for (int b = 0; b < S::kBlocks; ++b) {
@@ -165,7 +191,7 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
             const int index = n * kWave + lane;
             *reinterpret_cast<v4i *>(vt + piece_at<S::kStride>(index / S::kPieces, index % S::kPieces)) = v_next[n];
         }
-        if (!whole && p0 != p1) {                             // rows of one place see all that is read
+        if (!whole && (kShared || p0 != p1)) {                             // rows of one place see all that is read
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) odd |= not_finite<E>(v_next[n]);
         }
@@ -173,13 +199,15 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         const bool masked = !whole || bad != 0;
         if (masked) {
             const int reach = place - j0 - 4 * quarter, start = c.sinks - j0 - 4 * quarter;
+            const int ahead = low - j0 - 4 * quarter, behind = high - j0 - 4 * quarter;
             const unsigned long long off = bad >> (4 * quarter);
 #pragma unroll
             for (int b = 0; b < S::kBlocks; ++b)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int key = b * 16 + k;
-                    const bool sees = key <= reach && (c.window == 0 || key > reach - c.window || key < start);
+                    const bool sees = key <= reach && (c.window == 0 || key > reach - c.window || key < start) &&
+                                      (!kShared || (key >= ahead && key < behind));
                     if (off >> key & 1) s[b][k] = NAN;
                     s[b][k] = sees ? s[b][k] : -INFINITY;
                 }
@@ -275,10 +303,10 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
                 v4f{out[o][0] * f, out[o][1] * f, out[o][2] * f, out[o][3] * f};
     }
     __syncthreads();
-    const bool alone = keys.steps <= chunk;
+    const bool alone = !kShared && keys.steps <= chunk;
     const int64_t slot = (static_cast<int64_t>(pair) * g.blocks + block) * g.parts + part;
-    float *const partial = workspace + slot * part_floats(S::kRows, c.Dh);
-    if (c.stats != nullptr && alone && threadIdx.x < S::kRows && first + threadIdx.x < row_count) {
+    float *const partial = kShared ? nullptr : workspace + slot * part_floats(S::kRows, c.Dh);
+    if (!kShared && c.stats != nullptr && alone && threadIdx.x < S::kRows && first + threadIdx.x < row_count) {
         const int r = threadIdx.x;
         float m = tops[0][r], l = 0.0f;
 #pragma unroll
@@ -287,14 +315,16 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         for (int w = 0; w < S::kWaves; ++w)
             l += tops[w][r] == -INFINITY ? totals[w][r] : totals[w][r] * __builtin_amdgcn_exp2f((tops[w][r] - m) * scale);
         const int64_t at = first + r;
-        RowStats(m == -INFINITY ? m : m * scale - kLift<E>, l).store(c, rows.start + at / group, h * group + static_cast<int>(at % group));
+        RowStats(m == -INFINITY ? m : m * scale - kLift<E>, l).store(c, start + at / group, h * group + static_cast<int>(at % group));
     }
     if (dirty != 0) {                                         // rows that must not see what the product cannot hide
         __syncthreads();
         float *const scratch = reinterpret_cast<float *>(vt);
         for (int n = wave; n < S::kRows; n += S::kWaves)
-            if (first + n < row_count)
-                attend_part<E>(c, rows, first + n, h, scratch, keys, begin, end, alone, partial, S::kRows, n);
+            if (first + n < row_count) {
+                if constexpr (kShared) shared_part<E>(c, shared, unit, first + n, scratch, keys, begin, end);
+                else attend_part<E>(c, rows, first + n, h, scratch, keys, begin, end, alone, partial, S::kRows, n);
+            }
         return;
     }
     constexpr int kQuads = DP / 4;
@@ -315,8 +345,12 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
         if (alone) {
             const float inverse = l == 0.0f ? 0.0f : 1.0f / l;
             const int64_t at = first + r, t = at / group;
-            V *const y = static_cast<V *>(c.out) + ((rows.start + t) * c.Hq + h * group + at % group) * c.Dh + d;
+            V *const y = static_cast<V *>(c.out) + ((start + t) * c.Hq + h * group + at % group) * c.Dh + d;
             store4<E>(y, sum[0] * inverse, sum[1] * inverse, sum[2] * inverse, sum[3] * inverse);
+        } else if constexpr (kShared) {
+            const int64_t at = first + r, to = (start + at / group) * c.Hq + h * group + at % group;
+            *reinterpret_cast<v4f *>(shared.sums(c, unit.sum_part, to) + d) = sum;
+            if (d == 0) shared.settle(c, unit.sum_part, to, m == -INFINITY ? m : m * scale - kLift<E>, l);
         } else {
             *reinterpret_cast<v4f *>(partial + r * c.Dh + d) = sum;
             if (d == 0) {
@@ -325,6 +359,11 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(
             }
         }
     }
+}
+
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(AttendCall c, TokenGrid g, float *workspace) {
+    attend_tokens<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{});
 }
 
 template <class E, int DP, int kWaves>

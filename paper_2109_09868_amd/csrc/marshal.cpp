@@ -32,6 +32,7 @@ struct Library {
     decltype(&approxifer_cache_compact) cache_compact;
     decltype(&approxifer_cache_evict) cache_evict;
     decltype(&approxifer_attend_mass) attend_mass;
+    decltype(&approxifer_attend_shared) attend_shared;
 };
 
 // The handle of a loaded library: its entry points, by address, in the order above.
@@ -57,7 +58,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
         reinterpret_cast<decltype(Library::append)>(p[8]),         reinterpret_cast<decltype(Library::attend)>(p[9]),
         reinterpret_cast<decltype(Library::cache_reserve)>(p[10]), reinterpret_cast<decltype(Library::cache_fork)>(p[11]),
         reinterpret_cast<decltype(Library::cache_compact)>(p[12]), reinterpret_cast<decltype(Library::cache_evict)>(p[13]),
-        reinterpret_cast<decltype(Library::attend_mass)>(p[14])};
+        reinterpret_cast<decltype(Library::attend_mass)>(p[14]),   reinterpret_cast<decltype(Library::attend_shared)>(p[15])};
     PyObject *c = PyCapsule_New(lib, kCapsule, [](PyObject *o) { delete static_cast<Library *>(PyCapsule_GetPointer(o, kCapsule)); });
     if (c == nullptr) delete lib;
     return c;
@@ -451,6 +452,36 @@ PyObject *attend_mass(PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (library, q, k_pool, v_pool, table, lens, starts, groups, shared, max_rows, max_len, max_shared, window, sinks, scale or None, out, status,
+//  workspace or None)
+PyObject *attend_shared(PyObject *const *a, Py_ssize_t n) {
+    const Library *lib = n == 18 ? library(a[0]) : nullptr;
+    if (lib == nullptr) return nullptr;
+    Cache c(a[2], a[3], a[4], a[5], a[6]);
+    if (!c.ok) Py_RETURN_NONE;
+    const TokenRows q(a[1], c.type);
+    const at::Tensor *length = plain(a[8], kI32), *w = a[17] == Py_None ? nullptr : plain(a[17], kU8);
+    int64_t rows, most, common, window, sinks;
+    if (q.data == nullptr || q.Dh != c.Dh || q.heads > APPROXIFER_MAX_HEADS || !integer64(a[9], rows) || !integer64(a[10], most) ||
+        !integer64(a[11], common) || !integer64(a[12], window) || !integer64(a[13], sinks) || length == nullptr || length->dim() != 1 ||
+        (a[17] != Py_None && w == nullptr))
+        Py_RETURN_NONE;
+    double scale = 1.0 / std::sqrt(static_cast<double>(c.Dh));
+    if (a[14] != Py_None && !real(a[14], scale)) Py_RETURN_NONE;
+    const int64_t C = length->numel();
+    void *groups = shaped(a[7], kI32, C + 1), *shared = length->data_ptr(), *out = shaped(a[15], c.type, q.T, q.heads, q.Dh),
+         *status = shaped(a[16], kI32, c.seq.B);
+    if (groups == nullptr || shared == nullptr || out == nullptr || status == nullptr) Py_RETURN_NONE;
+    void *ws = w != nullptr ? w->data_ptr() : nullptr;
+    const size_t ws_bytes = w != nullptr ? static_cast<size_t>(w->numel()) : 0;
+    c.seq.T = q.T;
+    return status_of([&](void *s) {
+        return lib->attend_shared(&c.seq, static_cast<int>(q.heads), c.Hkv, c.Dh, c.dtype, q.data, q.stride, c.k, c.v, out,
+                                  static_cast<const int32_t *>(groups), static_cast<const int32_t *>(shared), C, rows, most, common, window,
+                                  sinks, scale, static_cast<int32_t *>(status), ws, ws_bytes, s);
+    });
+}
+
 int32_t *ints(void *p) { return static_cast<int32_t *>(p); }
 
 // (library, table, lens, refs, add, page, status)
@@ -572,6 +603,7 @@ PyMethodDef methods[] = {
     APPROXIFER_METHOD(wait_mask), APPROXIFER_METHOD(append),         APPROXIFER_METHOD(attend),
     APPROXIFER_METHOD(cache_reserve), APPROXIFER_METHOD(cache_fork), APPROXIFER_METHOD(cache_compact),
     APPROXIFER_METHOD(cache_evict),   APPROXIFER_METHOD(attend_mass),
+    APPROXIFER_METHOD(attend_shared),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -91,3 +91,22 @@ def test_attend_mass_refusals(lib):
     for args in ((0, 2, 4, 2, 64), (4, 0, 4, 2, 64), (4, 2, 3, 2, 64), (4, 2, 4, 2, 60), (4, 2, 4, 2, 264)):
         assert need(*args, torch.float16, 1, 100) == 0
     assert need(4, 2, 4, 2, 64, torch.float16, 1, 100) >= 256
+
+
+def _shared(lib, seq=None, Hq=4, Hkv=2, Dh=64, dtype=0, q=FAKE, qs=256, kp=FAKE, vp=FAKE, out=FAKE, groups=FAKE, shared=FAKE, C=1, rows=1,
+            length=48, common=20, window=0, sinks=0, scale=1.0, status=FAKE, ws=None, ws_bytes=0):
+    s = ctypes.byref(seq if seq is not None else _seq()) if seq is not False else None
+    return lib.approxifer_attend_shared(s, Hq, Hkv, Dh, dtype, q, qs, kp, vp, out, groups, shared, C, rows, length, common, window, sinks, scale,
+                                        status, ws, ws_bytes, None)
+
+
+def test_attend_shared_refusals(lib):
+    _sizes_are_refused(lib, _shared)
+    assert _shared(lib, groups=None) == -1 and _shared(lib, shared=None) == -1
+    assert _shared(lib, C=-1) == -2 and _shared(lib, common=-1) == -2 and _shared(lib, C=(1 << 20) + 1) == -3
+    import torch
+    need = binding.approxifer_attend_shared_workspace_bytes
+    for args in ((0, 2, 1, 4, 2, 64), (4, 0, 1, 4, 2, 64), (4, 2, -1, 4, 2, 64), (4, 2, 1, 3, 2, 64), (4, 2, 1, 4, 2, 60)):
+        assert need(*args, torch.float16, 1, 100, 50) == 0
+    assert need(2, 2, 1, 4, 2, 64, torch.float16, 1, 100, -1) == 0
+    assert need(2, 2, 1, 4, 2, 64, torch.float16, 1, 100, 50) % (2 * 4 * 66 * 4) == 0
