@@ -43,104 +43,144 @@ __device__ __forceinline__ unsigned ordered(float x) {
 }
 
 constexpr int kBins = 2048;
+constexpr int kEach = 4;                                      // places next to each other that a thread looks at
 
-__global__ __launch_bounds__(kThreads) void evict_select_kernel(EvictCall c, EvictSpace w) {
-    __shared__ int bins[kBins];
-    __shared__ int sums[16];
-    __shared__ int found_bin, found_rank, moved_from;
-    const int b = blockIdx.x, thread = threadIdx.x, length = c.lens[b], mask = (1 << c.shift) - 1;
-    int32_t *const kept = c.kept + static_cast<int64_t>(b) * c.budget, *const sources = w.sources + static_cast<int64_t>(b) * c.budget;
-    const int32_t *const row = c.table + static_cast<int64_t>(b) * c.M;
-    EvictPlan plan{APPROXIFER_GROUP_OK, 0, length, 0, 0, 0};
-    if (length < 0 || length > (static_cast<int64_t>(c.M) << c.shift) || length > c.mass_stride) {
-        plan.status = APPROXIFER_SEQUENCE_BAD;
-    } else if (length > c.budget) {
-        bool bad = false;                                     // a page that nobody holds could be given to somebody else meanwhile
-        for (int j = thread; j < c.before(length); j += kThreads) {
-            const int p = row[j];
-            bad |= p < 0 || p >= c.P || c.refs[p < 0 || p >= c.P ? 0 : p] < 1;
-        }
-        if (__syncthreads_or(bad)) plan.status = APPROXIFER_SEQUENCE_BAD_PAGE;
-        else plan.cut = 1;
-    }
-    if (plan.cut == 0) {                                      // all of it stays; what is refused keeps nothing that could be told
-        for (int i = thread; i < c.budget; i += kThreads) kept[i] = plan.status == APPROXIFER_GROUP_OK && i < length ? i : -1;
-        if (thread == 0) w.plans[b] = plan;
-        return;
-    }
-    const float *const mass = c.mass + b * c.mass_stride;
-    const int end = length - c.recent, most = c.budget - c.first - c.recent;      // of the places first..end-1 as many stay
-    unsigned cut = 0;                                         // the value of the last that stays; `ties` of those that have it do
-    int ties = 0;
-    if (most > 0) {
-        int rank = most;
+// A sequence that is cut: lists what stays of its middle, the places first..end-1, by kT threads; kHeld: there are no more of them than a
+// thread can hold kEach of.  Returns the first place that moves.
+template <int kT, bool kHeld>
+__device__ __forceinline__ int select_kept(const EvictCall &c, const float *mass, const int32_t *row, int end, int32_t *kept, int32_t *sources,
+                                           int *bins, int *sums, int *found) {
+    const int thread = threadIdx.x, most = c.budget - c.first - c.recent;         // as many of them stay
+    unsigned held[kEach];
+    int pages[kEach];
+    const auto look = [&](int j0) {                           // the keys of places j0.. (0 behind the end, as NaN: they are not counted)
+        float x[kEach];
 #pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-            for (int n = thread; n < kBins; n += kThreads) bins[n] = 0;
-            if (thread == 0) found_bin = 0, found_rank = 1;
-            __syncthreads();
-            for (int j = c.first + thread; j < end; j += kThreads) {
-                const unsigned u = ordered(mass[j]);
-                if (pass == 0 || (u >> (shift + bits)) == (cut >> (shift + bits))) atomicAdd(&bins[u >> shift & ((1 << bits) - 1)], 1);
-            }
-            __syncthreads();
-            const int high = kBins - 1 - 2 * thread, a = bins[high], d = bins[high - 1];  // from the largest down
-            int total;
-            const int above = block_scan(a + d, sums, &total);
-            if (above < rank && rank <= above + a) found_bin = high, found_rank = rank - above;
-            if (above + a < rank && rank <= above + a + d) found_bin = high - 1, found_rank = rank - above - a;
-            __syncthreads();
-            cut |= static_cast<unsigned>(found_bin) << shift;
-            rank = found_rank;
-            __syncthreads();
+        for (int k = 0; k < kEach; ++k) {
+            const int j = min(j0 + k, end - 1);
+            x[k] = mass[j];
+            pages[k] = row[j >> c.shift];
         }
-        ties = rank;
-    }
-    if (thread == 0) moved_from = c.budget;
-    const auto keep = [&](int place, int at) {
-        kept[at] = place;
-        sources[at] = row[place >> c.shift];
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) held[k] = ordered(x[k]);
     };
-    for (int j = thread; j < c.first; j += kThreads) keep(j, j);
-    for (int n = thread; n < c.recent; n += kThreads) keep(end + n, c.budget - c.recent + n);
-    __syncthreads();
-    int from = c.budget - c.recent;                           // the first that moves: one of the middle, or the first recent one
-    int larger = 0, equal = 0;                                // before this stretch
-    for (int j0 = c.first; j0 < end && most > 0; j0 += 4 * kThreads) {
-        const int j = j0 + 4 * thread;
-        bool is_larger[4], is_equal[4];
-        int count = 0;
+    if (kHeld) look(c.first + kEach * thread);
+    const auto keep = [&](int place, int page, int at) {
+        kept[at] = place;
+        sources[at] = page;
+    };
+    for (int j = thread; j < c.first; j += kT) keep(j, row[j >> c.shift], j);
+    for (int n = thread; n < c.recent; n += kT) keep(end + n, row[(end + n) >> c.shift], c.budget - c.recent + n);
+    if (thread == 0) found[2] = c.budget - c.recent;          // the first that moves: one of the middle, or the first recent one
+    if (most == 0) {
+        __syncthreads();
+        return found[2];
+    }
+    unsigned cut = 0;                                         // the value of the last that stays; `rank` of those that have it do
+    int rank = most;
+    for (int pass = 0; pass < 3; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
+        for (int n = thread; n < kBins; n += kT) bins[n] = 0;
+        __syncthreads();
+        const auto count = [&](unsigned u) {
+            if (pass == 0 || (u >> shift >> bits) == (cut >> shift >> bits)) atomicAdd(&bins[u >> shift & ((1 << bits) - 1)], 1);
+        };
+        if (kHeld) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const unsigned u = j + k < end ? ordered(mass[j + k]) : 0;
-            is_larger[k] = j + k < end && u > cut;
-            is_equal[k] = j + k < end && u == cut;
-            count += is_larger[k] + (is_equal[k] << 16);      // at most 4096 of each
+            for (int k = 0; k < kEach; ++k)
+                if (c.first + kEach * thread + k < end) count(held[k]);
+        } else {
+            for (int j = c.first + thread; j < end; j += kT) count(ordered(mass[j]));
         }
+        __syncthreads();
+        constexpr int kOwn = kBins / kT;                      // bins of a thread, from the largest down
+        int in[kOwn], mine = 0, total;
+#pragma unroll
+        for (int n = 0; n < kOwn; ++n) mine += in[n] = bins[kBins - 1 - kOwn * thread - n];
+        int above = block_scan(mine, sums, &total);
+#pragma unroll
+        for (int n = 0; n < kOwn; ++n) {
+            if (above < rank && rank <= above + in[n]) {
+                found[0] = kBins - 1 - kOwn * thread - n;
+                found[1] = rank - above;
+            }
+            above += in[n];
+        }
+        __syncthreads();
+        cut |= static_cast<unsigned>(found[0]) << shift;
+        rank = found[1];
+    }
+    int from = c.budget, larger = 0, equal = 0;               // of the stretches before this one
+    for (int j0 = c.first; j0 < end; j0 += kEach * kT) {
+        const int j = j0 + kEach * thread;
+        if (!kHeld) look(j);
+        int counts = 0;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)                       // at most 4096 of each
+            if (j + k < end) counts += (held[k] > cut) + ((held[k] == cut) << 16);
         int total;
-        const int before = block_scan(count, sums, &total);
+        const int before = block_scan(counts, sums, &total);
         int l = larger + (before & 0xffff), e = equal + (before >> 16);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (is_larger[k] || (is_equal[k] && e < ties)) {
-                const int at = c.first + l + min(e, ties);
-                keep(j + k, at);
+        for (int k = 0; k < kEach; ++k) {
+            if (j + k >= end) break;
+            if (held[k] > cut || (held[k] == cut && e < rank)) {
+                const int at = c.first + l + min(e, rank);
+                keep(j + k, pages[k], at);
                 if (at != j + k) from = min(from, at);
             }
-            l += is_larger[k];
-            e += is_equal[k];
+            l += held[k] > cut;
+            e += held[k] == cut;
         }
         larger += total & 0xffff;
         equal += total >> 16;
     }
-    atomicMin(&moved_from, from);
+    for (int o = 32; o > 0; o >>= 1) from = min(from, __shfl_xor(from, o));
+    if (lane_id() == 0 && from < c.budget) atomicMin(&found[2], from);
     __syncthreads();
+    return found[2];
+}
+
+template <int kT>
+__global__ __launch_bounds__(kT) void evict_select_kernel(EvictCall c, EvictSpace w) {
+    __shared__ int bins[kBins];
+    __shared__ int sums[16];
+    __shared__ int found[3];
+    const int b = blockIdx.x, thread = threadIdx.x, length = c.lens[b], mask = (1 << c.shift) - 1;
+    int32_t *const kept = c.kept + static_cast<int64_t>(b) * c.budget, *const sources = w.sources + static_cast<int64_t>(b) * c.budget;
+    const int32_t *const row = c.table + static_cast<int64_t>(b) * c.M;
+    EvictPlan plan{APPROXIFER_GROUP_OK, 0, length, 0, 0, 0};
+    bool bad = false;                                         // a page that nobody holds could be given to somebody else meanwhile
+    if (length < 0 || length > (static_cast<int64_t>(c.M) << c.shift) || length > c.mass_stride) {
+        plan.status = APPROXIFER_SEQUENCE_BAD;
+    } else if (length > c.budget) {
+        for (int j = thread; j < c.before(length); j += kT) {
+            const int p = row[j];
+            bad |= p < 0 || p >= c.P || c.refs[p < 0 || p >= c.P ? 0 : p] < 1;
+        }
+        plan.cut = 1;
+    }
+    if (plan.cut == 0) {                                      // all of it stays; what is refused keeps nothing that could be told
+        for (int i = thread; i < c.budget; i += kT) kept[i] = plan.status == APPROXIFER_GROUP_OK && i < length ? i : -1;
+        if (thread == 0) w.plans[b] = plan;
+        return;
+    }
+    const float *const mass = c.mass + b * c.mass_stride;
+    const int end = length - c.recent;
+    const int moved = end - c.first <= kEach * kT ? select_kept<kT, true>(c, mass, row, end, kept, sources, bins, sums, found)
+                                                  : select_kept<kT, false>(c, mass, row, end, kept, sources, bins, sums, found);
+    if (__syncthreads_or(bad)) {                              // none of its pages has been looked into
+        for (int i = thread; i < c.budget; i += kT) kept[i] = -1;
+        plan.status = APPROXIFER_SEQUENCE_BAD_PAGE;
+        plan.cut = 0;
+        if (thread == 0) w.plans[b] = plan;
+        return;
+    }
     const int after = c.after();
     // a last page that is not full will be written to by who goes on: it changes hands even where its tokens stay
-    plan.low = min(moved_from < c.budget ? moved_from >> c.shift : after, (c.budget & mask) != 0 ? c.budget >> c.shift : after);
+    plan.low = min(moved < c.budget ? moved >> c.shift : after, (c.budget & mask) != 0 ? c.budget >> c.shift : after);
     int32_t *const pages = w.pages + static_cast<int64_t>(b) * after;
-    for (int j0 = plan.low; j0 < after; j0 += kThreads) {
+    for (int j0 = plan.low; j0 < after; j0 += kT) {
         const int j = j0 + thread, p = j < after ? row[j] : 0;
         const bool wants = j < after && c.refs[p] > 1;
         int total;
@@ -194,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void evict_pages_kernel(const int32_t *re
     }
 }
 
-constexpr int kLoads = 8;                                     // pieces of 16 bytes that a thread has on their way
+constexpr int kLoads = 4;                                     // pieces of 16 bytes that a thread has on their way
 constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
 
 // The first `rows` workgroups bring the sequences up to date, the others copy: a head of a plane, or `pieces` of each of its rows, at a
@@ -260,23 +300,37 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, EvictSpace
         const auto address = [&](int page, int slot, int piece) {
             return pools + (((plane * c.P + page) * heads + head) * size + slot) * row_bytes + (part * pieces + piece) * 16;
         };
-        const int begin = plan.low << c.shift;
-        for (int i0 = begin; i0 < c.budget; i0 += tokens) {
-            v4f x[kLoads];
-            char *to[kLoads];
+        const int begin = plan.low << c.shift, last = c.budget - 1;
+        const auto index = [&](int k, int i0) { return min(i0 + token[k], last); };
+        int from[kLoads], slot[kLoads], to[kLoads];           // of the next stretch's pieces: asked for while this one's are on their way
+        const auto look_up = [&](int i0) {
 #pragma unroll
             for (int k = 0; k < kLoads; ++k) {
-                const int i = i0 + token[k];
-                if (token[k] < tokens && i < c.budget) {
-                    x[k] = *reinterpret_cast<const v4f *>(address(sources[i], kept[i] & mask, piece[k]));
-                    to[k] = address(page_of(plan, pages, i >> c.shift), i & mask, piece[k]);
-                }
+                const int i = index(k, i0);
+                from[k] = sources[i];
+                slot[k] = kept[i];
+                to[k] = pages[i >> c.shift];
             }
+            if (plan.need > 0) {
+#pragma unroll
+                for (int k = 0; k < kLoads; ++k) to[k] = to[k] >= 0 ? to[k] : w.list[plan.offset - 1 - to[k]];
+            }
+        };
+        look_up(begin);
+        for (int i0 = begin; i0 < c.budget; i0 += tokens) {
+            v4f x[kLoads];
+            char *at[kLoads];
+#pragma unroll
+            for (int k = 0; k < kLoads; ++k) {
+                x[k] = *reinterpret_cast<const v4f *>(address(from[k], slot[k] & mask, piece[k]));
+                at[k] = address(to[k], index(k, i0) & mask, piece[k]);
+            }
+            look_up(i0 + tokens);
             __builtin_amdgcn_s_waitcnt(kNoVmem);              // all that this stretch's tokens are written over has been read
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < kLoads; ++k)
-                if (token[k] < tokens && i0 + token[k] < c.budget) *reinterpret_cast<v4f *>(to[k]) = x[k];
+                if (token[k] < tokens && i0 + token[k] < c.budget) *reinterpret_cast<v4f *>(at[k]) = x[k];
         }
     }
 }
@@ -300,7 +354,10 @@ int launch_cache_evict(int32_t *table, int32_t *lens, int32_t *refs, float *mass
     w.pages = at + rounded(B * static_cast<int64_t>(sizeof(EvictPlan) / 4));
     w.sources = w.pages + rounded(static_cast<int64_t>(B) * c.after());
     w.list = w.sources + rounded(static_cast<int64_t>(B) * budget);
-    hipError_t e = launch_kernel(evict_select_kernel, dim3(B), dim3(kThreads), 0, stream, c, w);
+    // short sequences by fewer threads, which meet sooner
+    const int64_t longest = mass_stride < static_cast<int64_t>(M) << page_shift ? mass_stride : static_cast<int64_t>(M) << page_shift;
+    hipError_t e = longest <= 256 * kEach ? launch_kernel(evict_select_kernel<256>, dim3(B), dim3(256), 0, stream, c, w)
+                                          : launch_kernel(evict_select_kernel<kThreads>, dim3(B), dim3(kThreads), 0, stream, c, w);
     if (e == hipSuccess) e = launch_kernel(evict_pages_kernel, dim3(1), dim3(kThreads), 0, stream, refs, w, B, P);
     if (e == hipSuccess) {
         // rows are cut, never below a sector of 64 bytes, until there is work for every CU
