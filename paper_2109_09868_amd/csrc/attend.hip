@@ -6,8 +6,6 @@
 
 namespace approxifer {
 
-namespace {
-
 // Most rows of a sequence and cache head that the tokens kernel takes: more are read again for every 16, and the tiles kernel's products are
 // the better ones for them.  8 tokens by 4 heads (32 rows) of 8 sequences of up to 40000 keys: 284 us here, 186 there; 32-bit products cost
 // more than memory does, whichever kernel forms them, and the tiles kernel's 128 rows are mostly empty: 16 tokens (64 rows) of up to 6000
@@ -18,6 +16,8 @@ bool few_rows(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype) {
     const int64_t rows = max_rows * (Hq / Hkv), blocks = (rows + 15) / 16;
     return rows <= (dtype == APPROXIFER_F32 ? 64 : 16) && B * Hkv * blocks + (B + 3) / 4 < 1 << 24;
 }
+namespace {
+
 // Workgroups that it is given if keys are cut: two on every CU, in one round.  With 256 / 512 / 768 / 1024 / 2048 three sequences of up to
 // 131072 keys take 258 / 244 / 257 / 257 / 255 us.
 constexpr int64_t kTokenGroups = 512;
@@ -26,9 +26,11 @@ constexpr int64_t kTokenGroups = 512;
 // 384 windows of 1024 keys 44 us whole, 53 in two parts.
 constexpr int64_t kTokenRounds = 3, kTokenChunk = 24;
 
+}  // namespace
+
 // How the tokens kernel cuts the keys of a call into parts, given what workspace there is.
 TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
-                     size_t workspace_bytes) {
+                     size_t workspace_bytes, bool ragged) {
     const int64_t group = Hq / Hkv, pairs = B * Hkv, blocks = (max_rows * group + 15) / 16;
     const int64_t keys = dtype != APPROXIFER_F32 || Dh <= 64 ? 32 : 16;
     int64_t tiles = (max_len + keys - 1) / keys;
@@ -39,7 +41,7 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     int64_t parts = kTokenGroups / (pairs * blocks > 0 ? pairs * blocks : 1);
     parts = parts < (tiles + 7) / 8 ? parts : (tiles + 7) / 8;           // two tiles a wave at least
     const int64_t groups = pairs * blocks * (parts > 1 ? parts : 1), places = (groups + kTokenGroups - 1) / kTokenGroups * kTokenGroups;
-    if (groups * 7 < places * 6) {
+    if (ragged || groups * 7 < places * 6) {
         int64_t more = (kTokenRounds * kTokenGroups + pairs * blocks - 1) / (pairs * blocks > 0 ? pairs * blocks : 1);
         more = more < tiles / kTokenChunk ? more : tiles / kTokenChunk;
         parts = parts > more ? parts : more;
@@ -59,6 +61,8 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
     g.parts = static_cast<int>((tiles + g.chunk - 1) / g.chunk);
     return g;
 }
+
+namespace {
 
 // Into how many parts the tiles kernel cuts the keys of `heads` tiles of rows and cache heads.  A part takes `tile_us` a tile of 64 keys, all of
 // them at once as long as the GPU has room; the parts of a row are written and read again at 4.5 bytes a ps, and joined by a launch of

@@ -1,13 +1,15 @@
 // The weights that attention gave, added up per key: mass[j] += sum over rows and heads of exp2(c S - base) / total.
 //
-// A row's weights need its total, so this comes behind attention, which leaves every row's maximum and total.  Scores are formed again, the
-// other way round than there: a wave holds 64 keys (32 of long heads) as operands in registers and the rows of their sequence come by
-// in tiles of 32 through LDS, so that D = Q K^T has a key's scores in one lane and the one 32 lanes away, and a key's sum is formed where
-// its scores are.  Each workgroup has 4 such waves, a range of the cache's heads, and a part of the rows; where there is more than one
-// workgroup to a key, the sums meet in the workspace and are added in order, so that results do not depend on who came first.
+// A row's weights need its total, so this comes behind attention, which leaves every row's maximum and total.  For few rows it leaves the
+// scores, too: 4 bytes for a key and head next to the 4 Dh and more that the key and its value are, and not read from memory
+// again.  For many rows they are formed again, the other way round than there: a wave holds 64 keys (32 of long heads) as operands in
+// registers and the rows of their sequence come by in tiles through LDS, so that D = Q K^T has a key's scores in one lane and the one 32
+// lanes away, and a key's sum is formed where its scores are.  Each workgroup has 4 such waves, a range of the cache's heads, and a
+// part of the rows; where there is more than one workgroup to a key, the sums meet in the workspace and are added in order, so that
+// results do not depend on who came first.
 #pragma once
 
-#include "attend_pieces.h"
+#include "attend_tokens.h"
 
 namespace approxifer {
 
@@ -22,7 +24,7 @@ struct MassShape {
     static constexpr int kWaves = 4;
     static constexpr int kOwn = 32 * kCols;                              // keys of a wave
     static constexpr int kKeys = kOwn * kWaves;
-    static constexpr int kRows = 32;
+    static constexpr int kRows = kPieces <= 16 ? 64 : 32;                // of a tile
     static constexpr int kLoads = (kRows * kPieces + 255) / 256;         // pieces of a tile of rows that a thread brings
     static constexpr int kTile = kRows * kStride * 16;
 };
@@ -39,8 +41,8 @@ constexpr int64_t kMassBlocks = 1 << 20;                      // of a launch: mo
 
 // What a tile's rows need besides themselves.
 struct MassRows {
-    float base[32], inverse[32];
-    int place[32];
+    float base[64], inverse[64];
+    int place[64];
 };
 
 // One block of keys of a sequence, for one range of heads and part of the rows.
@@ -64,9 +66,9 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
     int to = rows.n;
     if (c.window > 0 && j0 >= c.sinks)
         to = static_cast<int>(min(static_cast<int64_t>(to), static_cast<int64_t>(j0) + S::kKeys - 1 + c.window - before));
-    const int64_t first = static_cast<int64_t>(from) * group, count = max(to - from, 0) * static_cast<int64_t>(group);
-    const int64_t all = (count + S::kRows - 1) / S::kRows;
-    const int64_t begin = all * part / g.parts, end = all * (part + 1) / g.parts;
+    const int first = from * group, count = max(to - from, 0) * group;           // T Hq is at most 2^30
+    const int all = (count + S::kRows - 1) / S::kRows;
+    const int begin = static_cast<int>(static_cast<int64_t>(all) * part / g.parts), end = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / g.parts);
 
     const int mine = j0 + wave * S::kOwn + col;               // this lane's keys: this one and, 32 behind it, another
     const int shift = c.seq.page_shift, in_page = (1 << shift) - 1;
@@ -98,25 +100,25 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
         v4i q_next[S::kLoads];
         float base_next = 0.0f, inverse_next = 0.0f;
         int place_next = -1;
-        const auto load = [&](int64_t tile) {
+        const auto load = [&](int tile) {
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) {
                 const int index = n * 256 + threadIdx.x;
-                const int64_t row = first + tile * S::kRows + index / S::kPieces;
+                const unsigned row = first + tile * S::kRows + index / S::kPieces;
                 q_next[n] = v4i{0, 0, 0, 0};
-                if (index < S::kRows * S::kPieces && row < first + count) {
-                    const int64_t t = rows.start + row / group;
-                    const V *x = static_cast<const V *>(c.q) + t * c.q_stride + (h * group + row % group) * static_cast<int64_t>(c.Dh);
+                if (index < S::kRows * S::kPieces && row < static_cast<unsigned>(first + count)) {
+                    const unsigned token = row / static_cast<unsigned>(group), g = row - token * group;
+                    const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + (h * group + g) * static_cast<int64_t>(c.Dh);
                     q_next[n] = query_piece<E>(x, index % S::kPieces * S::kPerPiece, Dq, whole_pieces, flip);
                 }
             }
             if (threadIdx.x < S::kRows) {
-                const int64_t row = first + tile * S::kRows + threadIdx.x;
+                const unsigned row = first + tile * S::kRows + threadIdx.x;
                 place_next = -1;
                 base_next = inverse_next = 0.0f;
-                if (row < first + count) {
-                    const int token = static_cast<int>(row / group);
-                    const float *x = c.stats + 2 * ((rows.start + token) * c.Hq + h * group + static_cast<int>(row % group));
+                if (row < static_cast<unsigned>(first + count)) {
+                    const unsigned token = row / static_cast<unsigned>(group);
+                    const float *x = c.stats + 2 * ((rows.start + token) * c.Hq + h * group + row - token * group);
                     base_next = x[0];
                     inverse_next = x[1];
                     place_next = rows.place(token);
@@ -139,11 +141,13 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
         load(begin);
         put(0);
         __syncthreads();
-        for (int64_t tile = begin; tile < end; ++tile) {
-            const int now = static_cast<int>(tile - begin) & 1;
+        for (int tile = begin; tile < end; ++tile) {
+            const int now = (tile - begin) & 1;
             if (tile + 1 < end) load(tile + 1);
             const char *const qt = tiles[now];
             const MassRows &info = infos[now];
+#pragma unroll 1
+            for (int r0 = 0; r0 < S::kRows; r0 += 32) {       // 32 of its rows
             v16f s[S::kCols];
 #pragma unroll
             for (int n = 0; n < S::kCols; ++n)
@@ -151,17 +155,18 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
                 for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
 #pragma unroll
             for (int p = 0; p < S::kSteps; ++p) {
-                const v4i x = *reinterpret_cast<const v4i *>(qt + piece_at<S::kStride>(col, 2 * p + half));
+                const v4i x = *reinterpret_cast<const v4i *>(qt + piece_at<S::kStride>(r0 + col, 2 * p + half));
 #pragma unroll
                 for (int n = 0; n < S::kCols; ++n) s[n] = multiply<E>(x, k[n][p], s[n]);
             }
-            const int p0 = info.place[0], p1 = info.place[S::kRows - 1];         // -1 where rows end within the tile
+            const int p0 = info.place[r0], p1 = info.place[r0 + 31];             // -1 where rows end within them
             const int j = j0 + wave * S::kOwn;
+            if (p0 < j && p1 >= 0 && p1 < j) continue;        // none sees a key of this wave's
             float of_tile[S::kCols] = {};
             const bool whole = j + S::kOwn - 1 <= p0 && p1 >= 0 && (c.window == 0 || j > p1 - c.window || j + S::kOwn <= c.sinks);
 #pragma unroll
             for (int e = 0; e < 16; e += 4) {
-                const int r = 2 * e + 4 * half;               // rows r .. r + 3
+                const int r = r0 + 2 * e + 4 * half;          // rows r .. r + 3
                 const v4f base = *reinterpret_cast<const v4f *>(info.base + r), inverse = *reinterpret_cast<const v4f *>(info.inverse + r);
                 const v4i place = *reinterpret_cast<const v4i *>(info.place + r);
 #pragma unroll
@@ -180,6 +185,7 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
             }
 #pragma unroll
             for (int n = 0; n < S::kCols; ++n) of_head[n] += of_tile[n];
+            }
             if (tile + 1 < end) put(now ^ 1);
             __syncthreads();
         }
@@ -228,6 +234,35 @@ hipError_t launch_mass_of(const AttendCall &c, const MassGrid &g, float *mass, i
     return launch_mass<E, 256, false>(c, g, mass, mass_stride, sums, stream);
 }
 
+// ---- few rows: from the scores that attention has kept
+template <class E, int DP, bool kWhole, bool kSmall>
+__global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_scores_kernel(AttendCall c, TokenGrid g, float *workspace) {
+    attend_tokens<E, DP, kWhole, kSmall, false, true>(c, g, workspace, SharedCall{});
+}
+template <class E, int DP, bool kWhole, bool kSmall>
+hipError_t launch_scores(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
+    return launch_kernel(attend_scores_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(token_blocks(c, g))), dim3(256), 0, stream, c, g,
+                         workspace);
+}
+template <class E, bool kSmall>
+hipError_t launch_scores_of(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
+    if (c.Dh == 64) return launch_scores<E, 64, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 128) return launch_scores<E, 128, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh == 256) return launch_scores<E, 256, true, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 64) return launch_scores<E, 64, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 96) return launch_scores<E, 96, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh < 128) return launch_scores<E, 128, false, kSmall>(c, g, workspace, stream);
+    if (c.Dh <= 192) return launch_scores<E, 192, false, kSmall>(c, g, workspace, stream);
+    return launch_scores<E, 256, false, kSmall>(c, g, workspace, stream);
+}
+template <class E>
+hipError_t launch_scores_of(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
+    return c.seq.page_shift >= 4 ? launch_scores_of<E, false>(c, g, workspace, stream) : launch_scores_of<E, true>(c, g, workspace, stream);
+}
+
+hipError_t launch_scores_f32(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
+hipError_t launch_scores_f16(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
+hipError_t launch_scores_bf16(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
 hipError_t launch_mass_f32(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, hipStream_t stream);
 hipError_t launch_mass_f16(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, hipStream_t stream);
 hipError_t launch_mass_bf16(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, hipStream_t stream);

@@ -23,6 +23,15 @@ MassGrid mass_grid(int64_t B, int Hq, int Hkv, int64_t max_rows, int64_t max_len
 }
 
 constexpr int64_t kAddBlocks = 1 << 20;
+constexpr int kRowsAhead = 4;                                 // of scores that a lane has on their way
+
+// Scores of few rows are kept where they fit into this many bytes; more is formed again.
+constexpr int64_t kMostScores = int64_t{1} << 31;
+int64_t score_stride(int64_t max_len) { return (max_len + 255) / 256 * 256; }
+int64_t score_bytes(int64_t T, int Hq, int64_t max_len) { return T * Hq * score_stride(max_len) * 4; }
+size_t parts_bytes(const TokenGrid &g, int Dh) {
+    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(16, Dh) * 4 + 256;
+}
 
 // A thread for every key: the slices' sums in their order.
 __global__ __launch_bounds__(256) void add_slices_kernel(AttendCall c, MassGrid g, float *mass, int64_t mass_stride, const float *sums) {
@@ -32,9 +41,68 @@ __global__ __launch_bounds__(256) void add_slices_kernel(AttendCall c, MassGrid 
         const int b = static_cast<int>(index % c.seq.B), j = static_cast<int>(index / c.seq.B) * 256 + threadIdx.x;
         const Rows rows = rows_of(c.seq, b);
         if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j >= rows.length) continue;
+        const int64_t step = c.seq.B * g.stride;
+        const float *from = sums + b * g.stride + j;
+        const int slices = g.slices();
         float x = 0.0f;
-        for (int s = 0; s < g.slices(); ++s) x += sums[(static_cast<int64_t>(s) * c.seq.B + b) * g.stride + j];
+        int s = 0;
+        for (; s + 8 <= slices; s += 8, from += 8 * step) {
+            float y[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) y[k] = from[k * step];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x += y[k];
+        }
+        for (; s < slices; ++s, from += step) x += *from;
         mass[b * mass_stride + j] += x;
+    }
+}
+
+// 256 keys of a sequence, 4 to a lane; four waves have its rows and heads in turn, and add their sums in order.
+__global__ __launch_bounds__(256) void mass_of_scores_kernel(AttendCall c, float *mass, int64_t mass_stride, int64_t blocks) {
+    __shared__ v4f sums[4][kWave];
+    const float scale = fabsf(c.scale) * 1.44269504088896340736f;
+    const int lane = lane_id(), wave = wave_id();
+    const int64_t work = blocks * c.seq.B;
+    for (int64_t index = blockIdx.x; index < work; index += gridDim.x) {
+        const int b = static_cast<int>(index % c.seq.B), j = static_cast<int>(index / c.seq.B) * 256 + 4 * lane;
+        const Rows rows = rows_of(c.seq, b);
+        if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j - 4 * lane >= rows.length) continue;
+        const float *const scores = c.scores + rows.start * c.Hq * c.score_stride + j, *const stats = c.stats + 2 * rows.start * c.Hq;
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < rows.n; ++i) {
+            const Visible see(c.window, c.sinks, rows.place(i));
+            bool sees[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sees[k] = see.sees(j + k);
+            if (!__any(sees[0] || sees[1] || sees[2] || sees[3])) continue;      // what nobody has looked at has no scores
+            for (int h0 = wave; h0 < c.Hq; h0 += 4 * kRowsAhead) {
+                v4f s[kRowsAhead];
+                v2f of_row[kRowsAhead];
+#pragma unroll
+                for (int a = 0; a < kRowsAhead; ++a) {
+                    const int64_t row = static_cast<int64_t>(i) * c.Hq + min(h0 + 4 * a, c.Hq - 1);
+                    of_row[a] = *reinterpret_cast<const v2f *>(stats + 2 * row);
+                    s[a] = *reinterpret_cast<const v4f *>(scores + (j < c.score_stride ? row * c.score_stride : 0));
+                }
+#pragma unroll
+                for (int a = 0; a < kRowsAhead; ++a)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float w = __builtin_amdgcn_exp2f(fmaf(s[a][k], scale, -of_row[a][0])) * of_row[a][1];
+                        sum[k] += sees[k] && h0 + 4 * a < c.Hq ? w : 0.0f;
+                    }
+            }
+        }
+        sums[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0) {
+            sum = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (j + k < rows.length) mass[b * mass_stride + j + k] += sum[k];
+        }
+        __syncthreads();
     }
 }
 
@@ -44,8 +112,13 @@ size_t attend_mass_least_bytes(int64_t T, int Hq) { return static_cast<size_t>(s
 
 size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                                    int64_t window, int64_t sinks) {
+    constexpr size_t kAll = static_cast<size_t>(1) << 60;
+    max_rows = max_rows < T ? max_rows : T;
+    if (few_rows(B, Hq, Hkv, max_rows, dtype) && score_bytes(T, Hq, max_len) <= kMostScores)
+        return static_cast<size_t>(stats_bytes(T, Hq) + score_bytes(T, Hq, max_len)) +
+               parts_bytes(token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll, true), Dh);
     const size_t parts = attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
-    const MassGrid g = mass_grid(B, Hq, Hkv, max_rows < T ? max_rows : T, max_len, static_cast<size_t>(1) << 60);
+    const MassGrid g = mass_grid(B, Hq, Hkv, max_rows, max_len, kAll);
     const size_t sums = g.slices() < 2 ? 0 : static_cast<size_t>(g.slices()) * B * g.stride * 4;
     return static_cast<size_t>(stats_bytes(T, Hq)) + (parts > sums ? parts : sums);
 }
@@ -56,6 +129,26 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
     const size_t stats = static_cast<size_t>(stats_bytes(c.seq.T, c.Hq)), room = workspace_bytes > stats ? workspace_bytes - stats : 0;
     c.stats = static_cast<float *>(workspace);
     float *const sums = c.stats + stats / 4;
+    const int64_t scores = score_bytes(c.seq.T, c.Hq, c.max_len);
+    if (few_rows(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.dtype) && c.max_rows > 0 && c.max_len > 0 && scores <= kMostScores &&
+        static_cast<size_t>(scores) <= room) {
+        c.scores = sums;
+        c.score_stride = score_stride(c.max_len);
+        float *const parts = sums + scores / 4;
+        const TokenGrid g = token_grid(c.seq.B, c.Hq, c.Hkv, c.Dh, c.dtype, c.max_rows, c.max_len, c.window, c.sinks, room - scores, true);
+        hipError_t e = c.dtype == APPROXIFER_F32   ? launch_scores_f32(c, g, parts, stream)
+                       : c.dtype == APPROXIFER_F16 ? launch_scores_f16(c, g, parts, stream)
+                                                   : launch_scores_bf16(c, g, parts, stream);
+        if (e == hipSuccess)
+            e = c.dtype == APPROXIFER_F32   ? join_tokens_f32(c, g, parts, stream)
+                : c.dtype == APPROXIFER_F16 ? join_tokens_f16(c, g, parts, stream)
+                                            : join_tokens_bf16(c, g, parts, stream);
+        const int64_t blocks = (c.max_len + 255) / 256, work = blocks * c.seq.B;
+        if (e == hipSuccess)
+            e = launch_kernel(mass_of_scores_kernel, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(256), 0, stream, c,
+                              mass, mass_stride, blocks);
+        return launch_status(e);
+    }
     const int rc = launch_attend(c, sums, room, stream);
     if (rc != APPROXIFER_OK || c.max_rows == 0 || c.max_len == 0) return rc;
     const MassGrid g = mass_grid(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.max_len, room);

@@ -6,4 +6,8 @@ hipError_t launch_mass_f16(const AttendCall &c, const MassGrid &g, float *mass, 
     return launch_mass_of<F16>(c, g, mass, mass_stride, sums, stream);
 }
 
+hipError_t launch_scores_f16(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
+    return launch_scores_of<F16>(c, g, workspace, stream);
+}
+
 }  // namespace approxifer

@@ -39,8 +39,9 @@ struct TokenGrid {
     __device__ __forceinline__ int chunk_of(int steps) const { return parts == 1 ? 0x7fffffff : max(chunk, (steps + parts - 1) / parts); }
 };
 
-// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.  kShared: as in attend_tiles().
-template <class E, int DP, bool kWhole, bool kSmall, bool kShared>
+// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.  kShared: as in attend_tiles().  kScores: scores are
+// kept, those of hidden keys as -infinity.
+template <class E, int DP, bool kWhole, bool kSmall, bool kShared, bool kScores = false>
 __device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, const SharedCall &shared) {
     typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
@@ -211,6 +212,11 @@ __device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGr
                     if (off >> key & 1) s[b][k] = NAN;
                     s[b][k] = sees ? s[b][k] : -INFINITY;
                 }
+        }
+        if (kScores && first + row16 < row_count) {
+            float *const to = c.scores + ((start + token) * c.Hq + head) * c.score_stride + j0 + 4 * quarter;
+#pragma unroll
+            for (int b = 0; b < S::kBlocks; ++b) *reinterpret_cast<v4f *>(to + 16 * b) = s[b];
         }
         float most = s[0][0];
 #pragma unroll
@@ -388,21 +394,33 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall c, TokenGri
                             n, (keys.steps + chunk - 1) / chunk);
 }
 
+inline int64_t token_blocks(const AttendCall &c, const TokenGrid &g) {
+    return static_cast<int64_t>(g.pairs) * g.parts * g.blocks + (c.status != nullptr ? (c.seq.B + 3) / 4 : 0);
+}
+
+template <class E, int DP>
+hipError_t join_tokens(const AttendCall &c, const TokenGrid &g, const float *workspace, hipStream_t stream) {
+    const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * g.rows;
+    const bool many = g.parts > 8;
+    if (g.parts < 2) return hipSuccess;
+    return launch_kernel(many ? attend_join_kernel<E, DP, 4> : attend_join_kernel<E, DP, 1>,
+                         dim3(static_cast<unsigned>(many ? all : (all + 3) / 4)), dim3(256), 0, stream, c, g, workspace);
+}
+template <class E>
+hipError_t join_tokens_of(const AttendCall &c, const TokenGrid &g, const float *workspace, hipStream_t stream) {
+    if (c.Dh <= 64) return join_tokens<E, 64>(c, g, workspace, stream);
+    if (c.Dh <= 96) return join_tokens<E, 96>(c, g, workspace, stream);
+    if (c.Dh <= 128) return join_tokens<E, 128>(c, g, workspace, stream);
+    if (c.Dh <= 192) return join_tokens<E, 192>(c, g, workspace, stream);
+    return join_tokens<E, 256>(c, g, workspace, stream);
+}
+
 template <class E, int DP, bool kWhole, bool kSmall>
 hipError_t launch_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {
-    typedef TokenShape<E, DP> S;
-    const int64_t work = static_cast<int64_t>(g.pairs) * g.parts * g.blocks;
-    const int64_t blocks = work + (c.status != nullptr ? (c.seq.B + S::kWaves - 1) / S::kWaves : 0);
+    const int64_t blocks = token_blocks(c, g);
     if (blocks == 0) return hipSuccess;                       // max_rows is 0: nothing but statuses is written
-    hipError_t e = launch_kernel(attend_tokens_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
-    if (e == hipSuccess && g.parts > 1) {
-        const int64_t all = static_cast<int64_t>(g.pairs) * g.blocks * g.rows;
-        const bool many = g.parts > 8;
-        e = launch_kernel(many ? attend_join_kernel<E, DP, 4> : attend_join_kernel<E, DP, 1>,
-                          dim3(static_cast<unsigned>(many ? all : (all + 3) / 4)), dim3(256), 0, stream, c, g,
-                          static_cast<const float *>(workspace));
-    }
-    return e;
+    const hipError_t e = launch_kernel(attend_tokens_kernel<E, DP, kWhole, kSmall>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, c, g, workspace);
+    return e == hipSuccess ? join_tokens<E, DP>(c, g, workspace, stream) : e;
 }
 
 template <class E, bool kSmall>
@@ -421,6 +439,13 @@ hipError_t launch_tokens_of(const AttendCall &c, const TokenGrid &g, float *work
     return c.seq.page_shift >= 4 ? launch_tokens_of<E, false>(c, g, workspace, stream) : launch_tokens_of<E, true>(c, g, workspace, stream);
 }
 
+hipError_t join_tokens_f32(const AttendCall &c, const TokenGrid &g, const float *workspace, hipStream_t stream);
+hipError_t join_tokens_f16(const AttendCall &c, const TokenGrid &g, const float *workspace, hipStream_t stream);
+hipError_t join_tokens_bf16(const AttendCall &c, const TokenGrid &g, const float *workspace, hipStream_t stream);
+// How the keys of calls of few rows are cut; ragged: for sequences of very different lengths.
+bool few_rows(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype);
+TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, int64_t window, int64_t sinks,
+                     size_t workspace_bytes, bool ragged = false);
 hipError_t launch_tokens_f32(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
 hipError_t launch_tokens_f16(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);
 hipError_t launch_tokens_bf16(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream);

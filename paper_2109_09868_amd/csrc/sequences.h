@@ -101,6 +101,8 @@ struct AttendCall {
     int max_rows, max_len, window, sinks;                     // window: 0 no limit
     float scale;
     float *stats = nullptr;                                   // [T][Hq][2], or null: of every row what RowStats says
+    float *scores = nullptr;                                  // [T][Hq][score_stride]: q . k of every key that is looked at, if they are kept
+    int64_t score_stride = 0;
 };
 // Of a row that attention has settled: what its weights are relative to (of c S, base 2), and the inverse of their sum.
 struct RowStats {
