@@ -2,7 +2,7 @@
 //
 // A row's weights need its total, so this comes behind attention, which leaves every row's maximum and total.  For few rows it leaves the
 // scores, too: 4 bytes for a key and head next to the 4 Dh and more that the key and its value are, and not read from memory
-// again.  For many rows they are formed again, the other way round than there: a wave holds 64 keys (32 of long heads) as operands in
+// again.  For many rows they are formed again, the other way round than there: a wave holds 32 keys as operands in
 // registers and the rows of their sequence come by in tiles through LDS, so that D = Q K^T has a key's scores in one lane and the one 32
 // lanes away, and a key's sum is formed where its scores are.  Each workgroup has 4 such waves, a range of the cache's heads, and a
 // part of the rows; where there is more than one workgroup to a key, the sums meet in the workspace and are added in order, so that
@@ -20,218 +20,250 @@ struct MassShape {
     static constexpr int kPieces = DP * kSize / 16;
     static constexpr int kStride = pow2_at_least(kPieces);
     static constexpr int kSteps = kPieces / 2;                           // products per block of scores
-    static constexpr int kCols = kSteps <= 8 ? 2 : 1;                    // blocks of 32 keys that a wave holds
     static constexpr int kWaves = 4;
-    static constexpr int kOwn = 32 * kCols;                              // keys of a wave
+    static constexpr int kThreads = kWaves * kWave;
+    static constexpr int kOwn = 32;                                      // keys of a wave
     static constexpr int kKeys = kOwn * kWaves;
-    static constexpr int kRows = kPieces <= 16 ? 64 : 32;                // of a tile
-    static constexpr int kLoads = (kRows * kPieces + 255) / 256;         // pieces of a tile of rows that a thread brings
+    static constexpr int kRows = kStride <= 16 ? 64 : 32;               // of a tile
+    static constexpr int kLoads = (kRows * kPieces + kThreads - 1) / kThreads;       // pieces of a tile of rows that a thread brings
     static constexpr int kTile = kRows * kStride * 16;
+    static constexpr int kAhead = kSteps % 4 == 0 ? 4 : 2;               // operands that are read at a time
 };
 
-// blocks: blocks of keys of the longest sequence; heads, parts: workgroups to a block's heads of the cache, and to its rows.
+// blocks: blocks of keys of the longest sequence; heads: workgroups to a block's heads of the cache; parts: at most as many to the tiles of
+// each of them, `chunk` to one.
 struct MassGrid {
     int64_t blocks;
-    int heads, parts;
+    int heads, parts, chunk;
+    int keys, rows;                                           // of a block, and tokens of a tile
     int64_t stride;                                           // of a sequence's sums in the workspace
     __host__ __device__ __forceinline__ int slices() const { return heads * parts; }
 };
-constexpr int kMassKeys = 256;                                // keys of a block are this or half of it
-constexpr int64_t kMassBlocks = 1 << 20;                      // of a launch: more blocks are taken in turn
+// The new tokens of a sequence that see a key of the block at j0, from..to - 1: those from the first key's place on; with a window, as far
+// as it reaches from the last one.
+struct MassTokens {
+    int from, to;
+    __device__ __forceinline__ MassTokens(const AttendCall &c, const MassGrid &g, const Rows &rows, int j0) {
+        const int before = rows.length - rows.n;              // places of tokens that are not new (negative: rows without a place)
+        from = max(max(0, -before), j0 - before);
+        to = rows.n;
+        if (c.window > 0 && j0 >= c.sinks)
+            to = static_cast<int>(min(static_cast<int64_t>(to), static_cast<int64_t>(j0) + g.keys - 1 + c.window - before));
+    }
+    // tiles of one head; of all heads of a group, one head's after the other's, and the parts that they make
+    __device__ __forceinline__ int tiles(const MassGrid &g) const { return to > from ? (to - from + g.rows - 1) / g.rows : 0; }
+    __device__ __forceinline__ int parts(const AttendCall &c, const MassGrid &g) const {
+        return max((tiles(g) * (c.Hq / c.Hkv) + g.chunk - 1) / g.chunk, 1);
+    }
+};
+constexpr int kMassBlocks = 4096;                             // of sequences and of keys in a launch: more are taken in turn
 
 // What a tile's rows need besides themselves.
 struct MassRows {
-    float base[64], inverse[64];
-    int place[64];
+    float base[128], inverse[128];
+    int place[128];
 };
 
-// One block of keys of a sequence, for one range of heads and part of the rows.
-template <class E, int DP, bool kWhole>
-__device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, int64_t index,
-                                           char (&tiles)[2][MassShape<E, DP>::kTile], MassRows (&infos)[2]) {
+// One block of keys of a sequence, for one range of heads and part of the rows.  kAligned: queries are at multiples of 16 bytes, a
+// tile's rows within 2^31 elements, and the scale is above 0; rows of whole heads then go straight from memory into LDS.
+template <class E, int DP, bool kWhole, bool kAligned>
+__device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, int slice, int b, int j0) {
     typedef typename E::Value V;
     typedef MassShape<E, DP> S;
+    // two objects, not one of two parts: reads of one do not wait for what is on its way into the other
+    __shared__ __align__(16) char tile0[S::kTile], tile1[S::kTile];
+    __shared__ __align__(16) MassRows info0, info1;
+    constexpr bool kDirect = kWhole && kAligned && S::kStride == S::kPieces && S::kRows * S::kPieces % S::kThreads == 0;
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, col = lane & 31;
-    const int slices = g.slices(), slice = static_cast<int>(index % slices);
-    const int b = static_cast<int>(index / slices % c.seq.B), j0 = static_cast<int>(index / slices / c.seq.B) * S::kKeys;
     const Rows rows = rows_of(c.seq, b);
     if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j0 >= rows.length) return;
-    const int group = c.Hq / c.Hkv, head_part = slice / g.parts, part = slice % g.parts;
-    const int h0 = static_cast<int>(static_cast<int64_t>(head_part) * c.Hkv / g.heads);
-    const int h1 = static_cast<int>(static_cast<int64_t>(head_part + 1) * c.Hkv / g.heads);
+    const MassTokens tokens(c, g, rows, j0);
+    // heads next to each other: a head keeps its XCD where there are 8 of them, and the parts that there are come before the others
+    const int group = c.Hq / c.Hkv, head_part = slice % g.heads, part = slice / g.heads;
+    if (part > 0 && part >= tokens.parts(c, g)) return;
+    const int h0 = head_part * c.Hkv / g.heads, h1 = (head_part + 1) * c.Hkv / g.heads;
+    const int tiles = tokens.tiles(g), begin = part * g.chunk, end = min(begin + g.chunk, tiles * group);
 
-    // tokens that see any of these keys: those from the first key's place on; with a window, as far as it reaches from the last one
-    const int before = rows.length - rows.n;                  // places of tokens that are not new (negative: rows without a place)
-    const int from = max(max(0, -before), j0 - before);
-    int to = rows.n;
-    if (c.window > 0 && j0 >= c.sinks)
-        to = static_cast<int>(min(static_cast<int64_t>(to), static_cast<int64_t>(j0) + S::kKeys - 1 + c.window - before));
-    const int first = from * group, count = max(to - from, 0) * group;           // T Hq is at most 2^30
-    const int all = (count + S::kRows - 1) / S::kRows;
-    const int begin = static_cast<int>(static_cast<int64_t>(all) * part / g.parts), end = static_cast<int>(static_cast<int64_t>(all) * (part + 1) / g.parts);
-
-    const int mine = j0 + wave * S::kOwn + col;               // this lane's keys: this one and, 32 behind it, another
+    const int mine = j0 + wave * S::kOwn + col;               // this lane's key
     const int shift = c.seq.page_shift, in_page = (1 << shift) - 1;
-    int64_t at[S::kCols];
-#pragma unroll
-    for (int n = 0; n < S::kCols; ++n) {
-        const int j = mine + 32 * n, page = j < rows.length ? page_of(c.seq, b, j) : -1;
-        at[n] = page < 0 ? -1 : (static_cast<int64_t>(page) * c.Hkv * (in_page + 1) + (j & in_page)) * c.Dh;
-    }
+    const int page = mine < rows.length ? page_of(c.seq, b, mine) : -1;
+    const int64_t at = page < 0 ? 0 : (static_cast<int64_t>(page) * c.Hkv * (in_page + 1) + (mine & in_page)) * c.Dh;
     const float scale = c.scale == 0.0f ? 1.0f : fabsf(c.scale) * 1.44269504088896340736f;
     const unsigned flip = c.scale < 0.0f ? (S::kSize == 4 ? 0x80000000u : 0x80008000u) : 0u;
     const bool whole_pieces = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % S::kPerPiece == 0;
     const int Dq = c.scale == 0.0f ? 0 : kWhole ? DP : c.Dh;  // scale 0: scores of 0 at scale 1
 
-    float sum[S::kCols] = {};
+    // A thread's pieces of a tile.  LDS takes what goes straight there one lane's 16 bytes behind the other's: each lane asks for the piece
+    // that the row's permutation has there.
+    const int piece0 = kDirect ? wave * S::kLoads * kWave + lane : static_cast<int>(threadIdx.x);
+    constexpr int kPieceStep = kDirect ? kWave : S::kThreads;
+    const auto row_of = [&](int n) { return (piece0 + n * kPieceStep) / S::kPieces; };
+    const auto column_of = [&](int n) {
+        const int piece = (piece0 + n * kPieceStep) % S::kPieces;
+        return (kDirect ? piece ^ permuted<S::kStride>(row_of(n)) : piece) * S::kPerPiece;
+    };
+    float sum = 0.0f;
     for (int h = h0; h < h1 && begin < end; ++h) {
-        float of_head[S::kCols] = {};                         // sums of sums: a rounding step is one of the few that there are at each level
-        v4i k[S::kCols][S::kSteps];
+        float of_head = 0.0f;                                 // sums of sums: a rounding step is one of the few that there are at each level
+        const V *const keys = static_cast<const V *>(c.k_pool) + at + static_cast<int64_t>(h) * (in_page + 1) * c.Dh;
+        v4i k[S::kSteps];
 #pragma unroll
-        for (int n = 0; n < S::kCols; ++n)
-#pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) {
-                const int d = (2 * s + half) * S::kPerPiece;
-                k[n][s] = v4i{0, 0, 0, 0};                    // behind the head, behind the sequence, or on no page
-                if (at[n] >= 0 && (kWhole || d < c.Dh))
-                    k[n][s] = *reinterpret_cast<const v4i *>(static_cast<const V *>(c.k_pool) + at[n] +
-                                                             static_cast<int64_t>(h) * (in_page + 1) * c.Dh + d);
-            }
+        for (int s = 0; s < S::kSteps; ++s) {
+            const int d = (2 * s + half) * S::kPerPiece;
+            const bool there = kWhole || d < c.Dh;            // behind the head: zeros
+            // (a key behind the sequence, or on no page, is whatever there is: its sum is not kept, or no number)
+            k[s] = *reinterpret_cast<const v4i *>(keys + (there ? d : 0));
+            if (!kWhole && !there) k[s] = v4i{0, 0, 0, 0};
+        }
         v4i q_next[S::kLoads];
-        float base_next = 0.0f, inverse_next = 0.0f;
+        v2f stats_next = {0.0f, 0.0f};                        // not looked at before all else of the tile is on its way
         int place_next = -1;
-        const auto load = [&](int tile) {
+        const V *const queries = static_cast<const V *>(c.q) + (rows.start + tokens.from) * c.q_stride + static_cast<int64_t>(h) * group * c.Dh;
+        int next_head = begin / max(tiles, 1), next_tile = begin - next_head * tiles;      // of what load() brings next
+        const auto load = [&](auto second) {
+            char *const to = second ? tile1 : tile0;
+            const V *const x = queries + next_tile * (S::kRows * c.q_stride) + next_head * c.Dh;
+            const int last = tokens.to - tokens.from - 1 - next_tile * S::kRows;           // rows behind it stand where it stands
 #pragma unroll
             for (int n = 0; n < S::kLoads; ++n) {
-                const int index = n * 256 + threadIdx.x;
-                const unsigned row = first + tile * S::kRows + index / S::kPieces;
-                q_next[n] = v4i{0, 0, 0, 0};
-                if (index < S::kRows * S::kPieces && row < static_cast<unsigned>(first + count)) {
-                    const unsigned token = row / static_cast<unsigned>(group), g = row - token * group;
-                    const V *x = static_cast<const V *>(c.q) + (rows.start + token) * c.q_stride + (h * group + g) * static_cast<int64_t>(c.Dh);
-                    q_next[n] = query_piece<E>(x, index % S::kPieces * S::kPerPiece, Dq, whole_pieces, flip);
+                if constexpr (kDirect) {
+                    const int at = min(row_of(n), last) * static_cast<int>(c.q_stride) + column_of(n);
+                    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(x + at),
+                                                     (__attribute__((address_space(3))) void *)(to + (wave * S::kLoads + n) * kWave * 16), 16, 0, 0);
+                } else {
+                    q_next[n] = v4i{0, 0, 0, 0};
+                    if (row_of(n) < S::kRows && row_of(n) <= last)
+                        q_next[n] = query_piece<E>(x + row_of(n) * c.q_stride, column_of(n), Dq, whole_pieces, flip);
                 }
             }
             if (threadIdx.x < S::kRows) {
-                const unsigned row = first + tile * S::kRows + threadIdx.x;
-                place_next = -1;
-                base_next = inverse_next = 0.0f;
-                if (row < static_cast<unsigned>(first + count)) {
-                    const unsigned token = row / static_cast<unsigned>(group);
-                    const float *x = c.stats + 2 * ((rows.start + token) * c.Hq + h * group + row - token * group);
-                    base_next = x[0];
-                    inverse_next = x[1];
-                    place_next = rows.place(token);
+                const int token = tokens.from + next_tile * S::kRows + min(static_cast<int>(threadIdx.x), last);
+                stats_next = *reinterpret_cast<const v2f *>(c.stats + 2 * ((h * group + next_head) * c.seq.T + rows.start + token));
+                place_next = static_cast<int>(threadIdx.x) <= last ? rows.place(token) : -1;
+            }
+            if (++next_tile == tiles) {
+                next_tile = 0;
+                ++next_head;
+            }
+        };
+        const auto put = [&](auto second) {
+            char *const to = second ? tile1 : tile0;
+            MassRows &info = second ? info1 : info0;
+            if constexpr (!kDirect) {
+#pragma unroll
+                for (int n = 0; n < S::kLoads; ++n) {
+                    if (row_of(n) < S::kRows)
+                        *reinterpret_cast<v4i *>(to + piece_at<S::kStride>(row_of(n), column_of(n) / S::kPerPiece)) = q_next[n];
                 }
             }
-        };
-        const auto put = [&](int buffer) {
-#pragma unroll
-            for (int n = 0; n < S::kLoads; ++n) {
-                const int index = n * 256 + threadIdx.x;
-                if (index < S::kRows * S::kPieces)
-                    *reinterpret_cast<v4i *>(tiles[buffer] + piece_at<S::kStride>(index / S::kPieces, index % S::kPieces)) = q_next[n];
-            }
             if (threadIdx.x < S::kRows) {
-                infos[buffer].base[threadIdx.x] = base_next;
-                infos[buffer].inverse[threadIdx.x] = inverse_next;
-                infos[buffer].place[threadIdx.x] = place_next;
+                info.base[threadIdx.x] = stats_next[0];
+                info.inverse[threadIdx.x] = stats_next[1];
+                info.place[threadIdx.x] = place_next;
             }
+            if constexpr (kDirect) __builtin_amdgcn_s_waitcnt(kNoVmem);
         };
-        load(begin);
-        put(0);
+        load(std::false_type{});
+        put(std::false_type{});
         __syncthreads();
-        for (int tile = begin; tile < end; ++tile) {
-            const int now = (tile - begin) & 1;
-            if (tile + 1 < end) load(tile + 1);
-            const char *const qt = tiles[now];
-            const MassRows &info = infos[now];
+        const auto step = [&](int tile, auto second) {
+            typedef std::integral_constant<bool, !decltype(second)::value> Other;
+            if (tile + 1 < end) load(Other{});
+            const char *const qt = second ? tile1 : tile0;
+            const MassRows &info = second ? info1 : info0;
+            const int j = j0 + wave * S::kOwn;
 #pragma unroll 1
             for (int r0 = 0; r0 < S::kRows; r0 += 32) {       // 32 of its rows
-            v16f s[S::kCols];
+                const int p0 = info.place[r0], p1 = info.place[r0 + 31];         // -1 where rows end within them
+                if (p0 < 0 || (p1 >= 0 && p1 < j)) continue;  // there are none, or none sees a key of this wave's
+                v16f s;
 #pragma unroll
-            for (int n = 0; n < S::kCols; ++n)
+                for (int e = 0; e < 16; ++e) s[e] = 0.0f;
+                // operands of the next products are on their way while these are formed: left alone, each product waits for its own
+                v4i x[2][S::kAhead];
+                const auto read = [&](int p0) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[n][e] = 0.0f;
+                    for (int p = 0; p < S::kAhead; ++p)
+                        x[p0 / S::kAhead & 1][p] = *reinterpret_cast<const v4i *>(qt + piece_at<S::kStride>(r0 + col, 2 * (p0 + p) + half));
+                };
+                read(0);
 #pragma unroll
-            for (int p = 0; p < S::kSteps; ++p) {
-                const v4i x = *reinterpret_cast<const v4i *>(qt + piece_at<S::kStride>(r0 + col, 2 * p + half));
+                for (int p0 = 0; p0 < S::kSteps; p0 += S::kAhead) {
+                    if (p0 + S::kAhead < S::kSteps) read(p0 + S::kAhead);
+                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int n = 0; n < S::kCols; ++n) s[n] = multiply<E>(x, k[n][p], s[n]);
-            }
-            const int p0 = info.place[r0], p1 = info.place[r0 + 31];             // -1 where rows end within them
-            const int j = j0 + wave * S::kOwn;
-            if (p0 < j && p1 >= 0 && p1 < j) continue;        // none sees a key of this wave's
-            float of_tile[S::kCols] = {};
-            const bool whole = j + S::kOwn - 1 <= p0 && p1 >= 0 && (c.window == 0 || j > p1 - c.window || j + S::kOwn <= c.sinks);
+                    for (int p = 0; p < S::kAhead; ++p) s = multiply<E>(x[p0 / S::kAhead & 1][p], k[p0 + p], s);
+                }
+                float of_rows = 0.0f;
+                const bool whole = j + S::kOwn - 1 <= p0 && p1 >= 0 && (c.window == 0 || j > p1 - c.window || j + S::kOwn <= c.sinks);
+                const auto add = [&](auto masked) {
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int r = r0 + 2 * e + 4 * half;          // rows r .. r + 3
-                const v4f base = *reinterpret_cast<const v4f *>(info.base + r), inverse = *reinterpret_cast<const v4f *>(info.inverse + r);
-                const v4i place = *reinterpret_cast<const v4i *>(info.place + r);
+                    for (int e = 0; e < 16; e += 4) {
+                        const int r = r0 + 2 * e + 4 * half;  // rows r .. r + 3
+                        const v4f base = *reinterpret_cast<const v4f *>(info.base + r), inverse = *reinterpret_cast<const v4f *>(info.inverse + r);
+                        v4i place = {0, 0, 0, 0};
+                        if constexpr (masked) place = *reinterpret_cast<const v4i *>(info.place + r);
 #pragma unroll
-                for (int n = 0; n < S::kCols; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float w = __builtin_amdgcn_exp2f(fmaf(s[n][e + i], scale, -base[i]));
-                        if (whole) {
-                            of_tile[n] = fmaf(w, inverse[i], of_tile[n]);
-                        } else {
-                            const int key = mine + 32 * n;
-                            const bool sees = key <= place[i] && (c.window == 0 || key > place[i] - c.window || key < c.sinks);
-                            of_tile[n] += sees ? w * inverse[i] : 0.0f;
+                        for (int i = 0; i < 4; ++i) {
+                            float score = s[e + i], share = inverse[i];
+                            if constexpr (masked) {           // a row that is no number must not reach what it does not see either
+                                const bool sees = mine <= place[i] && (c.window == 0 || mine > place[i] - c.window || mine < c.sinks);
+                                score = sees ? score : -INFINITY;
+                                share = sees ? share : 0.0f;
+                            }
+                            of_rows = fmaf(__builtin_amdgcn_exp2f(fmaf(score, scale, -base[i])), share, of_rows);
                         }
                     }
+                };
+                if (whole) add(std::false_type{});
+                else add(std::true_type{});
+                of_head += of_rows;
             }
-#pragma unroll
-            for (int n = 0; n < S::kCols; ++n) of_head[n] += of_tile[n];
-            }
-            if (tile + 1 < end) put(now ^ 1);
+            if (tile + 1 < end) put(Other{});
             __syncthreads();
+        };
+        for (int tile = begin; tile < end; tile += 2) {
+            step(tile, std::false_type{});
+            if (tile + 1 < end) step(tile + 1, std::true_type{});
         }
-#pragma unroll
-        for (int n = 0; n < S::kCols; ++n) sum[n] += of_head[n];
+        sum += of_head;
     }
-#pragma unroll
-    for (int n = 0; n < S::kCols; ++n) {
-        const float x = half_sum(sum[n]);
-        const int j = mine + 32 * n;
-        if (half != 0 || j >= rows.length) continue;
-        if (slices == 1) mass[b * mass_stride + j] += x;
-        else sums[(static_cast<int64_t>(slice) * c.seq.B + b) * g.stride + j] = x;
-    }
+    sum = half_sum(sum);
+    if (half != 0 || mine >= rows.length) return;
+    if (g.slices() == 1) mass[b * mass_stride + mine] += sum;
+    else sums[(static_cast<int64_t>(slice) * c.seq.B + b) * g.stride + mine] = sum;
 }
 
-template <class E, int DP, bool kWhole>
-__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 16 ? 1 : 2)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
+template <class E, int DP, bool kWhole, bool kAligned>
+__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
                                                                                                   int64_t mass_stride, float *sums) {
     typedef MassShape<E, DP> S;
-    __shared__ __align__(16) char tiles[2][S::kTile];
-    __shared__ __align__(16) MassRows infos[2];
-    const int64_t work = g.blocks * (kMassKeys / S::kKeys) * c.seq.B * g.slices();
-    for (int64_t index = blockIdx.x; index < work; index += gridDim.x)
-        mass_block<E, DP, kWhole>(c, g, mass, mass_stride, sums, index, tiles, infos);
+    for (int64_t block = blockIdx.z; block < g.blocks; block += gridDim.z)
+        for (int b = blockIdx.y; b < c.seq.B; b += gridDim.y)
+            mass_block<E, DP, kWhole, kAligned>(c, g, mass, mass_stride, sums, blockIdx.x, b, static_cast<int>(block * S::kKeys));
 }
 
-template <class E, int DP, bool kWhole>
+template <class E, int DP, bool kWhole, bool kAligned>
 hipError_t launch_mass(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, hipStream_t stream) {
     typedef MassShape<E, DP> S;
-    static_assert(S::kKeys == kMassKeys || S::kKeys == kMassKeys / 2, "keys of a block");
-    const int64_t blocks = g.blocks * (kMassKeys / S::kKeys) * c.seq.B * g.slices();
-    return launch_kernel(attend_mass_kernel<E, DP, kWhole>, dim3(static_cast<unsigned>(blocks < kMassBlocks ? blocks : kMassBlocks)), dim3(256),
-                         0, stream, c, g, mass, mass_stride, sums);
+    if (g.keys != S::kKeys || g.rows != S::kRows) return hipErrorInvalidValue;   // mass_grid() says otherwise than MassShape
+    const dim3 grid(g.slices(), c.seq.B < kMassBlocks ? c.seq.B : kMassBlocks,
+                    static_cast<unsigned>(g.blocks < kMassBlocks ? g.blocks : kMassBlocks));
+    return launch_kernel(attend_mass_kernel<E, DP, kWhole, kAligned>, grid, dim3(S::kThreads), 0, stream, c, g, mass, mass_stride, sums);
 }
 
 template <class E>
 hipError_t launch_mass_of(const AttendCall &c, const MassGrid &g, float *mass, int64_t mass_stride, float *sums, hipStream_t stream) {
-    if (c.Dh == 64) return launch_mass<E, 64, true>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh == 128) return launch_mass<E, 128, true>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh == 256) return launch_mass<E, 256, true>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh < 64) return launch_mass<E, 64, false>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh <= 96) return launch_mass<E, 96, false>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh < 128) return launch_mass<E, 128, false>(c, g, mass, mass_stride, sums, stream);
-    if (c.Dh <= 192) return launch_mass<E, 192, false>(c, g, mass, mass_stride, sums, stream);
-    return launch_mass<E, 256, false>(c, g, mass, mass_stride, sums, stream);
+    const bool aligned = reinterpret_cast<uintptr_t>(c.q) % 16 == 0 && c.q_stride % (16 / sizeof(typename E::Value)) == 0 &&
+                         c.q_stride < 1 << 24 && c.scale > 0.0f;
+    if (c.Dh == 64 && aligned) return launch_mass<E, 64, true, true>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh == 128 && aligned) return launch_mass<E, 128, true, true>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh == 256 && aligned) return launch_mass<E, 256, true, true>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh <= 64) return launch_mass<E, 64, false, false>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh <= 96) return launch_mass<E, 96, false, false>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh <= 128) return launch_mass<E, 128, false, false>(c, g, mass, mass_stride, sums, stream);
+    if (c.Dh <= 192) return launch_mass<E, 192, false, false>(c, g, mass, mass_stride, sums, stream);
+    return launch_mass<E, 256, false, false>(c, g, mass, mass_stride, sums, stream);
 }
 
 // ---- few rows: from the scores that attention has kept

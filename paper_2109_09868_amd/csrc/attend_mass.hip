@@ -5,20 +5,30 @@ namespace approxifer {
 
 namespace {
 
+constexpr int64_t kMassGroups = 4096;
 int64_t stats_bytes(int64_t T, int Hq) { return (T * Hq * 8 + 255) / 256 * 256; }
 
-// Workgroups to a block of keys: its heads first, then its rows, until there are four for every CU or a part has no more than four tiles.
-MassGrid mass_grid(int64_t B, int Hq, int Hkv, int64_t max_rows, int64_t max_len, size_t room) {
+// As many workgroups as take three times what the GPU holds, where there are the tiles for it: first a block's heads are dealt out, then the
+// tiles of a head, the same number to each workgroup (keys that come first are seen by more rows).
+MassGrid mass_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len, size_t room) {
+    const int bytes = (Dh <= 64 ? 64 : Dh <= 96 ? 96 : Dh <= 128 ? 128 : Dh <= 192 ? 192 : 256) * (dtype == APPROXIFER_F32 ? 4 : 2);
     MassGrid g;
-    g.blocks = (max_len + kMassKeys - 1) / kMassKeys;
-    g.stride = g.blocks * kMassKeys;
-    const int64_t blocks = g.blocks * B, want = (1024 + blocks - 1) / (blocks > 0 ? blocks : 1);
-    const int64_t tiles = (max_rows * (Hq / Hkv) + 31) / 32;
+    g.keys = 128;                                             // as MassShape has it
+    g.rows = bytes <= 256 ? 64 : 32;
+    g.blocks = (max_len + g.keys - 1) / g.keys;
+    g.stride = g.blocks * g.keys;
+    const int64_t blocks = g.blocks * B, tiles = (max_rows + g.rows - 1) / g.rows * (Hq / Hkv);
     const int64_t most = static_cast<int64_t>(room / (static_cast<size_t>(B > 0 ? B : 1) * (g.stride > 0 ? g.stride : 1) * 4));
-    const int64_t slices = want < most ? want : most;
-    g.heads = static_cast<int>(slices < 1 ? 1 : slices < Hkv ? slices : Hkv);
-    int64_t parts = slices / Hkv < (tiles + 3) / 4 ? slices / Hkv : (tiles + 3) / 4;
-    g.parts = static_cast<int>(parts < 1 ? 1 : parts);
+    int64_t heads = (kMassGroups + blocks - 1) / (blocks > 0 ? blocks : 1);
+    heads = heads < Hkv ? heads : Hkv;
+    g.heads = static_cast<int>(heads < 1 || most < heads ? 1 : heads);
+    int64_t chunk = blocks * Hkv * tiles / kMassGroups;
+    chunk = chunk > 4 ? chunk : 4;
+    const int64_t parts = most / g.heads;
+    if (g.heads * parts < 2) chunk = tiles;
+    else if ((tiles + chunk - 1) / chunk > parts) chunk = (tiles + parts - 1) / parts;
+    g.chunk = static_cast<int>(chunk < tiles ? chunk : tiles > 0 ? tiles : 1);
+    g.parts = static_cast<int>(tiles > 0 ? (tiles + g.chunk - 1) / g.chunk : 1);
     return g;
 }
 
@@ -33,28 +43,34 @@ size_t parts_bytes(const TokenGrid &g, int Dh) {
     return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(16, Dh) * 4 + 256;
 }
 
-// A thread for every key: the slices' sums in their order.
-__global__ __launch_bounds__(256) void add_slices_kernel(AttendCall c, MassGrid g, float *mass, int64_t mass_stride, const float *sums) {
+// A block of keys: four threads to each, with a quarter of the slices' sums, and those in their order.
+__global__ __launch_bounds__(512) void add_slices_kernel(AttendCall c, MassGrid g, float *mass, int64_t mass_stride, const float *sums) {
+    __shared__ float quarters[4][128];
     const int64_t work = g.blocks * c.seq.B;
-    static_assert(kMassKeys == 256, "a thread for every key of a block");
+    const int quarter = threadIdx.x >> 7, key = threadIdx.x & 127;
     for (int64_t index = blockIdx.x; index < work; index += gridDim.x) {
-        const int b = static_cast<int>(index % c.seq.B), j = static_cast<int>(index / c.seq.B) * 256 + threadIdx.x;
+        const int b = static_cast<int>(index % c.seq.B), j0 = static_cast<int>(index / c.seq.B) * g.keys, j = j0 + key;
         const Rows rows = rows_of(c.seq, b);
-        if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j >= rows.length) continue;
+        if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j0 >= rows.length) continue;
         const int64_t step = c.seq.B * g.stride;
-        const float *from = sums + b * g.stride + j;
-        const int slices = g.slices();
+        const int parts = MassTokens(c, g, rows, j0).parts(c, g), all = g.heads * parts;
+        const int begin = all * quarter / 4, end = all * (quarter + 1) / 4;
         float x = 0.0f;
-        int s = 0;
-        for (; s + 8 <= slices; s += 8, from += 8 * step) {
+        for (int n0 = begin; n0 < end; n0 += 8) {             // eight of them on their way at a time
             float y[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) y[k] = from[k * step];
+            for (int k = 0; k < 8; ++k) {
+                const int n = min(n0 + k, end - 1);
+                y[k] = sums[n * step + b * g.stride + j];
+            }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x += y[k];
+            for (int k = 0; k < 8; ++k) x += n0 + k < end ? y[k] : 0.0f;
         }
-        for (; s < slices; ++s, from += step) x += *from;
-        mass[b * mass_stride + j] += x;
+        quarters[quarter][key] = x;
+        __syncthreads();
+        if (quarter == 0 && j < rows.length)
+            mass[b * mass_stride + j] += ((x + quarters[1][key]) + quarters[2][key]) + quarters[3][key];
+        __syncthreads();
     }
 }
 
@@ -68,7 +84,7 @@ __global__ __launch_bounds__(256) void mass_of_scores_kernel(AttendCall c, float
         const int b = static_cast<int>(index % c.seq.B), j = static_cast<int>(index / c.seq.B) * 256 + 4 * lane;
         const Rows rows = rows_of(c.seq, b);
         if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j - 4 * lane >= rows.length) continue;
-        const float *const scores = c.scores + rows.start * c.Hq * c.score_stride + j, *const stats = c.stats + 2 * rows.start * c.Hq;
+        const float *const scores = c.scores + rows.start * c.Hq * c.score_stride + j, *const stats = c.stats + 2 * rows.start;
         v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int i = 0; i < rows.n; ++i) {
             const Visible see(c.window, c.sinks, rows.place(i));
@@ -81,8 +97,9 @@ __global__ __launch_bounds__(256) void mass_of_scores_kernel(AttendCall c, float
                 v2f of_row[kRowsAhead];
 #pragma unroll
                 for (int a = 0; a < kRowsAhead; ++a) {
-                    const int64_t row = static_cast<int64_t>(i) * c.Hq + min(h0 + 4 * a, c.Hq - 1);
-                    of_row[a] = *reinterpret_cast<const v2f *>(stats + 2 * row);
+                    const int h = min(h0 + 4 * a, c.Hq - 1);
+                    const int64_t row = static_cast<int64_t>(i) * c.Hq + h;
+                    of_row[a] = *reinterpret_cast<const v2f *>(stats + 2 * (h * c.seq.T + i));
                     s[a] = *reinterpret_cast<const v4f *>(scores + (j < c.score_stride ? row * c.score_stride : 0));
                 }
 #pragma unroll
@@ -118,7 +135,7 @@ size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh
         return static_cast<size_t>(stats_bytes(T, Hq) + score_bytes(T, Hq, max_len)) +
                parts_bytes(token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll, true), Dh);
     const size_t parts = attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
-    const MassGrid g = mass_grid(B, Hq, Hkv, max_rows, max_len, kAll);
+    const MassGrid g = mass_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, kAll);
     const size_t sums = g.slices() < 2 ? 0 : static_cast<size_t>(g.slices()) * B * g.stride * 4;
     return static_cast<size_t>(stats_bytes(T, Hq)) + (parts > sums ? parts : sums);
 }
@@ -151,13 +168,13 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
     }
     const int rc = launch_attend(c, sums, room, stream);
     if (rc != APPROXIFER_OK || c.max_rows == 0 || c.max_len == 0) return rc;
-    const MassGrid g = mass_grid(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.max_len, room);
+    const MassGrid g = mass_grid(c.seq.B, c.Hq, c.Hkv, c.Dh, c.dtype, c.max_rows, c.max_len, room);
     hipError_t e = c.dtype == APPROXIFER_F32   ? launch_mass_f32(c, g, mass, mass_stride, sums, stream)
                    : c.dtype == APPROXIFER_F16 ? launch_mass_f16(c, g, mass, mass_stride, sums, stream)
                                                : launch_mass_bf16(c, g, mass, mass_stride, sums, stream);
     if (e == hipSuccess && g.slices() > 1) {
         const int64_t work = g.blocks * c.seq.B;
-        e = launch_kernel(add_slices_kernel, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(256), 0, stream, c, g,
+        e = launch_kernel(add_slices_kernel, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(512), 0, stream, c, g,
                           mass, mass_stride, static_cast<const float *>(sums));
     }
     return launch_status(e);

@@ -12,6 +12,9 @@ typedef short v8s __attribute__((ext_vector_type(8)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
+constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
+constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
+
 // D += A B of 16-byte pieces: A [32 x 2 pieces], B [2 pieces x 32]; lane l has row (column) l % 32 and piece l / 32.
 template <class E>
 __device__ __forceinline__ v16f multiply(v4i a, v4i b, v16f d);

@@ -22,8 +22,6 @@
 
 namespace approxifer {
 
-constexpr int kMfma = 0x8, kDsRead = 0x100;                   // of sched_group_barrier
-constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
 
 // slots: tiles of rows of all sequences (single: one for each); parts: workgroups that share a tile's keys, `chunk` tiles of 64 each or
 // as many more as it takes.

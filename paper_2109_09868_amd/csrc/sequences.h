@@ -100,7 +100,7 @@ struct AttendCall {
     int32_t *status;
     int max_rows, max_len, window, sinks;                     // window: 0 no limit
     float scale;
-    float *stats = nullptr;                                   // [T][Hq][2], or null: of every row what RowStats says
+    float *stats = nullptr;                                   // [Hq][T][2], or null: of every row what RowStats says
     float *scores = nullptr;                                  // [T][Hq][score_stride]: q . k of every key that is looked at, if they are kept
     int64_t score_stride = 0;
 };
@@ -110,7 +110,7 @@ struct RowStats {
     __device__ __forceinline__ RowStats(float top, float total)
         : base(top == -INFINITY ? 0.0f : top), inverse(total == 0.0f ? 0.0f : 1.0f / total) {}
     __device__ __forceinline__ void store(const AttendCall &c, int64_t t, int head) const {
-        float *const at = c.stats + 2 * (t * c.Hq + head);
+        float *const at = c.stats + 2 * (head * c.seq.T + t);
         at[0] = base;
         at[1] = inverse;
     }
