@@ -190,7 +190,6 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
 #pragma unroll
                 for (int p0 = 0; p0 < S::kSteps; p0 += S::kAhead) {
                     if (p0 + S::kAhead < S::kSteps) read(p0 + S::kAhead);
-                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int p = 0; p < S::kAhead; ++p) s = multiply<E>(x[p0 / S::kAhead & 1][p], k[p0 + p], s);
                 }
@@ -235,7 +234,7 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
 }
 
 template <class E, int DP, bool kWhole, bool kAligned>
-__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
+__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 16 ? 1 : MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
                                                                                                   int64_t mass_stride, float *sums) {
     typedef MassShape<E, DP> S;
     for (int64_t block = blockIdx.z; block < g.blocks; block += gridDim.z)

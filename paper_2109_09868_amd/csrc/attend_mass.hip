@@ -5,7 +5,7 @@ namespace approxifer {
 
 namespace {
 
-constexpr int64_t kMassGroups = 4096;
+constexpr int64_t kMassGroups = 8192;
 int64_t stats_bytes(int64_t T, int Hq) { return (T * Hq * 8 + 255) / 256 * 256; }
 
 // As many workgroups as take three times what the GPU holds, where there are the tiles for it: first a block's heads are dealt out, then the
