@@ -268,7 +268,8 @@ hipError_t launch_mass_of(const AttendCall &c, const MassGrid &g, float *mass, i
 // ---- few rows: from the scores that attention has kept
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_scores_kernel(AttendCall c, TokenGrid g, float *workspace) {
-    attend_tokens<E, DP, kWhole, kSmall, false, true>(c, g, workspace, SharedCall{});
+    __shared__ __align__(16) char lds[TokenShape<E, DP>::kLds];
+    attend_tokens<E, DP, kWhole, kSmall, false, true>(c, g, workspace, SharedCall{}, 0, lds);
 }
 template <class E, int DP, bool kWhole, bool kSmall>
 hipError_t launch_scores(const AttendCall &c, const TokenGrid &g, float *workspace, hipStream_t stream) {

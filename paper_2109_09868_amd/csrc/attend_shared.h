@@ -30,6 +30,9 @@ struct SharedCall {
     }
 };
 
+// Whether there is an instance of both kernels in one: of heads for which two of its workgroups share a CU.
+inline bool shared_both(int Dh, int dtype, int page_shift) { return (Dh == 64 || (Dh == 128 && dtype != APPROXIFER_F32)) && page_shift >= 4; }
+
 // The last k of 0..n-1 with at(k) <= x, where at() rises and at(0) <= x; 64 at a time, by the whole wave.
 template <class F>
 __device__ __forceinline__ int last_at_most(int n, int64_t x, F at) {
@@ -49,39 +52,62 @@ struct SharedGroup {
     int g0, g1, length;
     bool ok;
     __device__ __forceinline__ SharedGroup(const Sequences &s, const SharedCall &shared, int c)
-        : g0(shared.groups[c]), g1(shared.groups[c + 1]), length(shared.shared[c]) {
+        : SharedGroup(s, shared, shared.groups[c], shared.groups[c + 1], shared.shared[c]) {}
+    __device__ __forceinline__ SharedGroup(const Sequences &s, const SharedCall &shared, int a, int b, int l) : g0(a), g1(b), length(l) {
         ok = g0 >= 0 && g0 <= g1 && g1 <= s.B && length >= 0 && length <= shared.max_shared;
     }
 };
 
+// The first 64 groups, one to a lane: asked for early, so that a search waits for no load of its own.
+struct GroupLanes {
+    int g0, g1, length;
+    __device__ __forceinline__ explicit GroupLanes(const SharedCall &shared) {
+        const int k = min(lane_id(), shared.C - 1);
+        g0 = shared.groups[k];
+        g1 = shared.groups[k + 1];
+        length = shared.shared[k];
+    }
+};
+
 // How many of sequence b's first places are its group's: 0 without a group that can be used.
-__device__ __forceinline__ int shared_length(const Sequences &s, const SharedCall &shared, int b, int *group = nullptr) {
+__device__ __forceinline__ int shared_length(const Sequences &s, const SharedCall &shared, const GroupLanes &lanes, int b, int *group = nullptr) {
+    if (shared.C <= kWave) {
+        const unsigned long long in = __ballot(lane_id() < shared.C && lanes.g0 <= b && b < lanes.g1);
+        if (in == 0) return 0;
+        const int k = __ffsll(in) - 1, length = __builtin_amdgcn_readlane(lanes.length, k);
+        if (group != nullptr) *group = k;
+        return __builtin_amdgcn_readlane(lanes.g0, k) >= 0 && __builtin_amdgcn_readlane(lanes.g1, k) <= s.B && length >= 0 && length <= shared.max_shared
+                   ? length
+                   : 0;
+    }
     const int c = last_at_most(shared.C, b, [&](int k) { return static_cast<int64_t>(shared.groups[k]); });
     const SharedGroup g(s, shared, c);
-    const bool in = b >= g.g0 && b < g.g1;
     if (group != nullptr) *group = c;
-    return in && g.ok ? g.length : 0;
+    return b >= g.g0 && b < g.g1 && g.ok ? g.length : 0;
 }
 
 // The sequence of a group that its common places are read from, the first that holds them all, or the longest; and how many it holds.
-__device__ __forceinline__ int shared_leader(const AttendCall &c, const SharedGroup &g, int *length) {
+// lens: those of the group's first 64 sequences, one to a lane.
+__device__ __forceinline__ int shared_leader(const AttendCall &c, int g0, int g1, int shared_length, int lens, int *length) {
     const int64_t room = static_cast<int64_t>(c.seq.M) << c.seq.page_shift;
-    int best = -1, leader = g.g0;
-    for (int i0 = g.g0; i0 < g.g1; i0 += kWave) {
+    int best = -1, leader = g0;
+    for (int i0 = g0; i0 < g1; i0 += kWave) {
         const int i = i0 + lane_id();
-        int l = i < g.g1 ? c.seq.lens[i] : -1;
+        int l = i >= g1 ? -1 : i0 == g0 ? lens : c.seq.lens[i];
         if (l > room || l > c.max_len) l = -1;
-        int most = min(l, g.length);
+        l = min(l, shared_length);
+        int most = l;
         for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o));
         if (most > best) {
             best = most;
-            leader = i0 + __ffsll(__ballot(min(l, g.length) == most)) - 1;
+            leader = i0 + __ffsll(__ballot(l == most)) - 1;
         }
-        if (best == g.length) break;
+        if (best == shared_length) break;
     }
     *length = max(best, 0);
     return leader;
 }
+__device__ __forceinline__ int shared_lens(const AttendCall &c, int g0, int g1) { return c.seq.lens[min(g0 + lane_id(), g1 - 1)]; }
 
 // What a workgroup does: rows (tokens times heads) from token `start` on, of which it has block `block`, and keys low..end-1 of sequence b.
 struct SharedUnit {
@@ -89,10 +115,15 @@ struct SharedUnit {
     int h, b, low, end, part, parts, chunk, sum_part;
     int g0, g1, before;                                       // common: the group's sequences; own: g0 = g1, and the place of the first token
     int64_t tokens;                                           // common: of the group
+    int length, lens;                                         // common: the shared length, and lengths of its first sequences by lane
 
     template <int kKeys>
     __device__ __forceinline__ int chunk_of(int steps) const {
         return parts == 1 ? 0x7fffffff : max(chunk / kKeys, (steps + parts - 1) / parts);
+    }
+    // of common places: whose pages they are read from, and how many there are.  (Last: places are looked up meanwhile.)
+    __device__ __forceinline__ void find_leader(const AttendCall &c) {
+        if (g0 != g1) b = shared_leader(c, g0, g1, length, lens, &end);
     }
     // the least and largest place of a wave's 16 rows
     __device__ __forceinline__ void places_of(int place, int *p0, int *p1) const {
@@ -135,6 +166,7 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const Sha
     SharedUnit u;
     u.rows = 0;
     const int group = c.Hq / c.Hkv;
+    const GroupLanes lanes(shared);
     const int64_t heads = shared.common_slots * c.Hkv, common = heads * shared.common_parts;
     if (x < common) {
         u.part = u.sum_part = static_cast<int>(x / heads);
@@ -144,18 +176,38 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const Sha
         u.h = static_cast<int>(index % c.Hkv);
         // rows of sequences that are bad may lie anywhere
         const auto row_of = [&](int b) { return min(max(static_cast<int64_t>(c.seq.starts[min(max(b, 0), c.seq.B)]), int64_t{0}), c.seq.T); };
-        const auto begin_of = [&](int k) { return row_of(shared.groups[k]) * group / R + k; };
-        const int k = last_at_most(shared.C, slot, begin_of);
-        const SharedGroup g(c.seq, shared, k);
-        if (!g.ok || g.length == 0 || g.g0 == g.g1) return u;
-        const int64_t r0 = row_of(g.g0), r1 = row_of(g.g1);
-        u.block = slot - begin_of(k);
+        int g0, g1, length;
+        int64_t r0, r1, first;                                // its rows, and the number of its first block
+        if (shared.C <= kWave) {
+            const int64_t rows0 = row_of(lanes.g0), rows1 = row_of(lanes.g1), begin = rows0 * group / R + min(lane_id(), shared.C - 1);
+            const unsigned long long before = __ballot(lane_id() < shared.C && begin <= slot);
+            const int k = before != 0 ? 63 - __clzll(before) : 0;
+            g0 = __builtin_amdgcn_readlane(lanes.g0, k);
+            g1 = __builtin_amdgcn_readlane(lanes.g1, k);
+            length = __builtin_amdgcn_readlane(lanes.length, k);
+            r0 = __builtin_amdgcn_readlane(static_cast<int>(rows0), k);       // T is at most 2^24
+            r1 = __builtin_amdgcn_readlane(static_cast<int>(rows1), k);
+            first = r0 * group / R + k;
+        } else {
+            const auto begin_of = [&](int k) { return row_of(shared.groups[k]) * group / R + k; };
+            const int k = last_at_most(shared.C, slot, begin_of);
+            g0 = shared.groups[k];
+            g1 = shared.groups[k + 1];
+            length = shared.shared[k];
+            r0 = row_of(g0);
+            r1 = row_of(g1);
+            first = begin_of(k);
+        }
+        const SharedGroup g(c.seq, shared, g0, g1, length);
+        if (!g.ok || length == 0 || g0 == g1) return u;
+        u.block = slot - first;
         if (u.block < 0 || u.block * R >= (r1 - r0) * group) return u;
-        u.b = shared_leader(c, g, &u.end);
+        u.lens = shared_lens(c, g0, g1);
+        u.length = length;
         u.start = r0;
         u.low = 0;
-        u.g0 = g.g0;
-        u.g1 = g.g1;
+        u.g0 = g0;
+        u.g1 = g1;
         u.tokens = r1 - r0;
         u.rows = u.tokens * group;
         return u;
@@ -176,7 +228,7 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const Sha
     }
     const Rows rows = rows_of(c.seq, u.b);
     if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || u.block < 0 || u.block * R >= static_cast<int64_t>(rows.n) * group) return u;
-    u.low = shared_length(c.seq, shared, u.b);
+    u.low = shared_length(c.seq, shared, lanes, u.b);
     u.start = rows.start;
     u.end = rows.length;
     u.g0 = u.g1 = u.b;
@@ -188,23 +240,27 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const Sha
 // The place of token t of a unit in its sequence; negative where there is none.
 __device__ __forceinline__ int shared_place(const AttendCall &c, const SharedUnit &u, int64_t t) {
     if (u.g0 == u.g1) return u.before + static_cast<int>(t - u.start);
-    const int32_t *const starts = c.seq.starts;
+    const int32_t *const starts = c.seq.starts, *const lens = c.seq.lens;
     // where all have as many rows, this is it
     const int64_t tokens = u.tokens;
     int b = u.g0 + static_cast<int>((t - u.start) * (u.g1 - u.g0) / (tokens > 0 ? tokens : 1));
     b = min(max(b, u.g0), u.g1 - 1);
-    if (starts[b] > t || starts[b + 1] <= t) {
+    int r0 = starts[b], r1 = starts[b + 1], length = lens[b];
+    if (r0 > t || r1 <= t) {
         int lo = u.g0, hi = u.g1;
         while (hi - lo > 1) {
             const int mid = lo + (hi - lo) / 2;
             if (starts[mid] <= t) lo = mid;
             else hi = mid;
         }
-        b = lo;
+        r0 = starts[lo];
+        r1 = starts[lo + 1];
+        length = lens[lo];
     }
-    const Rows r = rows_of(c.seq, b);
-    if (!r.ok || r.n > c.max_rows || r.length > c.max_len || t < r.start || t >= r.start + r.n) return -1;
-    return r.place(static_cast<int>(t - r.start));
+    // as rows_of() has it
+    const bool ok = r0 >= 0 && r0 <= r1 && r1 <= c.seq.T && length >= 0 && length <= (static_cast<int64_t>(c.seq.M) << c.seq.page_shift) &&
+                    r1 - r0 <= c.max_rows && length <= c.max_len && t >= r0 && t < r1;
+    return ok ? length - (r1 - r0) + static_cast<int>(t - r0) : -1;
 }
 
 // One wave: a row of a unit over tiles begin..end-1, element by element.  scratch: 256 floats of LDS.
@@ -234,13 +290,15 @@ __device__ __forceinline__ void shared_part(const AttendCall &c, const SharedCal
 // One wave: the status of sequence b.
 __device__ __forceinline__ int shared_status(const AttendCall &c, const SharedCall &shared, int b) {
     int k = 0;
-    const int length = shared_length(c.seq, shared, b, &k), st = attend_status(c, b);
+    const GroupLanes lanes(shared);
+    const int length = shared_length(c.seq, shared, lanes, b, &k), st = attend_status(c, b);
     if (st != APPROXIFER_GROUP_OK || length == 0) return st;
     const Rows r = rows_of(c.seq, b);
     if (r.n == 0) return APPROXIFER_GROUP_OK;
     // the pages that are read for it: those of its group's places that its rows see
     int there = 0;
-    const int leader = shared_leader(c, SharedGroup(c.seq, shared, k), &there);
+    const int g0 = shared.groups[k], g1 = shared.groups[k + 1];
+    const int leader = shared_leader(c, g0, g1, length, shared_lens(c, g0, g1), &there);
     const int upto = min(there, r.length);
     const Visible first(c.window, c.sinks, max(r.place(0), 0));
     return pages_status(c.seq, leader, 0, min(min(c.sinks, upto), first.from), min(first.from, upto), upto);
@@ -262,10 +320,11 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(AttendCall c, S
     }
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave_id(), t = at / c.Hq;
     if (at >= all) return;
+    const GroupLanes lanes(shared);
     const int b = last_at_most(c.seq.B, t, [&](int k) { return static_cast<int64_t>(c.seq.starts[k]); });
     const Rows rows = rows_of(c.seq, b);
     if (!rows.ok || rows.n > c.max_rows || rows.length > c.max_len || t < rows.start || t >= rows.start + rows.n) return;
-    const int first = shared_length(c.seq, shared, b) > 0 ? 0 : shared.common_parts, parts = shared.common_parts + shared.own_parts;
+    const int first = shared_length(c.seq, shared, lanes, b) > 0 ? 0 : shared.common_parts, parts = shared.common_parts + shared.own_parts;
     float top = -INFINITY, total = 0.0f, out[kPerLane] = {};
     for (int from = first; from < parts; from += kWave) {
         const int p = from + lane, count = min(parts - from, kWave);

@@ -8,12 +8,30 @@ namespace approxifer {
 
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_shared_tiles_kernel(AttendCall c, SharedCall shared) {
-    attend_tiles<E, DP, kWhole, kSmall, true>(c, TileGrid{}, nullptr, shared);
+    __shared__ __align__(16) char lds[TileShape<E, DP>::kLds];
+    attend_tiles<E, DP, kWhole, kSmall, true>(c, TileGrid{}, nullptr, shared, blockIdx.x, lds);
 }
 
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_shared_tokens_kernel(AttendCall c, SharedCall shared) {
-    attend_tokens<E, DP, kWhole, kSmall, true>(c, TokenGrid{}, nullptr, shared);
+    __shared__ __align__(16) char lds[TokenShape<E, DP>::kLds];
+    attend_tokens<E, DP, kWhole, kSmall, true>(c, TokenGrid{}, nullptr, shared, blockIdx.x, lds);
+}
+
+// Common places by tiles and own ones by tokens in one launch: the ones wait for the matrix cores, the others for memory.  Of every
+// 8 `period` workgroups the first 8 are tiles, as long as there are any: one for each XCD.
+template <class E, int DP>
+__global__ __launch_bounds__(256, 2) void attend_shared_both_kernel(AttendCall c, SharedCall shared, int tiles, int period) {
+    constexpr int kTiles = TileShape<E, DP>::kLds, kTokens = TokenShape<E, DP>::kLds;
+    __shared__ __align__(16) char lds[kTiles > kTokens ? kTiles : kTokens];
+    const int x = blockIdx.x, round = x / (8 * period), at = x - round * 8 * period, before = min(8 * round + min(at, 8), tiles);
+    if (at < 8 && 8 * round + at < tiles) {
+        shared.own_slots = 0;
+        attend_tiles<E, DP, true, false, true>(c, TileGrid{}, nullptr, shared, 8 * round + at, lds);
+    } else {
+        shared.common_slots = 0;
+        attend_tokens<E, DP, true, false, true>(c, TokenGrid{}, nullptr, shared, x - before, lds);
+    }
 }
 
 // F<E, DP, kWhole, kSmall>::run() for a call's head: as many instances as the kernels for single sequences have.
@@ -53,6 +71,19 @@ template <class E>
 hipError_t launch_shared_tokens_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
     return c.seq.page_shift >= 4 ? shared_instance<SharedTokens, E, false>(c, shared, stream)
                                  : shared_instance<SharedTokens, E, true>(c, shared, stream);
+}
+template <class E, int DP>
+hipError_t launch_shared_both(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    const int64_t tiles = shared.common_slots * shared.common_parts * c.Hkv, all = shared_blocks(c, shared);
+    const int64_t period = all / tiles;
+    return launch_kernel(attend_shared_both_kernel<E, DP>, dim3(static_cast<unsigned>(all)), dim3(256), 0, stream, c, shared,
+                         static_cast<int>(tiles), static_cast<int>(period < 1 ? 1 : period));
+}
+template <class E>
+hipError_t launch_shared_both_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
+    if constexpr (sizeof(typename E::Value) == 2)
+        if (c.Dh == 128) return launch_shared_both<E, 128>(c, shared, stream);
+    return launch_shared_both<E, 64>(c, shared, stream);
 }
 template <class E>
 hipError_t launch_shared_join_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {

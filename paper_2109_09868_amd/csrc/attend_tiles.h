@@ -78,22 +78,23 @@ __device__ __forceinline__ int slot_owner(const Sequences &s, int64_t slot, int 
 }
 
 // kWhole: Dh is DP.  kSmall: pages of fewer tokens than a wave loads of a tile.  kShared: rows are those of a group of sequences, or of one,
-// and keys the ones that the group has in common, or the others; g is then not used, and sums always meet in the workspace.
+// and keys the ones that the group has in common, or the others; workgroup `group_index` of that call has them, g is not used, and sums
+// always meet in the workspace.  lds: TileShape::kLds bytes.
 template <class E, int DP, bool kWhole, bool kSmall, bool kShared>
-__device__ __forceinline__ void attend_tiles(const AttendCall &c, const TileGrid &g, float *workspace, const SharedCall &shared) {
+__device__ __forceinline__ void attend_tiles(const AttendCall &c, const TileGrid &g, float *workspace, const SharedCall &shared, int64_t group_index,
+                                             char *lds) {
     typedef typename E::Value V;
     typedef TileShape<E, DP> S;
     constexpr bool kDirect = kWhole && !kSmall && S::kStride == S::kPieces;
     constexpr int kKeys = S::kKeys, kBlocks = kKeys / 32, kSteps = S::kPieces / 2, kOut = DP / 32;
     constexpr int kVec = S::kSize == 2 ? 1 : kOut % 4 == 0 ? 4 : kOut % 2 == 0 ? 2 : 1;
-    __shared__ __align__(16) char lds[S::kLds];
     const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(wave_id()), half = lane >> 5, row32 = lane & 31;
     const int group = c.Hq / c.Hkv;
     int part, index = 0, h, b;
     int64_t tile = 0;
     SharedUnit unit;
     if constexpr (kShared) {
-        unit = shared_unit(c, shared, blockIdx.x, S::kRows);
+        unit = shared_unit(c, shared, group_index, S::kRows);
         if (unit.rows == 0) return;
         part = unit.part;
         h = unit.h;
@@ -126,6 +127,8 @@ __device__ __forceinline__ void attend_tiles(const AttendCall &c, const TileGrid
     int place, p0, p1, w0, w1;                                // places: this row's, and the least and largest of the tile and of the wave
     if constexpr (kShared) {
         place = shared_place(c, unit, start + token);
+        unit.find_leader(c);
+        b = unit.b;
         unit.places_of(place, S::kWaves, reinterpret_cast<int *>(lds), &p0, &p1, &w0, &w1);
     } else {
         place = rows.place(token);
@@ -468,7 +471,8 @@ __device__ __forceinline__ void attend_tiles(const AttendCall &c, const TileGrid
 
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_tiles_kernel(AttendCall c, TileGrid g, float *workspace) {
-    attend_tiles<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{});
+    __shared__ __align__(16) char lds[TileShape<E, DP>::kLds];
+    attend_tiles<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{}, 0, lds);
 }
 
 template <class E, int DP, int kWaves>

@@ -29,6 +29,7 @@ struct TokenShape {
     static constexpr int kTile = kKeys * kStride * 16;
     static constexpr int kOutBytes = kRows * DP * 4;                     // a wave's sums, when the waves meet
     static constexpr int kBytes = kTile > kOutBytes ? kTile : kOutBytes;
+    static constexpr int kLds = kWaves * kBytes;
     static_assert(kPieces % 4 == 0 && kKeys * kPieces % kWave == 0, "whole pieces per lane");
 };
 
@@ -39,14 +40,14 @@ struct TokenGrid {
     __device__ __forceinline__ int chunk_of(int steps) const { return parts == 1 ? 0x7fffffff : max(chunk, (steps + parts - 1) / parts); }
 };
 
-// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.  kShared: as in attend_tiles().  kScores: scores are
+// kWhole: Dh is DP.  kSmall: pages of fewer than 16 tokens.  kShared: as in attend_tiles().  lds: TokenShape::kLds bytes.  kScores: scores are
 // kept, those of hidden keys as -infinity.
 template <class E, int DP, bool kWhole, bool kSmall, bool kShared, bool kScores = false>
-__device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, const SharedCall &shared) {
+__device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGrid &g, float *workspace, const SharedCall &shared,
+                                              int64_t group_index, char *lds) {
     typedef typename E::Value V;
     typedef TokenShape<E, DP> S;
     constexpr int kKeys = S::kKeys, kOut = DP / 16;
-    __shared__ __align__(16) char lds[S::kWaves * S::kBytes];
     __shared__ float tops[S::kWaves][16], totals[S::kWaves][16];
     __shared__ int dirty;
     const int lane = lane_id(), wave = wave_id(), quarter = lane >> 4, row16 = lane & 15;
@@ -54,7 +55,7 @@ __device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGr
     int part, h, b, pair = 0, block = 0;
     SharedUnit unit;
     if constexpr (kShared) {
-        unit = shared_unit(c, shared, blockIdx.x, S::kRows);
+        unit = shared_unit(c, shared, group_index, S::kRows);
         if (unit.rows == 0) return;
         part = unit.part;
         h = unit.h;
@@ -87,6 +88,8 @@ __device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGr
     int place, p0, p1;                                        // places: this row's, and the least and largest of the block
     if constexpr (kShared) {
         place = shared_place(c, unit, start + token);
+        unit.find_leader(c);
+        b = unit.b;
         unit.places_of(place, &p0, &p1);
     } else {
         place = rows.place(token);
@@ -369,7 +372,8 @@ __device__ __forceinline__ void attend_tokens(const AttendCall &c, const TokenGr
 
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_tokens_kernel(AttendCall c, TokenGrid g, float *workspace) {
-    attend_tokens<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{});
+    __shared__ __align__(16) char lds[TokenShape<E, DP>::kLds];
+    attend_tokens<E, DP, kWhole, kSmall, false>(c, g, workspace, SharedCall{}, 0, lds);
 }
 
 template <class E, int DP, int kWaves>
