@@ -123,7 +123,10 @@ struct SharedUnit {
     }
     // of common places: whose pages they are read from, and how many there are.  (Last: places are looked up meanwhile.)
     __device__ __forceinline__ void find_leader(const AttendCall &c) {
-        if (g0 != g1) b = shared_leader(c, g0, g1, length, lens, &end);
+        if (g0 != g1) {
+            b = __builtin_amdgcn_readfirstlane(shared_leader(c, g0, g1, length, lens, &end));
+            end = __builtin_amdgcn_readfirstlane(end);
+        }
     }
     // the least and largest place of a wave's 16 rows
     __device__ __forceinline__ void places_of(int place, int *p0, int *p1) const {
@@ -161,10 +164,8 @@ struct SharedUnit {
     }
 };
 
-// The unit of workgroup x, R rows a block; rows = 0: none.
-__device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const SharedCall &shared, int64_t x, int R) {
-    SharedUnit u;
-    u.rows = 0;
+__device__ __forceinline__ SharedUnit shared_unit_of(const AttendCall &c, const SharedCall &shared, int64_t x, int R) {
+    SharedUnit u{};
     const int group = c.Hq / c.Hkv;
     const GroupLanes lanes(shared);
     const int64_t heads = shared.common_slots * c.Hkv, common = heads * shared.common_parts;
@@ -234,6 +235,29 @@ __device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const Sha
     u.g0 = u.g1 = u.b;
     u.before = rows.length - rows.n;
     u.rows = static_cast<int64_t>(rows.n) * group;
+    return u;
+}
+
+// The unit of workgroup x, R rows a block; rows = 0: none.  All of it is the workgroup's, which the compiler cannot know: loops and addresses
+// that depend on what is not known to be are kept by lanes, and their loads wait one for the other.
+__device__ __forceinline__ SharedUnit shared_unit(const AttendCall &c, const SharedCall &shared, int64_t x, int R) {
+    SharedUnit u = shared_unit_of(c, shared, x, R);
+    const auto same = [](auto &v) { v = __builtin_amdgcn_readfirstlane(static_cast<int>(v)); };       // T is at most 2^24, T Hq 2^30
+    same(u.rows);
+    if (u.rows == 0) return u;
+    same(u.start);
+    same(u.block);
+    same(u.h);
+    same(u.b);
+    same(u.low);
+    same(u.end);
+    same(u.part);
+    same(u.sum_part);
+    same(u.g0);
+    same(u.g1);
+    same(u.before);
+    same(u.tokens);
+    same(u.length);
     return u;
 }
 

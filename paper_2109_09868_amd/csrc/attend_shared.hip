@@ -45,10 +45,10 @@ SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh,
     s.single = rows <= r;
     s.common_slots = T * group / R + C;
     s.own_slots = s.single ? B : T * group / r + B;
-    // parts: as many as fill the GPU once, of two tiles a wave at least, as far as writing and joining them costs less than it gives
+    // parts: as many as fill the GPU once, of a tile a wave or two of a workgroup's at least, as far as writing and joining them costs less than it gives
     const auto cut = [&](bool tiles, int64_t units, int64_t keys, int *chunk) {
         const int64_t places = !tiles ? 512 : Dh > 128 || (wide && Dh > 64) ? 256 : wide ? 768 : 512;
-        int64_t parts = least(places / (units > 0 ? units : 1), (keys + 255) / 256);
+        int64_t parts = least(places / (units > 0 ? units : 1), (keys + 127) / 128);
         if (tiles) {
             const double tile_us = Dh * (!wide ? 0.0086 : Dh > 64 ? 0.0625 : 0.053), part_us = static_cast<double>(T) * Hq * Dh * 8.0 / 4.5e6;
             parts = least(parts, static_cast<int64_t>(std::sqrt(keys / 64.0 * tile_us / part_us) + 0.5));
