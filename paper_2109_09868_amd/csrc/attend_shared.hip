@@ -26,8 +26,6 @@ struct SharedPlan {
     int64_t bytes;                                            // of workspace; 0: not worth it, or not possible
 };
 
-constexpr int64_t kShareGpu = 512;                            // workgroups that the GPU holds at a time
-
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
 
 SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
@@ -100,9 +98,7 @@ int launch_attend_shared(const AttendCall &c, const int32_t *groups, const int32
     hipError_t e = hipSuccess;
     if (p.common_tiles == p.own_tiles) {
         e = run(p.own_tiles, s);
-    } else if (p.common_tiles && shared_both(c.Dh, c.dtype, c.seq.page_shift) && s.own_slots * c.Hkv * s.own_parts <= kShareGpu) {
-        // 200 sequences behind 16 prompts (400 workgroups with their own keys) 33 us instead of 45; but 192 sequences of 8 heads (1536
-        // workgroups) 156 instead of 97: where either fills the GPU they only take places from each other
+    } else if (p.common_tiles && shared_both(c.Dh, c.dtype, c.seq.page_shift)) {
         e = c.dtype == APPROXIFER_F32   ? launch_shared_both_f32(c, s, stream)
             : c.dtype == APPROXIFER_F16 ? launch_shared_both_f16(c, s, stream)
                                         : launch_shared_both_bf16(c, s, stream);

@@ -18,19 +18,20 @@ __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_shared_tokens_
     attend_tokens<E, DP, kWhole, kSmall, true>(c, TokenGrid{}, nullptr, shared, blockIdx.x, lds);
 }
 
-// Common places by tiles and own ones by tokens in one launch: the ones wait for the matrix cores, the others for memory.  Of every
-// 8 `period` workgroups the first 8 are tiles, as long as there are any: one for each XCD.
+// Common places by tiles and own ones by tokens in one launch, the tiles first: they are fewer and take longer, and the others go where they
+// leave room.  192 sequences behind 8003 tokens (8 heads of 128, bf16) 94 us, in two launches 48 and 51, and 156 with tiles dealt out among
+// the others; 200 behind 16 prompts (2 heads of 128, fp16) 32 us, in two launches 28 and 17.
 template <class E, int DP>
-__global__ __launch_bounds__(256, 2) void attend_shared_both_kernel(AttendCall c, SharedCall shared, int tiles, int period) {
+__global__ __launch_bounds__(256, 2) void attend_shared_both_kernel(AttendCall c, SharedCall shared, int tiles) {
     constexpr int kTiles = TileShape<E, DP>::kLds, kTokens = TokenShape<E, DP>::kLds;
     __shared__ __align__(16) char lds[kTiles > kTokens ? kTiles : kTokens];
-    const int x = blockIdx.x, round = x / (8 * period), at = x - round * 8 * period, before = min(8 * round + min(at, 8), tiles);
-    if (at < 8 && 8 * round + at < tiles) {
+    const int x = blockIdx.x;
+    if (x < tiles) {
         shared.own_slots = 0;
-        attend_tiles<E, DP, true, false, true>(c, TileGrid{}, nullptr, shared, 8 * round + at, lds);
+        attend_tiles<E, DP, true, false, true>(c, TileGrid{}, nullptr, shared, x, lds);
     } else {
         shared.common_slots = 0;
-        attend_tokens<E, DP, true, false, true>(c, TokenGrid{}, nullptr, shared, x - before, lds);
+        attend_tokens<E, DP, true, false, true>(c, TokenGrid{}, nullptr, shared, x - tiles, lds);
     }
 }
 
@@ -74,10 +75,8 @@ hipError_t launch_shared_tokens_of(const AttendCall &c, const SharedCall &shared
 }
 template <class E, int DP>
 hipError_t launch_shared_both(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
-    const int64_t tiles = shared.common_slots * shared.common_parts * c.Hkv, all = shared_blocks(c, shared);
-    const int64_t period = all / tiles;
-    return launch_kernel(attend_shared_both_kernel<E, DP>, dim3(static_cast<unsigned>(all)), dim3(256), 0, stream, c, shared,
-                         static_cast<int>(tiles), static_cast<int>(period < 1 ? 1 : period));
+    return launch_kernel(attend_shared_both_kernel<E, DP>, dim3(shared_blocks(c, shared)), dim3(256), 0, stream, c, shared,
+                         static_cast<int>(shared.common_slots * shared.common_parts * c.Hkv));
 }
 template <class E>
 hipError_t launch_shared_both_of(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {

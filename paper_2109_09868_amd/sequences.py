@@ -3,6 +3,7 @@
     prompt that all queries share -> one sequence -> fork to the N workers of every group
         -> coded tokens appended and attended to, one or many at a time -> predictions, decoded by the serving loop's calls
         -> sequences that ended are dropped, pages close up
+        -> sequences that have grown too long keep the tokens that were read most
 
 Every step on the cache is one call of the C ABI, and a few of torch's on the sequences' statuses.  Pools, tables and the page calls'
 workspace are allocated once, the new tokens' queries and outputs and attention's scratch with every call.  SequenceModel is a stand-in
@@ -25,10 +26,12 @@ class SequenceCache:
     reserve() or fork() said.  A sequence that was refused room has no place for the new tokens that come with the others':
     append() writes nothing of them to the pages and attend() answers zeros, until it is reserved again.  fork() changes how many
     sequences there are.
+
+    weigh: attend() adds up the weights that every token is given, over heads and layers, in mass, by which evict() chooses.
     """
 
     def __init__(self, layers, heads, kv_heads, head_dim, max_sequences, max_pages, pages, device, page=16, dtype=None, window=0, sinks=0,
-                 rotary_base=10000.0):
+                 rotary_base=10000.0, weigh=False):
         import torch
         i32 = torch.int32
         self.heads, self.kv_heads, self.head_dim, self.page = heads, kv_heads, head_dim, page
@@ -48,6 +51,9 @@ class SequenceCache:
                       for name in ("status", "refused", "whole", "_seen", "_asked")}
         self.moved = torch.empty((pages,), dtype=i32, device=device)
         self.live = torch.empty((1,), dtype=i32, device=device)
+        # mass: [sequences, places]; dropped: how many tokens evict() has taken from each sequence, None as long as it has taken none
+        self._masses = torch.zeros((max_sequences, max_pages * page), dtype=torch.float32, device=device) if weigh else None
+        self.dropped = self._common = None
         self._show(0, 0)
         need = binding.approxifer_cache_workspace_bytes(max_sequences, max_sequences, pages)
         self._workspace = torch.empty((need,), dtype=torch.uint8, device=device)
@@ -58,6 +64,7 @@ class SequenceCache:
         self.table, self.lens, self.refs = self._tables[now][:n], self._lens[now][:n], self._refs[now]
         for name, t in self._each.items():
             setattr(self, name, t[:n])
+        self.mass = None if self._masses is None else self._masses[:n]
 
     def _settle(self):
         """Whom the calls for new tokens pass by, after refused has changed."""
@@ -75,7 +82,16 @@ class SequenceCache:
         self.refs.zero_()
         self.status.zero_()
         self.refused.zero_()
+        self.dropped = self._common = None
+        if self.mass is not None:
+            self.mass.zero_()
         self._settle()
+
+    def share(self, groups, lengths):
+        """Sequences groups[c] .. groups[c + 1] - 1 have their first lengths[c] tokens in common (lists; until the next begin(), fork() or
+        evict()): attend() then reads those once for all of them."""
+        import torch
+        self._common = tuple(torch.tensor(x, dtype=torch.int32, device=self.device) for x in (groups, lengths)) + (max(lengths, default=0),)
 
     def reserve(self, add, lost=None):
         """Room for add[b] more tokens (an int32 device tensor, or a number for all) of every sequence but those where lost (an int32
@@ -106,6 +122,10 @@ class SequenceCache:
     def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
         """The new tokens' heads, normed and rotated; keys and values go to their pages.  Returns the queries."""
         import torch
+        if positions is None and self.dropped is not None:    # places have closed up, positions go on
+            t = torch.arange(q.shape[0], dtype=torch.int32, device=self.device)
+            b = torch.searchsorted(starts, t, right=True).sub_(1).clamp_(0, self.sequences - 1)
+            positions = (self._seen[b] - starts[b + 1] + t + self.dropped[b]).to(torch.int32)
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         binding.approxifer_append(q, k, v, self.pools[layer, 0], self.pools[layer, 1], self.table,
                                   self._seen, starts, self.freq, q_weight=q_weight, k_weight=k_weight, positions=positions, axis=axis,
@@ -116,12 +136,53 @@ class SequenceCache:
         """What the new tokens read in their sequences: [T, heads, head_dim]."""
         import torch
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        if self.mass is not None or self._common is not None:
+            return self._attend_more(layer, q, starts, max_rows, max_len, out)
         need = binding.approxifer_attend_workspace_bytes(q.shape[0], self.sequences, self.heads, self.kv_heads, self.head_dim, self.dtype,
                                                          max_rows, max_len, self.window, self.sinks)
         workspace = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else binding.NO_WORKSPACE
         binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self._seen, starts, max_rows, max_len,
                                   window=self.window, sinks=self.sinks, out=out, status=self.status, workspace=workspace)
         return out
+
+    def _attend_more(self, layer, q, starts, max_rows, max_len, out):
+        """attend() that adds up its weights, or reads what is common once."""
+        import torch
+        sizes = (self.heads, self.kv_heads, self.head_dim, self.dtype, max_rows, max_len)
+        k, v = self.pools[layer, 0], self.pools[layer, 1]
+        if self.mass is not None:
+            need = binding.approxifer_attend_mass_workspace_bytes(q.shape[0], self.sequences, *sizes, self.window, self.sinks)
+        else:
+            groups, lengths, longest = self._common
+            need = binding.approxifer_attend_shared_workspace_bytes(q.shape[0], self.sequences, lengths.numel(), *sizes, longest, self.window,
+                                                                    self.sinks)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=self.device) if need else binding.NO_WORKSPACE
+        if self.mass is not None:
+            binding.approxifer_attend_mass(q, k, v, self.table, self._seen, starts, self.mass, max_rows, max_len, window=self.window,
+                                           sinks=self.sinks, out=out, status=self.status, workspace=workspace)
+        else:
+            binding.approxifer_attend_shared(q, k, v, self.table, self._seen, starts, groups, lengths, max_rows, max_len, longest,
+                                             window=self.window, sinks=self.sinks, out=out, status=self.status, workspace=workspace)
+        return out
+
+    def evict(self, budget, first=0, recent=0):
+        """Sequences of more than `budget` tokens keep their `first` first and `recent` last ones and, of the others, those that were given
+        the largest weights.  status says what became of each.  Returns the places that stay [sequences, budget] int32, then -1."""
+        import torch
+        if self.mass is None:
+            raise ValueError("a cache that evicts adds up weights: weigh=True")
+        before = self.lens.clone()
+        n, i32 = self.sequences, torch.int32
+        kept = torch.empty((n, int(budget)), dtype=i32, device=self.device)
+        need = binding.approxifer_cache_evict_workspace_bytes(n, budget, self.pages, self.page)
+        binding.approxifer_cache_evict(self.pools, self.table, self.lens, self.refs, self.mass, budget, first=first, recent=recent, kept=kept,
+                                       status=self.status, workspace=torch.empty((max(need, 16),), dtype=torch.uint8, device=self.device))
+        if self.dropped is None:
+            self.dropped = torch.zeros((n,), dtype=i32, device=self.device)
+        self.dropped += before - self.lens
+        self._common = None
+        self._settle()
+        return kept
 
     def fork(self, parents, keep=None):
         """Sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens: lists or int32 device tensors.
@@ -133,10 +194,18 @@ class SequenceCache:
         if n > self.max_sequences:
             raise ValueError("at most %d sequences" % self.max_sequences)
         new = 1 - self._now
+        old = parents.clamp(min=0).long() if self.dropped is not None or self.mass is not None else None
         binding.approxifer_cache_fork(self.pools, self.table, self.lens, self.refs, parents, keep=keep,
                                       table_out=self._tables[new][:n], lens_out=self._lens[new][:n], refs_out=self._refs[new],
                                       status=self._each["status"][:n], workspace=self._workspace)
+        if self.dropped is not None:
+            self.dropped = self.dropped[old] * (parents >= 0)
+        masses = None if self.mass is None else self.mass[old]
         self._show(new, n)
+        if masses is not None:                                # a token's stays with it; places that are no longer held have none
+            held = torch.arange(masses.shape[1], device=self.device) < self.lens[:, None]
+            self.mass.copy_(masses.masked_fill_(~held, 0.0))
+        self._common = None
         self.refused.copy_(self.status)
         return self._settle()
 
@@ -192,12 +261,15 @@ class CodedSequences:
     lost [G, N] int32 holds the first status other than 0 that the cache has had for each worker's sequence: one that got no page,
     or no place in its table, misses tokens from then on.  Such a worker counts as one that never answers, so a group can
     spare S of them; a group that has lost more gets APPROXIFER_GROUP_BAD_MASK from the decoder, and values of 0.
+
+    share: the prompt is attended to once for all sequences, not once for each (a cache that weighs does not).
     """
 
-    def __init__(self, model, cache, G, K, N, S, sign_mode=binding.SIGN_SURVIVOR_RANK, nodes=None):
+    def __init__(self, model, cache, G, K, N, S, sign_mode=binding.SIGN_SURVIVOR_RANK, nodes=None, share=False):
         self.model, self.cache, self.G, self.K, self.N, self.S, self.sign_mode = model, cache, G, K, N, S, sign_mode
         self.alpha, self.beta = nodes or binding.approxifer_chebyshev_nodes(K, N)
-        self.length = 0
+        self.length = self.prompt = 0
+        self.share = share
 
     @property
     def lost(self):
@@ -211,6 +283,8 @@ class CodedSequences:
         refused = self.cache.fork(parents)
         refused.copy_(torch.where(lost == 0, refused, lost))
         self.cache._settle()
+        if self.share and self.prompt:
+            self.cache.share([0, parents.numel()], [self.prompt])
 
     def _starts(self, sequences, n):
         import torch
@@ -223,6 +297,7 @@ class CodedSequences:
         self.cache.reserve(n)
         self.model.read(self.cache, prompt, self._starts(1, n), n, n)
         self.cache.lose()
+        self.prompt = n
         self._fork([0] * (self.G * self.N))
         self.length = n
 
@@ -239,6 +314,15 @@ class CodedSequences:
         last = preds.view(G, N, n, -1)[:, :, -1].contiguous()
         mask, _ = binding.approxifer_wait_mask(torch.where(self.cache.whole.view(G, N), arrival, math.inf), N - self.S)
         return binding.approxifer_decode(last, mask, self.alpha, self.beta, self.S, self.sign_mode)
+
+    def evict(self, budget, first=0, recent=0):
+        """Every worker's sequence of more than `budget` tokens is cut to that many, each by its own weights (SequenceCache.evict()).  A
+        worker for whose sequence there were no pages is lost."""
+        kept = self.cache.evict(budget, first, recent)
+        self.cache.lose()
+        self.cache._settle()
+        self.length, self.prompt = min(self.length, budget), 0
+        return kept
 
     def finish(self, groups):
         """Drops all groups but those listed, in their order, and closes up the pages that this leaves free."""
@@ -264,6 +348,8 @@ def main():
     ap.add_argument("--tokens", type=int, default=128, help="tokens of each query")
     ap.add_argument("--steps", type=int, default=16, help="single tokens after that")
     ap.add_argument("--layers", type=int, default=2)
+    ap.add_argument("--share", action="store_true", help="read the prompt once for all sequences")
+    ap.add_argument("--keep", type=int, default=0, help="cut sequences to this many tokens when half of the single ones are there")
     args = ap.parse_args()
     dev = torch.device("cuda:0")
     G, K, S = args.groups, args.queries, args.stragglers
@@ -280,8 +366,9 @@ def main():
     more = [draw(G, K, 1, width) for _ in range(args.steps)]
 
     def serve(workers, stragglers, nodes=None):
-        cache = SequenceCache(args.layers, heads, heads, width // heads, G * workers, pages, G * workers * pages + pages, dev)
-        coded = CodedSequences(model, cache, G, K, workers, stragglers, nodes=nodes)
+        cache = SequenceCache(args.layers, heads, heads, width // heads, G * workers, pages,
+                              G * workers * pages * (2 if args.keep else 1) + pages, dev, weigh=args.keep > 0)
+        coded = CodedSequences(model, cache, G, K, workers, stragglers, nodes=nodes, share=args.share)
         _, arrival = serving.exponential_arrivals(G, workers, 3, dev)
         out = []
         torch.cuda.synchronize()
@@ -290,7 +377,9 @@ def main():
         out.append(coded.step(texts, arrival)[0])
         torch.cuda.synchronize()
         first = time.perf_counter() - t
-        for x in more:
+        for i, x in enumerate(more):
+            if args.keep and i == len(more) // 2:
+                coded.evict(args.keep, 4, args.keep // 4)
             out.append(coded.step(x, arrival)[0])
         torch.cuda.synchronize()
         rest = (time.perf_counter() - t - first) / max(args.steps, 1)
