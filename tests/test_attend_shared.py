@@ -304,3 +304,22 @@ def test_nothing_to_do_and_refusals(binding):
     assert e.value.code == -2
     out, status = binding.approxifer_attend_shared(q, kp, vp, table, lens, starts, _i([0]), _i([]), 1, 24, 20)
     assert status.tolist() == [0, 0] and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("dtype", ALL, ids=list(ref.DTYPES))
+@pytest.mark.parametrize("heads,kv", [(2, 2), (8, 1), (48, 1)])
+def test_more_groups_than_a_wave_has_lanes(binding, dtype, heads, kv):
+    # 70 groups of one to four sequences, some of them empty; sequences of one to three new tokens
+    sizes = [(3 * c) % 5 for c in range(70)]
+    groups = [sum(sizes[:c]) for c in range(71)]
+    B = groups[-1] + 3
+    own = [3 + b % 5 for b in range(B)]
+    assert B >= 2 * 70
+    _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], own, [1] * B, heads, kv, 64, 16, apart=True)
+    _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], own, [b % 3 for b in range(B)], 4, 2, 64, 16, window=20, sinks=2)
+
+
+def test_a_first_group_behind_others_rows(binding):
+    # groups that begin with the third sequence, whose rows are not the first
+    _check(binding, torch.bfloat16, [2, 12, 40], [90, 300], [1 + b for b in range(43)], [1 + (b % 2) for b in range(43)], 16, 2, 128, 16, apart=True)
+    _check(binding, torch.bfloat16, [35, 40], [300], [1 + b for b in range(43)], [1] * 43, 64, 2, 128, 16, apart=True)
