@@ -30,6 +30,9 @@ struct SharedCall {
     }
 };
 
+// Whether there is an instance of the kernel of tiles.  float32 heads of more than 64 floats and up to 128 have none: at 1024 rows it takes 245 us
+// for 233.
+inline bool shared_tiles(int Dh, int dtype) { return dtype != APPROXIFER_F32 || Dh <= 64 || Dh > 128; }
 // Whether there is an instance of both kernels in one: of heads for which two of its workgroups share a CU.
 inline bool shared_both(int Dh, int dtype, int page_shift) { return (Dh == 64 || (Dh == 128 && dtype != APPROXIFER_F32)) && page_shift >= 4; }
 

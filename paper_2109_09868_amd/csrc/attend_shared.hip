@@ -33,9 +33,26 @@ SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh,
     SharedPlan p{};
     const int64_t group = Hq / Hkv, rows = max_rows * group;
     const bool wide = dtype == APPROXIFER_F32;
-    if (C < 1 || B < 2 * C || max_shared < 1 || rows > 64 || rows < 1 || max_len < 1) return p;
-    p.common_tiles = T * group > (wide ? 64 : 32) * C;
-    p.own_tiles = rows > (wide ? 64 : 16);
+    // Whether it pays.  What is saved is keys that come from a cache where the sequences are read side by side, and rows that are empty in every
+    // sequence's own tiles; what it costs is that two parts of every row at least are written and joined.  Microseconds, attend() -> here, 8
+    // heads of the cache of 128, new tokens times heads of a group = rows:
+    //   bf16, 64 sequences behind 8000 places: rows 32 263 -> 114, 48 270 -> 157, 64 272 -> 246, 128 290 -> 344; behind 2000: 74 -> 52,
+    //   75 -> 67, 77 -> 88, 83 -> 139.
+    //   float32, which waits for products: 64 behind 2000: rows 8 103 -> 71, 12 101 -> 112, 16 101 -> 125, 20 192 -> 167, 24 192 -> 182, 32
+    //   193 -> 237; four groups of them behind 4000: 701 -> 434, 703 -> 622, 706 -> 810, 1386 -> 1046, 1390 -> 1233, 1392 -> 1614.  A quarter of
+    //   the rows of attend()'s tiles of 16 has to be empty.
+    //   bf16, rows 4, 32 groups behind 4000: of 2 sequences 105 -> 115, of 3 151 -> 132, of 4 173 -> 122, of 8 311 -> 154; with heads that are
+    //   no group (12 of 64) of 2 119 -> 78, of 8 254 -> 105.
+    // Behind 512 places there is little to save: 8 groups of 8 18 -> 21, 32 of 8 54 -> 49.
+    if (C < 1 || B < (group > 1 ? 3 : 2) * C || max_shared < 1 || rows < 1 || max_len < 1) return p;
+    if (rows > (wide ? 12 * ((rows + 15) / 16) : 48)) return p;
+    // Which kernel has a group's common places: tiles of 128 rows wait less for keys, tiles of 16 split finer.  Rows of a group, tokens -> tiles,
+    // behind 4000 places: bf16, 8 groups, heads of 128: 16 37 -> 45, 32 46 -> 41, 64 83 -> 55, 256 208 -> 114; 16 groups, 12 heads of 64: 16
+    // 63 -> 62, 24 83 -> 76, 32 93 -> 87, 64 166 -> 132 (one group: 32 15.7 -> 15.9).  float32 behind 2000: 4 groups, 128 rows of 64 147 -> 150,
+    // 512 99 -> 90 (4 heads of the cache), 384 of 96 104 -> 118, 512 of 256 247 -> 211; of 128, behind 4000, 460 -> 652.
+    p.common_tiles = shared_tiles(Dh, dtype) && T * group >= (wide ? 257 : 32) * C;
+    // and its sequences' own ones: bf16, 4 groups of 16, 1024 places: 16 rows 58 -> 70, 32 91 -> 81, 64 144 -> 101; float32 64 341 -> 412
+    p.own_tiles = !wide && rows > 16;
     SharedCall &s = p.call;
     s.C = static_cast<int>(C);
     s.max_shared = static_cast<int>(max_shared);

@@ -54,7 +54,8 @@ inline unsigned shared_blocks(const AttendCall &c, const SharedCall &shared) {
 template <class E, int DP, bool kWhole, bool kSmall>
 struct SharedTiles {
     static hipError_t run(const AttendCall &c, const SharedCall &shared, hipStream_t stream) {
-        return launch_kernel(attend_shared_tiles_kernel<E, DP, kWhole, kSmall>, dim3(shared_blocks(c, shared)), dim3(256), 0, stream, c, shared);
+        if constexpr (sizeof(typename E::Value) == 4 && DP > 64 && DP <= 128) return hipErrorInvalidValue;   // as shared_tiles() says
+        else return launch_kernel(attend_shared_tiles_kernel<E, DP, kWhole, kSmall>, dim3(shared_blocks(c, shared)), dim3(256), 0, stream, c, shared);
     }
 };
 template <class E, int DP, bool kWhole, bool kSmall>

@@ -57,6 +57,13 @@ def _query(c, heads, dim, dtype, seed=7, big=1.0):
     return (big * torch.randn((c["T"], heads, dim), generator=torch.Generator().manual_seed(seed))).to(dtype)
 
 
+def _apart(dtype, B, C, group, new):
+    """Whether reading what is common for itself pays for what joining costs."""
+    rows = group * new
+    few = rows <= (12 * -(-rows // 16) if dtype == torch.float32 else 48)
+    return few and B >= (3 if group > 1 else 2) * C
+
+
 def _check(binding, dtype, groups, shared, own, new, heads, kv, dim, page, window=0, sinks=0, scale=None, big=1.0, apart=False):
     """apart: what is common has to be read for itself: the size of the workspace tells."""
     c = _cache(1, dtype, groups, shared, own, new, kv, dim, page)
@@ -83,7 +90,8 @@ HEADS = [(12, 12, 64, 16), (8, 2, 128, 16), (6, 3, 80, 8), (5, 1, 72, 32), (4, 4
 @pytest.mark.parametrize("dtype", ALL, ids=list(ref.DTYPES))
 @pytest.mark.parametrize("heads,kv,dim,page", HEADS)
 def test_types_and_heads(binding, dtype, heads, kv, dim, page):
-    _check(binding, dtype, [0, 5], [150], [1, 7, 64, 65, 20], [1] * 5, heads, kv, dim, page, apart=True)                 # tokens
+    _check(binding, dtype, [0, 5], [150], [1, 7, 64, 65, 20], [1] * 5, heads, kv, dim, page,
+           apart=_apart(dtype, 5, 1, heads // kv, 1))                                                                    # tokens
     _check(binding, dtype, [0, 3, 7], [130, 67], [3, 7, 4, 33, 1, 2, 9], [1, 2, 1, 0, 1, 2, 1], heads, kv, dim, page)    # mixed
     _check(binding, dtype, [0, 3, 7], [130, 67], [3, 7, 4, 33, 1, 2, 9], [1] * 7, heads, kv, dim, page, window=40, sinks=3)
 
@@ -93,7 +101,7 @@ def test_types_and_heads(binding, dtype, heads, kv, dim, page):
 @pytest.mark.parametrize("B,new", [(2, 1), (9, 1), (40, 1), (6, 5), (3, 16)])
 def test_few_and_many_rows_of_a_group(binding, dtype, kv, group, B, new):
     own = [new + (7 * b) % 41 for b in range(B)]
-    _check(binding, dtype, [0, B], [200], own, [new] * B, kv * group, kv, 64, 16, apart=new * group <= 64)
+    _check(binding, dtype, [0, B], [200], own, [new] * B, kv * group, kv, 64, 16, apart=_apart(dtype, B, 1, group, new))
     _check(binding, dtype, [0, B // 2, B], [33, 90], own, [new - b % 2 if new > 1 else 1 for b in range(B)], kv * group, kv, 128, 16)
 
 
@@ -315,8 +323,28 @@ def test_more_groups_than_a_wave_has_lanes(binding, dtype, heads, kv):
     B = groups[-1] + 3
     own = [3 + b % 5 for b in range(B)]
     assert B >= 2 * 70
-    _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], own, [1] * B, heads, kv, 64, 16, apart=True)
+    _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], own, [1] * B, heads, kv, 64, 16,
+           apart=_apart(dtype, B, 70, heads // kv, 1))
     _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], own, [b % 3 for b in range(B)], 4, 2, 64, 16, window=20, sinks=2)
+
+
+@pytest.mark.parametrize("dtype", ALL, ids=list(ref.DTYPES))
+@pytest.mark.parametrize("heads,kv", [(5, 1), (33, 1)])
+def test_more_groups_of_more_sequences(binding, dtype, heads, kv):
+    sizes = [(3 * c) % 7 + 1 for c in range(70)]
+    groups = [2 + sum(sizes[:c]) for c in range(71)]
+    B = groups[-1] + 3
+    assert _apart(dtype, B, 70, heads // kv, 1)
+    _check(binding, dtype, groups, [5 + (7 * c) % 40 for c in range(70)], [3 + b % 5 for b in range(B)], [1] * B, heads, kv, 64, 16, apart=True)
+
+
+@pytest.mark.parametrize("dtype", ALL, ids=list(ref.DTYPES))
+@pytest.mark.parametrize("dim,page", [(8, 16), (64, 16), (64, 8), (40, 4), (160, 16), (192, 8), (200, 32), (256, 16), (256, 1)])
+def test_rows_of_a_group_that_fill_tiles(binding, dtype, dim, page):
+    # 272 rows, and 281 of sequences of one to three tokens of which a window takes some
+    _check(binding, dtype, [0, 34], [150], [1 + b for b in range(34)], [1] * 34, 8, 1, dim, page, apart=True)
+    new = [1 + b % 3 for b in range(36)]
+    _check(binding, dtype, [1, 36], [150], [b + 3 for b in range(36)], new, 8, 2, dim, page, window=40, sinks=3, apart=True)
 
 
 def test_a_first_group_behind_others_rows(binding):
