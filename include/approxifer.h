@@ -448,7 +448,8 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
  *               attended to as if they shared nothing.
  *   d_workspace as for approxifer_attend(), of approxifer_attend_shared_workspace_bytes(); without one, or with too small a one, and
  *               where sharing would cost more than it gives, the call is approxifer_attend()
- * Where d_groups falls, any row may be unwritten or wrong.  A page that is not in 0 .. P - 1 of the sequence that a group's places are read from
+ * Common places' weights are rounded to the type once where a group has many rows, as those of many rows are in approxifer_attend().
+ * Where d_groups or d_starts falls, any row may be unwritten or wrong.  A page that is not in 0 .. P - 1 of the sequence that a group's places are read from
  * makes the rows of the others that see it NaN too, and their statuses APPROXIFER_SEQUENCE_BAD_PAGE.
  * Others, and what is returned, as approxifer_attend(), with ERR_BAD_SHAPE also for a negative C or max_shared and ERR_LIMIT for a C beyond
  * 2^20; the call consists of up to three launches.

