@@ -235,7 +235,7 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
 
 // Waits for the matrix cores and for the vector units by turns: a score takes one product and then a shift, a power and a sum.  Two prompts of
 // up to 4001 tokens (32 heads of 128 on 8, bf16) 177 to 189 us by card, 555 to 520 TFLOP/s of the scores that are seen, of the call's 383; matrix
-// cores busy 23 %, vector units 45 %.  Registers for three workgroups a CU; two take as long (185).  A wave with 64 keys and
+// cores busy 27 %, vector units 52 %.  Registers for three workgroups a CU; two take as long (185).  A wave with 64 keys and
 // rows of all heads of a group in a tile took 223.
 template <class E, int DP, bool kWhole, bool kAligned>
 __global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 16 ? 1 : MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
