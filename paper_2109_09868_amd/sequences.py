@@ -186,7 +186,8 @@ class SequenceCache:
 
     def fork(self, parents, keep=None):
         """Sequence i continues old sequence parents[i] (-1: empty), all of it or keep[i] tokens: lists or int32 device tensors.
-        Returns refused: a sequence for which there was no page is empty."""
+        Returns refused: a sequence for which there was no page, or whose parent there is not, is empty.  Of a sequence that evict() has
+        cut, a part's next token gets the position that the whole one's would less the tokens left out."""
         import torch
         parents, keep = (x if x is None or isinstance(x, torch.Tensor) else torch.tensor(x, dtype=torch.int32, device=self.device)
                          for x in (parents, keep))
@@ -194,13 +195,12 @@ class SequenceCache:
         if n > self.max_sequences:
             raise ValueError("at most %d sequences" % self.max_sequences)
         new = 1 - self._now
-        old = parents.clamp(min=0).long() if self.dropped is not None or self.mass is not None else None
         binding.approxifer_cache_fork(self.pools, self.table, self.lens, self.refs, parents, keep=keep,
                                       table_out=self._tables[new][:n], lens_out=self._lens[new][:n], refs_out=self._refs[new],
                                       status=self._each["status"][:n], workspace=self._workspace)
         if self.dropped is not None:
-            self.dropped = self.dropped[old] * (parents >= 0)
-        masses = None if self.mass is None else self.mass[old]
+            self.dropped = self._of(self.dropped, parents)
+        masses = None if self.mass is None else self._of(self.mass, parents)
         self._show(new, n)
         if masses is not None:                                # a token's stays with it; places that are no longer held have none
             held = torch.arange(masses.shape[1], device=self.device) < self.lens[:, None]
@@ -208,6 +208,13 @@ class SequenceCache:
         self._common = None
         self.refused.copy_(self.status)
         return self._settle()
+
+    def _of(self, rows, parents):
+        """The rows of the sequences' parents, zeros for those that have none."""
+        if not self.sequences:
+            return rows.new_zeros((parents.numel(),) + rows.shape[1:])
+        none = ((parents < 0) | (parents >= self.sequences)).view((-1,) + (1,) * (rows.dim() - 1))
+        return rows[parents.clamp(0, self.sequences - 1).long()].masked_fill_(none, 0)
 
     def compact(self):
         """Moves live pages together; afterwards pages live[0] and up are free."""

@@ -220,6 +220,27 @@ def test_a_cache_that_does_not_weigh_does_not_evict():
         cache.evict(4)
 
 
+def test_forks_of_sequences_that_are_not_there():
+    import torch
+    from paper_2109_09868_amd import sequences
+    dev = torch.device("cuda:0")
+    cache = sequences.SequenceCache(1, 2, 2, 16, 4, 4, 20, dev, page=PAGE, weigh=True)
+    cache.begin(2)
+    cache.reserve(8)
+    cache.mass[:, :8] = torch.arange(1.0, 17.0, device=dev).view(2, 8)
+    cache.evict(6, 1, 2)
+    assert cache.dropped.tolist() == [2, 2]
+    parents = torch.tensor([1, 2, -1, 0], dtype=torch.int32, device=dev)       # the second is none of the two that there are
+    refused = cache.fork(parents).tolist()
+    assert refused[0] == refused[2] == refused[3] == 0 and refused[1] != 0
+    assert cache.lens.tolist() == [6, 0, 0, 6] and cache.dropped.tolist() == [2, 0, 0, 2]
+    assert cache.mass[:, :6].tolist() == [[9.0, 12.0, 13.0, 14.0, 15.0, 16.0], [0.0] * 6, [0.0] * 6, [1.0, 4.0, 5.0, 6.0, 7.0, 8.0]]
+    assert not cache.mass[:, 6:].any()
+    cache.fork([])
+    cache.fork([-1, -1])
+    assert cache.lens.tolist() == [0, 0] and cache.dropped.tolist() == [0, 0] and not cache.mass.any()
+
+
 @pytest.mark.parametrize("options", [["--share"], ["--keep", "48"]])
 def test_the_command_runs(options):
     import os
