@@ -35,11 +35,25 @@ MassGrid mass_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_ro
 }
 
 constexpr int64_t kAddBlocks = 1 << 20;
+// One CU is slow to bring the scores of many rows, so that short sequences are dealt out to more of them: with fewer blocks of 256
+// keys than this and more rows than 64 a block is of 64 keys.  12 heads of 64, float32, prompts of 34 tokens 28.7 -> 15.7 us the call, of 64
+// 44 -> 18.6, twelve of them 52 -> 26; one token of 48 sequences behind 2000 127 -> 130.
+// Eight waves a block there; of 256 keys and few rows they took 18 for four's 15 us (16 sequences of up to 32768 keys, 32 heads).
+constexpr int64_t kFewScoreBlocks = 512;
 constexpr int kRowsAhead = 4;                                 // of scores that a lane has on their way
 
 // Scores of few rows are kept where they fit into this many bytes; more is formed again.  16 sequences of up to 32768 keys, 32 heads (67 MB of
 // scores): 327 us, formed again 583; 24 of up to 129 17 and 30.
 constexpr int64_t kMostScores = int64_t{1} << 31;
+// Whether that is what is done: for the rows for which attention has its kernel of few rows, and of float32, whose products are dear, for more
+// of them where heads are grouped.  Formed again -> kept, prompts of 34, 129, 300 tokens: 3 heads of 256 on 1, 12 sequences 60 -> 20, 89 -> 45,
+// 141 -> 96 us; 8 heads of 128 on 2 37 -> 16, 54 -> 39, 87 -> 90, 48 sequences 40 -> 25, 115 -> 86, 263 -> 224; 12 heads of 64 on 12, of 64
+// and 129 tokens, 24 -> 26, 46 -> 47.  bf16, 32 heads of 128 on 8, 12 prompts of 34 24 -> 31, of 64 26 -> 48.
+bool keeps_scores(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype) {
+    const int64_t blocks = (max_rows * (Hq / Hkv) + 15) / 16;
+    return few_rows(B, Hq, Hkv, max_rows, dtype) ||
+           (dtype == APPROXIFER_F32 && Hq > Hkv && max_rows <= 256 && B * Hkv * blocks + (B + 3) / 4 < 1 << 24);
+}
 int64_t score_stride(int64_t max_len) { return (max_len + 255) / 256 * 256; }
 int64_t score_bytes(int64_t T, int Hq, int64_t max_len) { return T * Hq * score_stride(max_len) * 4; }
 size_t parts_bytes(const TokenGrid &g, int Dh) {
@@ -77,48 +91,52 @@ __global__ __launch_bounds__(512) void add_slices_kernel(AttendCall c, MassGrid 
     }
 }
 
-// Waits for the scores, which attention has just left: 16 sequences of up to 32768 keys and 32 heads 14 us, 24 of up to 129 and 12 heads 4.
-// 256 keys of a sequence, 4 to a lane; four waves have its rows and heads in turn, and add their sums in order.
-__global__ __launch_bounds__(256) void mass_of_scores_kernel(AttendCall c, float *mass, int64_t mass_stride, int64_t blocks) {
-    __shared__ v4f sums[4][kWave];
+// Waits for the scores, which attention has just left: 16 sequences of up to 32768 keys and 32 heads 15 us, 24 of up to 129 and 12 heads 4.
+// 4 kLanes keys of a sequence, 4 to a lane; the groups of kLanes lanes of kWaves waves have its rows' heads in turn, and add their sums in order.
+template <int kLanes, int kWaves>
+__global__ __launch_bounds__(kWave * kWaves) void mass_of_scores_kernel(AttendCall c, float *mass, int64_t mass_stride, int64_t blocks) {
+    __shared__ v4f sums[kWaves * kWave / kLanes][kLanes];
     const float scale = fabsf(c.scale) * 1.44269504088896340736f;
-    const int lane = lane_id(), wave = wave_id();
+    constexpr int kSets = kWave / kLanes, kAll = kWaves * kSets;
+    const int lane = lane_id() % kLanes, set = kSets == 1 ? __builtin_amdgcn_readfirstlane(wave_id()) : wave_id() * kSets + lane_id() / kLanes;
     const int64_t work = blocks * c.seq.B;
     for (int64_t index = blockIdx.x; index < work; index += gridDim.x) {
-        const int b = static_cast<int>(index % c.seq.B), j = static_cast<int>(index / c.seq.B) * 256 + 4 * lane;
+        const int b = static_cast<int>(index % c.seq.B), j0 = static_cast<int>(index / c.seq.B) * (4 * kLanes), j = j0 + 4 * lane;
         const Rows rows = rows_of(c.seq, b);
-        if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j - 4 * lane >= rows.length) continue;
+        if (!rows.ok || rows.n == 0 || rows.n > c.max_rows || rows.length > c.max_len || j0 >= rows.length) continue;
         const float *const scores = c.scores + rows.start * c.Hq * c.score_stride + j, *const stats = c.stats + 2 * rows.start;
         v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int i = 0; i < rows.n; ++i) {
-            const Visible see(c.window, c.sinks, rows.place(i));
-            bool sees[4];
+        // from the first token that sees one of them to the last; what a row does not see has no scores, but there is memory
+        const int before = rows.length - rows.n, from = max(0, j0 - before) * c.Hq;
+        int to = rows.n;
+        if (c.window > 0 && j0 >= c.sinks)
+            to = static_cast<int>(min(static_cast<int64_t>(to), static_cast<int64_t>(j0) + 4 * kLanes - 1 + c.window - before));
+        const int all = to * c.Hq;
+        for (int r0 = from + set; r0 < all; r0 += kAll * kRowsAhead) {
+            v4f s[kRowsAhead];
+            v2f of_row[kRowsAhead];
+            int tokens[kRowsAhead];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sees[k] = see.sees(j + k);
-            if (!__any(sees[0] || sees[1] || sees[2] || sees[3])) continue;      // what nobody has looked at has no scores
-            for (int h0 = wave; h0 < c.Hq; h0 += 4 * kRowsAhead) {
-                v4f s[kRowsAhead];
-                v2f of_row[kRowsAhead];
+            for (int a = 0; a < kRowsAhead; ++a) {
+                const int row = min(r0 + kAll * a, all - 1), i = rows.n == 1 ? 0 : row / c.Hq, h = row - i * c.Hq;
+                tokens[a] = i;
+                of_row[a] = *reinterpret_cast<const v2f *>(stats + 2 * (h * c.seq.T + i));
+                s[a] = *reinterpret_cast<const v4f *>(scores + row * c.score_stride);
+            }
 #pragma unroll
-                for (int a = 0; a < kRowsAhead; ++a) {
-                    const int h = min(h0 + 4 * a, c.Hq - 1);
-                    const int64_t row = static_cast<int64_t>(i) * c.Hq + h;
-                    of_row[a] = *reinterpret_cast<const v2f *>(stats + 2 * (h * c.seq.T + i));
-                    s[a] = *reinterpret_cast<const v4f *>(scores + (j < c.score_stride ? row * c.score_stride : 0));
+            for (int a = 0; a < kRowsAhead; ++a) {
+                const Visible see(c.window, c.sinks, rows.place(tokens[a]));
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float w = __builtin_amdgcn_exp2f(fmaf(s[a][k], scale, -of_row[a][0])) * of_row[a][1];
+                    sum[k] += see.sees(j + k) && r0 + kAll * a < all ? w : 0.0f;
                 }
-#pragma unroll
-                for (int a = 0; a < kRowsAhead; ++a)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float w = __builtin_amdgcn_exp2f(fmaf(s[a][k], scale, -of_row[a][0])) * of_row[a][1];
-                        sum[k] += sees[k] && h0 + 4 * a < c.Hq ? w : 0.0f;
-                    }
             }
         }
-        sums[wave][lane] = sum;
+        sums[set][lane] = sum;
         __syncthreads();
-        if (wave == 0) {
-            sum = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+        if (set == 0) {
+            for (int w = 1; w < kAll; ++w) sum += sums[w][lane];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 if (j + k < rows.length) mass[b * mass_stride + j + k] += sum[k];
@@ -135,7 +153,7 @@ size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh
                                    int64_t window, int64_t sinks) {
     constexpr size_t kAll = static_cast<size_t>(1) << 60;
     max_rows = max_rows < T ? max_rows : T;
-    if (few_rows(B, Hq, Hkv, max_rows, dtype) && score_bytes(T, Hq, max_len) <= kMostScores)
+    if (keeps_scores(B, Hq, Hkv, max_rows, dtype) && score_bytes(T, Hq, max_len) <= kMostScores)
         return static_cast<size_t>(stats_bytes(T, Hq) + score_bytes(T, Hq, max_len)) +
                parts_bytes(token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll, true), Dh);
     const size_t parts = attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
@@ -151,7 +169,7 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
     c.stats = static_cast<float *>(workspace);
     float *const sums = c.stats + stats / 4;
     const int64_t scores = score_bytes(c.seq.T, c.Hq, c.max_len);
-    if (few_rows(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.dtype) && c.max_rows > 0 && c.max_len > 0 && scores <= kMostScores &&
+    if (keeps_scores(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.dtype) && c.max_rows > 0 && c.max_len > 0 && scores <= kMostScores &&
         static_cast<size_t>(scores) <= room) {
         c.scores = sums;
         c.score_stride = score_stride(c.max_len);
@@ -164,9 +182,10 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
             e = c.dtype == APPROXIFER_F32   ? join_tokens_f32(c, g, parts, stream)
                 : c.dtype == APPROXIFER_F16 ? join_tokens_f16(c, g, parts, stream)
                                             : join_tokens_bf16(c, g, parts, stream);
-        const int64_t blocks = (c.max_len + 255) / 256, work = blocks * c.seq.B;
+        const bool few = (c.max_len + 255) / 256 * c.seq.B < kFewScoreBlocks && c.max_rows * c.Hq > 64;
+        const int64_t blocks = few ? (c.max_len + 63) / 64 : (c.max_len + 255) / 256, work = blocks * c.seq.B;
         if (e == hipSuccess)
-            e = launch_kernel(mass_of_scores_kernel, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(256), 0, stream, c,
+            e = launch_kernel(few ? mass_of_scores_kernel<16, 8> : mass_of_scores_kernel<64, 4>, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(few ? 512 : 256), 0, stream, c,
                               mass, mass_stride, blocks);
         return launch_status(e);
     }
