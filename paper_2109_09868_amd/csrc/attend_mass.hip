@@ -45,14 +45,15 @@ constexpr int kRowsAhead = 4;                                 // of scores that 
 // Scores of few rows are kept where they fit into this many bytes; more is formed again.  16 sequences of up to 32768 keys, 32 heads (67 MB of
 // scores): 327 us, formed again 583; 24 of up to 129 17 and 30.
 constexpr int64_t kMostScores = int64_t{1} << 31;
-// Whether that is what is done: for the rows for which attention has its kernel of few rows, and of float32, whose products are dear, for more
-// of them where heads are grouped.  Formed again -> kept, prompts of 34, 129, 300 tokens: 3 heads of 256 on 1, 12 sequences 60 -> 20, 89 -> 45,
-// 141 -> 96 us; 8 heads of 128 on 2 37 -> 16, 54 -> 39, 87 -> 90, 48 sequences 40 -> 25, 115 -> 86, 263 -> 224; 12 heads of 64 on 12, of 64
-// and 129 tokens, 24 -> 26, 46 -> 47.  bf16, 32 heads of 128 on 8, 12 prompts of 34 24 -> 31, of 64 26 -> 48.
-bool keeps_scores(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype) {
+// Whether that is what is done: for the rows for which attention has its kernel of few rows, and of float32, whose products are dear, for up to
+// 256 tokens of heads of more than 64.  Formed again -> kept, prompts of 88, 129, 300 tokens: 8 heads of 96, two sequences 40 -> 22,
+// 49 -> 30, 58 -> 45 us, 48 of them 70 -> 54, 144 -> 82, 301 -> 209; 8 heads of 128 on 2, 12 sequences of 34, 129, 300 37 -> 16, 54 -> 39, 87 -> 90; 4
+// heads of 256, 12 sequences 67 -> 40, 90 -> 48, 148 -> 123, 48 of them 74 -> 88, 179 -> 138, 375 -> 409; 12 heads of 64, 12 sequences 27 -> 32,
+// 46 -> 46, 80 -> 103.  bf16, 32 heads of 128 on 8, 12 prompts of 34 24 -> 31, of 64 26 -> 48.
+bool keeps_scores(int64_t B, int Hq, int Hkv, int Dh, int64_t max_rows, int dtype) {
     const int64_t blocks = (max_rows * (Hq / Hkv) + 15) / 16;
     return few_rows(B, Hq, Hkv, max_rows, dtype) ||
-           (dtype == APPROXIFER_F32 && Hq > Hkv && max_rows <= 256 && B * Hkv * blocks + (B + 3) / 4 < 1 << 24);
+           (dtype == APPROXIFER_F32 && Dh > 64 && max_rows <= 256 && B * Hkv * blocks + (B + 3) / 4 < 1 << 24);
 }
 int64_t score_stride(int64_t max_len) { return (max_len + 255) / 256 * 256; }
 int64_t score_bytes(int64_t T, int Hq, int64_t max_len) { return T * Hq * score_stride(max_len) * 4; }
@@ -153,7 +154,7 @@ size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh
                                    int64_t window, int64_t sinks) {
     constexpr size_t kAll = static_cast<size_t>(1) << 60;
     max_rows = max_rows < T ? max_rows : T;
-    if (keeps_scores(B, Hq, Hkv, max_rows, dtype) && score_bytes(T, Hq, max_len) <= kMostScores)
+    if (keeps_scores(B, Hq, Hkv, Dh, max_rows, dtype) && score_bytes(T, Hq, max_len) <= kMostScores)
         return static_cast<size_t>(stats_bytes(T, Hq) + score_bytes(T, Hq, max_len)) +
                parts_bytes(token_grid(B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks, kAll, true), Dh);
     const size_t parts = attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
@@ -169,7 +170,7 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
     c.stats = static_cast<float *>(workspace);
     float *const sums = c.stats + stats / 4;
     const int64_t scores = score_bytes(c.seq.T, c.Hq, c.max_len);
-    if (keeps_scores(c.seq.B, c.Hq, c.Hkv, c.max_rows, c.dtype) && c.max_rows > 0 && c.max_len > 0 && scores <= kMostScores &&
+    if (keeps_scores(c.seq.B, c.Hq, c.Hkv, c.Dh, c.max_rows, c.dtype) && c.max_rows > 0 && c.max_len > 0 && scores <= kMostScores &&
         static_cast<size_t>(scores) <= room) {
         c.scores = sums;
         c.score_stride = score_stride(c.max_len);

@@ -210,3 +210,11 @@ def test_nothing_to_do_and_refusals(binding):
             binding.approxifer_attend_mass(q, kp, vp, table, lens, starts, mass, 1, 40, workspace=small)
         assert e.value.code == -12
     assert torch.all(mass == 1.0)
+
+
+@pytest.mark.parametrize("dtype", ALL, ids=list(ref.DTYPES))
+@pytest.mark.parametrize("heads,kv,dim", [(4, 1, 72), (2, 2, 96), (4, 2, 128), (3, 1, 200), (2, 1, 256)])
+def test_prompts_on_either_side_of_what_keeps_its_scores(binding, dtype, heads, kv, dim):
+    _check(binding, dtype, [256, 130, 41], [256, 130, 1], heads, kv, dim, 16)
+    _check(binding, dtype, [400, 256, 3], [200, 17, 3], heads, kv, dim, 8, window=70, sinks=5)
+    _check(binding, dtype, [300, 258, 257], [257, 258, 16], heads, kv, dim, 16)
