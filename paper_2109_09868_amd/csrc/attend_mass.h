@@ -238,8 +238,8 @@ __device__ __forceinline__ void mass_block(const AttendCall &c, const MassGrid &
 // cores busy 27 %, vector units 52 %.  Registers for three workgroups a CU; two take as long (185).  A wave with 64 keys and
 // rows of all heads of a group in a tile took 223.
 template <class E, int DP, bool kWhole, bool kAligned>
-__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 16 ? 1 : MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(AttendCall c, MassGrid g, float *mass,
-                                                                                                  int64_t mass_stride, float *sums) {
+__global__ __launch_bounds__(256, (MassShape<E, DP>::kSteps > 16 ? 1 : MassShape<E, DP>::kSteps > 8 ? 2 : 3)) void attend_mass_kernel(
+    AttendCall c, MassGrid g, float *mass, int64_t mass_stride, float *sums) {
     typedef MassShape<E, DP> S;
     for (int64_t block = blockIdx.z; block < g.blocks; block += gridDim.z)
         for (int b = blockIdx.y; b < c.seq.B; b += gridDim.y)

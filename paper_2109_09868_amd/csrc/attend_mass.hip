@@ -185,9 +185,10 @@ int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *wor
                                             : join_tokens_bf16(c, g, parts, stream);
         const bool few = (c.max_len + 255) / 256 * c.seq.B < kFewScoreBlocks && c.max_rows * c.Hq > 64;
         const int64_t blocks = few ? (c.max_len + 63) / 64 : (c.max_len + 255) / 256, work = blocks * c.seq.B;
+        const dim3 grid(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks));
         if (e == hipSuccess)
-            e = launch_kernel(few ? mass_of_scores_kernel<16, 8> : mass_of_scores_kernel<64, 4>, dim3(static_cast<unsigned>(work < kAddBlocks ? work : kAddBlocks)), dim3(few ? 512 : 256), 0, stream, c,
-                              mass, mass_stride, blocks);
+            e = few ? launch_kernel(mass_of_scores_kernel<16, 8>, grid, dim3(512), 0, stream, c, mass, mass_stride, blocks)
+                    : launch_kernel(mass_of_scores_kernel<64, 4>, grid, dim3(256), 0, stream, c, mass, mass_stride, blocks);
         return launch_status(e);
     }
     const int rc = launch_attend(c, sums, room, stream);

@@ -331,7 +331,8 @@ __device__ __forceinline__ int shared_status(const AttendCall &c, const SharedCa
     return pages_status(c.seq, leader, 0, min(min(c.sinks, upto), first.from), min(first.from, upto), upto);
 }
 
-// 4 us for 24 rows of 12 heads in 5 parts, 13 for 192 of 32 heads of 128 in 10.  A wave joins a row: its parts' sums in their order, eight of them on their way at a time.  The last workgroups: statuses, a wave for each.
+// 4 us for 24 rows of 12 heads in 5 parts, 13 for 192 of 32 heads of 128 in 10.  A wave joins a row: its parts' sums in their order, eight of them on
+// their way at a time.  The last workgroups: statuses, a wave for each.
 template <class E, int DP>
 __global__ __launch_bounds__(256) void attend_shared_join_kernel(AttendCall c, SharedCall shared) {
     typedef typename E::Value V;

@@ -7,7 +7,7 @@
 namespace approxifer {
 
 // Common places by tiles: 8 x 6 blocks of 128 rows on 8003 places take 48 us (192 sequences, 32 heads of 128 on 8, bf16), 524 TFLOP/s: each
-// workgroup has a few tiles of keys, of which one is on its way while another is used, and waits a third of its time for them.
+// workgroup has a few tiles of keys, of which one is on its way while another is used, and waits for them.
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_shared_tiles_kernel(AttendCall c, SharedCall shared) {
     __shared__ __align__(16) char lds[TileShape<E, DP>::kLds];

@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kT) void evict_select_kernel(EvictCall c, EvictSpac
 }
 
 // 5 us for up to 64 sequences, most of it the launch and a chain of three loads: pages that sequences give away decide on others', so that it
-// cannot be part of the launch before it.  One workgroup: free pages, ascending, for the sequences in their order; where one finds too few, those behind it that want any do too.
+// cannot be part of the launch before it.  One workgroup: free pages, ascending, for the sequences in their order; where one finds too few, those
+// behind it that want any do too.
 __global__ __launch_bounds__(kThreads) void evict_pages_kernel(const int32_t *refs, EvictSpace w, int B, int P) {
     __shared__ int sums[16];
     __shared__ long long wide_sums[16];
@@ -243,8 +244,8 @@ constexpr int kLoads = 4;                                     // pieces of 16 by
 constexpr int kNoVmem = 0x0f70;                               // of s_waitcnt: until no load from memory is on its way
 
 // 333 us for 1.6 GB (above).  Which places are read is looked up for the next stretch while this one's four pieces a thread are on their way, and
-// all four are asked for without a branch between them: with both left to their order 1014 us.  The first `rows` workgroups bring the sequences up to date, the others copy: a head of a plane, or `pieces` of each of its rows, at a
-// time.
+// all four are asked for without a branch between them: with both left to their order 1014 us.  The first `rows` workgroups bring
+// the sequences up to date, the others copy: a head of a plane, or `pieces` of each of its rows, at a time.
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictCall c, EvictSpace w, char *pools, int64_t planes, int64_t heads,
                                                          int64_t row_bytes, int pieces, int rows) {
     const int thread = threadIdx.x, after = c.after(), mask = (1 << c.shift) - 1;
