@@ -367,11 +367,11 @@ int launch_cache_evict(int32_t *table, int32_t *lens, int32_t *refs, float *mass
                                           : launch_kernel(evict_select_kernel<kThreads>, dim3(B), dim3(kThreads), 0, stream, c, w);
     if (e == hipSuccess) e = launch_kernel(evict_pages_kernel, dim3(1), dim3(kThreads), 0, stream, refs, w, B, P);
     if (e == hipSuccess) {
-        // rows are cut, never below a sector of 64 bytes, until there is work for every CU
-        int pieces = static_cast<int>(row_bytes / 16);
-        const int64_t whole = planes * heads * B;
-        while (pieces % 2 == 0 && pieces >= 8 && whole * (row_bytes / 16 / pieces) < 1024) pieces /= 2;
-        const int64_t items = whole * (row_bytes / 16 / pieces);
+        // rows are cut, never below a sector of 64 bytes, until there is work for every CU; without pools there may be no piece in a row
+        const int64_t whole = planes * heads * B, row = whole > 0 ? row_bytes / 16 : 1;
+        int pieces = static_cast<int>(row);
+        while (pieces % 2 == 0 && pieces >= 8 && whole * (row / pieces) < 1024) pieces /= 2;
+        const int64_t items = whole * (row / pieces);
         const int rows = B < 1024 ? B : 1024;
         e = launch_kernel(evict_move_kernel, dim3(static_cast<unsigned>(rows + (items < 65536 ? items : 65536))), dim3(256), 0, stream, c, w,
                           static_cast<char *>(pools), planes, heads, row_bytes, pieces, rows);
