@@ -114,9 +114,10 @@ class SequenceCache:
         return self._settle()
 
     def lose(self):
-        """Sequences of whose tokens the last append() or attend() told something else than 0 are refused from now on."""
+        """Sequences of which the last append(), attend() or evict() told something else than 0 are refused from now on, with that status;
+        those that were refused already stay so with what was told first."""
         import torch
-        self.refused.add_(self.status)                        # 0 for those that are refused already: their calls saw no places
+        self.refused.addcmul_(self.status, self.whole)
         torch.eq(self.refused, 0, out=self.whole)
 
     def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
