@@ -166,18 +166,25 @@ class SequenceCache:
                                              window=self.window, sinks=self.sinks, out=out, status=self.status, workspace=workspace)
         return out
 
-    def evict(self, budget, first=0, recent=0):
+    def evict(self, budget, first=0, recent=0, lost=None):
         """Sequences of more than `budget` tokens keep their `first` first and `recent` last ones and, of the others, those that were given
-        the largest weights.  status says what became of each.  Returns the places that stay [sequences, budget] int32, then -1."""
+        the largest weights, but for those where lost (as in reserve()) is not 0: they stay as they are, take no pages, and stay refused.
+        status says what became of each.  Returns the places that stay [sequences, budget] int32, then -1."""
         import torch
         if self.mass is None:
             raise ValueError("a cache that evicts adds up weights: weigh=True")
+        if lost is not None and lost is not self.refused:
+            self.refused.copy_(lost)
+            self._settle()
         before = self.lens.clone()
         n, i32 = self.sequences, torch.int32
+        lens = self.lens if lost is None else self._seen      # 0: nothing to cut
         kept = torch.empty((n, int(budget)), dtype=i32, device=self.device)
         need = binding.approxifer_cache_evict_workspace_bytes(n, budget, self.pages, self.page)
-        binding.approxifer_cache_evict(self.pools, self.table, self.lens, self.refs, self.mass, budget, first=first, recent=recent, kept=kept,
+        binding.approxifer_cache_evict(self.pools, self.table, lens, self.refs, self.mass, budget, first=first, recent=recent, kept=kept,
                                        status=self.status, workspace=torch.empty((max(need, 16),), dtype=torch.uint8, device=self.device))
+        if lost is not None:
+            torch.where(self.whole, lens, before, out=self.lens)
         if self.dropped is None:
             self.dropped = torch.zeros((n,), dtype=i32, device=self.device)
         self.dropped += before - self.lens
@@ -325,8 +332,8 @@ class CodedSequences:
 
     def evict(self, budget, first=0, recent=0):
         """Every worker's sequence of more than `budget` tokens is cut to that many, each by its own weights (SequenceCache.evict()).  A
-        worker for whose sequence there were no pages is lost."""
-        kept = self.cache.evict(budget, first, recent)
+        worker for whose sequence there were no pages is lost; the sequences of those that are lost already stay as they are."""
+        kept = self.cache.evict(budget, first, recent, lost=self.cache.refused)
         self.cache.lose()
         self.cache._settle()
         self.length, self.prompt = min(self.length, budget), 0

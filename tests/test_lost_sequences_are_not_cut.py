@@ -68,6 +68,12 @@ def _told(cache, b, status):
     cache._settle()
 
 
+def _answer(served, device, seed):
+    import torch
+    x = np.random.default_rng(seed).standard_normal((1, K, 1, WIDTH)).astype(np.float32)
+    return served.step(torch.from_numpy(x).to(device), torch.arange(1.0, N + 1.0, device=device).view(1, N))
+
+
 def test_a_second_status_does_not_change_the_first(device):
     # eviction tells of refused sequences too, as append() and attend() do not
     served = _served(device, 10 + 3 + 6)
@@ -80,3 +86,49 @@ def test_a_second_status_does_not_change_the_first(device):
     for expected in (24, 23):
         served.evict(expected)
         assert served.lost.tolist()[0][0] == 2 and max(served.lost.tolist()[0]) == 3
+
+
+def test_a_lost_worker_takes_no_pages(device):
+    served = _served(device, 10 + 3 + 18)
+    cache = served.cache
+    _told(cache, 0, 2)
+    before, masses, table = cache.lens.tolist(), cache.mass[0].clone(), cache.table[0].clone()
+    kept = served.evict(24)
+    assert cache.status.tolist() == [0, 0, 0, 0] and served.lost.tolist() == [[2, 0, 0, 0]]
+    assert cache.lens.tolist() == [before[0], 24, 24, 24] and (cache.table[0] == table).all() and (cache.mass[0] == masses).all()
+    assert (kept[0] == -1).all() and kept[1:].tolist() == [list(range(1, 25))] * 3
+    _, status = _answer(served, device, 6)
+    assert status.tolist() == [0] and served.lost.tolist() == [[2, 0, 0, 0]] and cache.lens.tolist() == [before[0], 25, 25, 25]
+
+
+def test_what_was_told_first_stays(device):
+    served = _served(device, 10 + 3 + 6)
+    cache = served.cache
+    _told(cache, 0, 2)
+    cache.table[0, 3] = -1                                    # as its status says: a page of it is none
+    served.evict(24)
+    assert served.lost.tolist() == [[2, 0, 3, 3]] and cache.lens.tolist() == [PROMPT, 24, PROMPT, PROMPT]
+    for budget in (23, 8):                                    # the cut sequence alone, again
+        served.evict(budget)
+        assert served.lost.tolist() == [[2, 0, 3, 3]] and cache.lens.tolist() == [PROMPT, budget, PROMPT, PROMPT]
+    # statuses of a call that does not pass over them
+    cache.status.copy_(cache.refused)
+    cache.lose()
+    assert served.lost.tolist() == [[2, 0, 3, 3]] and cache.whole.tolist() == [False, True, False, False]
+
+
+def test_a_refused_sequence_is_cut_and_has_room_again(device):
+    from paper_2109_09868_amd import sequences
+    cache = sequences.SequenceCache(1, HEADS, KV, 8, 2, 4, 5, device, page=PAGE, weigh=True)
+    cache.begin(2)
+    assert cache.reserve(8).tolist() == [0, 0] and cache.reserve(8).tolist() == [3, 3]
+    cache.evict(4, 1, 1)
+    assert cache.status.tolist() == [0, 0] and cache.lens.tolist() == [4, 4] and cache.refused.tolist() == [3, 3]
+    assert cache.reserve(4).tolist() == [0, 0] and cache.lens.tolist() == [8, 8]
+    # one of them, as reserve() has it
+    assert cache.reserve(8).tolist() == [3, 3]
+    lost = cache.refused.clone()
+    lost[1] = 0
+    kept = cache.evict(4, 1, 1, lost=lost)
+    assert cache.lens.tolist() == [8, 4] and cache.refused.tolist() == [3, 0] and (kept[0] == -1).all() and (kept[1] >= 0).all()
+    assert cache.whole.tolist() == [False, True] and cache.dropped.tolist() == [4, 8]
