@@ -19,12 +19,20 @@ bool few_rows(int64_t B, int Hq, int Hkv, int64_t max_rows, int dtype) {
 namespace {
 
 // Workgroups that it is given if keys are cut: two on every CU, in one round.  With 256 / 512 / 768 / 1024 / 2048 three sequences of up to
-// 131072 keys take 258 / 244 / 257 / 257 / 255 us.
-constexpr int64_t kTokenGroups = 512;
+// 131072 keys take 258 / 244 / 257 / 257 / 255 us.  Of heads of more than 128 a CU has room for one: one sequence of 40000 keys (2 heads of
+// 256, bf16) 30 us in 256 workgroups, 41 in 314; 12 of 8000 42 in 240, 47 in 504; one of 10000 (8 of 256) 26 and 36 in 320.
+int64_t token_groups(int Dh) { return Dh > 128 ? 256 : 512; }
+// Parts of a row that are worth their writing and joining.  Whole / two: 32 sequences of 4000 keys (8 heads of 128, bf16) 92 / 96 us, 16 of
+// 1000 (12 of 64, 32 bits) 21 / 27, 96 of 2000 (8 of 128, bf16) 134 / 142, one of 512 10 / 12; heads of 256 leave CUs empty: one of 512 keys
+// 20 / 18, of 270 16 / 18.
+bool worth_two(int Dh, int64_t units, int64_t tiles) { return Dh > 128 && 2 * units <= token_groups(Dh) && tiles > 12; }
 // Where that leaves more than a seventh of the places empty, as many as make three rounds, if each still has 24 tiles: 264 heads of sequences
 // of 4000 keys (bf16, 128) 108 us in six parts each and 136 in one, 288 (32 bits, 64) 116 and 144; with 1000 keys 40 us either way, and
 // 384 windows of 1024 keys 44 us whole, 53 in two parts.
 constexpr int64_t kTokenRounds = 3, kTokenChunk = 24;
+// If they have not, and some CUs would have two workgroups and some one, one each: one sequence of 17230 keys (32 heads on 4 of 64, fp16) 12.5 us
+// in 180 workgroups, 13.6 in 272; 11 of 1574 (4 of 128, fp16) 14.2 in 220, 15.8 in 308; 12 of 1000 (12 of 64, 32 bits) 20 in 144, 23 in 432.
+constexpr int64_t kCUs = 256;
 
 }  // namespace
 
@@ -38,15 +46,18 @@ TokenGrid token_grid(int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_
         const int64_t most = (sinks + keys - 1) / keys + (window + 16) / keys + 2;
         tiles = tiles < most ? tiles : most;
     }
-    int64_t parts = kTokenGroups / (pairs * blocks > 0 ? pairs * blocks : 1);
+    const int64_t units = pairs * blocks > 0 ? pairs * blocks : 1, round = ragged ? 512 : token_groups(Dh);
+    int64_t parts = round / units;
     parts = parts < (tiles + 7) / 8 ? parts : (tiles + 7) / 8;           // two tiles a wave at least
-    const int64_t groups = pairs * blocks * (parts > 1 ? parts : 1), places = (groups + kTokenGroups - 1) / kTokenGroups * kTokenGroups;
+    const int64_t groups = units * (parts > 1 ? parts : 1), places = (groups + round - 1) / round * round;
     if (ragged || groups * 7 < places * 6) {
-        int64_t more = (kTokenRounds * kTokenGroups + pairs * blocks - 1) / (pairs * blocks > 0 ? pairs * blocks : 1);
+        int64_t more = (kTokenRounds * round + units - 1) / units;
         more = more < tiles / kTokenChunk ? more : tiles / kTokenChunk;
+        if (!ragged && more <= parts && Dh <= 128 && groups > kCUs) parts = kCUs / units;
         parts = parts > more ? parts : more;
     }
-    const int64_t room = static_cast<int64_t>(workspace_bytes) / (pairs * blocks * part_floats(16, Dh) * 4 + 1);
+    if (parts == 2 && !ragged && !worth_two(Dh, units, tiles)) parts = 1;
+    const int64_t room = static_cast<int64_t>(workspace_bytes / (static_cast<size_t>(units) * part_floats(16, Dh) * 4));
     parts = parts < room ? parts : room;
     TokenGrid g;
     g.pairs = static_cast<int>(pairs);
@@ -93,10 +104,10 @@ TileGrid tile_grid(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int
         const int64_t most = (sinks + 63) / 64 + (window + kTileRows) / 64 + 2;
         tiles = tiles < most ? tiles : most;
     }
-    // half of the tiles that only make up a sequence's number can be empty
-    const int64_t heads = (g.single ? B : T * group / kTileRows + (B + 1) / 2) * Hkv;
+    // as many as there are where all sequences have max_rows tokens; half of the tiles that only make up a sequence's number can be empty
+    const int64_t heads = (T == B * max_rows ? B * ((max_rows * group + kTileRows - 1) / kTileRows) : g.single ? B : T * group / kTileRows + (B + 1) / 2) * Hkv;
     int64_t parts = tile_parts(T * Hq, heads, tiles, Dh, dtype);
-    const int64_t room = static_cast<int64_t>(workspace_bytes) / (g.slots * Hkv * part_floats(kTileRows, Dh) * 4 + 1);
+    const int64_t room = static_cast<int64_t>(workspace_bytes / (static_cast<size_t>(g.slots) * Hkv * part_floats(kTileRows, Dh) * 4));
     parts = parts < room ? parts : room;
     g.parts = static_cast<int>(parts < 2 ? 1 : parts);
     g.chunk = static_cast<int>((tiles + g.parts - 1) / g.parts);

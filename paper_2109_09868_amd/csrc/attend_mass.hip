@@ -58,7 +58,7 @@ bool keeps_scores(int64_t B, int Hq, int Hkv, int Dh, int64_t max_rows, int dtyp
 int64_t score_stride(int64_t max_len) { return (max_len + 255) / 256 * 256; }
 int64_t score_bytes(int64_t T, int Hq, int64_t max_len) { return T * Hq * score_stride(max_len) * 4; }
 size_t parts_bytes(const TokenGrid &g, int Dh) {
-    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(16, Dh) * 4 + 256;
+    return g.parts < 2 ? 0 : static_cast<size_t>(g.pairs) * g.blocks * g.parts * part_floats(16, Dh) * 4;
 }
 
 // 5 us of two prompts' 383.  A block of keys: four threads to each, with a quarter of the slices' sums, and those in their order.
