@@ -11,7 +11,7 @@ namespace approxifer {
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_shared_tiles_kernel(AttendCall c, SharedCall shared) {
     __shared__ __align__(16) char lds[TileShape<E, DP>::kLds];
-    attend_tiles<E, DP, kWhole, kSmall, true>(c, TileGrid{}, nullptr, shared, blockIdx.x, lds);
+    attend_tiles_shared<E, DP, kWhole, kSmall>(c, shared, blockIdx.x, lds);
 }
 
 // Own places, and common ones of few rows.  192 sequences' 33 to 512 own places (8 heads of 128, bf16) 50 us, 4.3 TB/s.  24 sequences behind
@@ -19,7 +19,7 @@ __global__ __launch_bounds__(256, (TileShape<E, DP>::kGroups)) void attend_share
 template <class E, int DP, bool kWhole, bool kSmall>
 __global__ __launch_bounds__(256, (DP > 128 ? 1 : 2)) void attend_shared_tokens_kernel(AttendCall c, SharedCall shared) {
     __shared__ __align__(16) char lds[TokenShape<E, DP>::kLds];
-    attend_tokens<E, DP, kWhole, kSmall, true>(c, TokenGrid{}, nullptr, shared, blockIdx.x, lds);
+    attend_tokens<E, DP, kWhole, kSmall, true, false>(c, TokenGrid{}, nullptr, shared, blockIdx.x, lds);
 }
 
 // Common places by tiles and own ones by tokens in one launch, the tiles first: they are fewer and take longer, and the others go where they
@@ -32,10 +32,10 @@ __global__ __launch_bounds__(256, 2) void attend_shared_both_kernel(AttendCall c
     const int x = blockIdx.x;
     if (x < tiles) {
         shared.own_slots = 0;
-        attend_tiles<E, DP, true, false, true>(c, TileGrid{}, nullptr, shared, x, lds);
+        attend_tiles_shared<E, DP, true, false>(c, shared, x, lds);
     } else {
         shared.common_slots = 0;
-        attend_tokens<E, DP, true, false, true>(c, TokenGrid{}, nullptr, shared, x - tiles, lds);
+        attend_tokens<E, DP, true, false, true, false>(c, TokenGrid{}, nullptr, shared, x - tiles, lds);
     }
 }
 
