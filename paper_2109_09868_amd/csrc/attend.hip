@@ -79,13 +79,14 @@ namespace {
 // them at once as long as the GPU has room; the parts of a row are written and read again at 4.5 bytes a ps, and joined by a launch of
 // about 6 us more.  So sqrt(tiles tile_us / us a part) of them are the least time, if that is less than without any.  Whole / two or three / more
 // parts: 1000 tokens of 32 heads on 8 (bf16, 128) 30 us / 46 in two, 16 tokens of 4 sequences of up to 40000 keys 932 / 106 in sixteen; in 32 bits four
-// prompts of 500 (8 heads of 128) 80 / 60 / 71, one of 1000 (4 heads on one) 49 in four, 35 in eight.
+// prompts of 500 (8 heads of 128) 80 / 60 / 71, one of 1000 (4 heads on one) 49 in four, 35 in eight.  Where every CU has a tile already, 32-bit
+// products gain nothing from a second one: four prompts of 1000 (12 heads of 64) 117 us whole, 138 in two.
 int64_t tile_parts(int64_t rows, int64_t heads, int64_t tiles, int Dh, int dtype) {
     const bool wide = dtype == APPROXIFER_F32;
     const int64_t places = Dh > 128 || (wide && Dh > 64) ? 256 : wide ? 768 : 512;       // workgroups at a time
     int64_t most = places / (heads > 0 ? heads : 1);
     most = most < tiles / 2 ? most : tiles / 2;
-    if (most < 2) return 1;
+    if (most < 2 || (wide && heads > kCUs)) return 1;
     const double tile_us = Dh * (!wide ? 0.0086 : Dh > 64 ? 0.0625 : 0.053);
     const double part_us = static_cast<double>(rows) * Dh * 8.0 / 4.5e6;
     int64_t parts = static_cast<int64_t>(std::sqrt(tiles * tile_us / part_us) + 0.5);
