@@ -447,7 +447,10 @@ size_t approxifer_attend_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, 
  *   max_shared  bound of d_shared.  Sequences of a group that reaches outside 0 .. B, or whose d_shared is not in 0 .. max_shared, are
  *               attended to as if they shared nothing.
  *   d_workspace as for approxifer_attend(), of approxifer_attend_shared_workspace_bytes(); without one, or with too small a one, and
- *               where sharing would cost more than it gives, the call is approxifer_attend()
+ *               where the sequences have so many rows each that reading is not what they wait for, or hardly more than one is in a
+ *               group, the call is approxifer_attend()
+ * How long the common places are does not decide here: behind few of them the call takes longer than approxifer_attend() would.
+ * approxifer_attend_shared_pays() says which one to call.
  * Common places' weights are rounded to the type once where a group has many rows, as those of many rows are in approxifer_attend().
  * Where d_groups or d_starts falls, any row may be unwritten or wrong.  A page that is not in 0 .. P - 1 of the sequence that a group's places are read from
  * makes the rows of the others that see it NaN too, and their statuses APPROXIFER_SEQUENCE_BAD_PAGE.
@@ -461,6 +464,10 @@ int approxifer_attend_shared(const approxifer_sequences *h_seq, int Hq, int Hkv,
                              size_t workspace_bytes, void *stream);
 size_t approxifer_attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows,
                                                 int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks);
+/* 1 where approxifer_attend_shared() is expected to take less time than approxifer_attend(), both with workspaces of the sizes that are
+ * asked for, if about all C groups have max_shared places in common; else 0, also for sizes that the calls refuse.  Host arithmetic only. */
+int approxifer_attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int page, int64_t max_rows,
+                                  int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks);
 
 /*
  * approxifer_attend(), which also adds up the weights that it gives: for every place j of sequence b

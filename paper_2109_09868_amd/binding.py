@@ -53,6 +53,7 @@ EXPORTS = (
     "approxifer_cache_workspace_bytes",
     "approxifer_attend_shared",
     "approxifer_attend_shared_workspace_bytes",
+    "approxifer_attend_shared_pays",
     "approxifer_attend_mass",
     "approxifer_attend_mass_workspace_bytes",
     "approxifer_cache_evict",
@@ -149,6 +150,8 @@ def load() -> ctypes.CDLL:
     lib.approxifer_attend_shared.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, vp, vp, q, q, q, q, q, q, f, vp, vp, z, vp]
     lib.approxifer_attend_shared_workspace_bytes.restype = z
     lib.approxifer_attend_shared_workspace_bytes.argtypes = [q, q, q, i, i, i, i, q, q, q, q, q]
+    lib.approxifer_attend_shared_pays.restype = i
+    lib.approxifer_attend_shared_pays.argtypes = [q, q, q, i, i, i, i, i, q, q, q, q, q]
     lib.approxifer_attend_mass.restype = i
     lib.approxifer_attend_mass.argtypes = [seq, i, i, i, i, vp, q, vp, vp, vp, vp, q, q, q, q, q, f, vp, vp, z, vp]
     lib.approxifer_attend_mass_workspace_bytes.restype = z
@@ -673,6 +676,12 @@ def approxifer_attend_shared_workspace_bytes(T, B, C, Hq, Hkv, Dh, dtype, max_ro
     """Bytes of scratch memory with which approxifer_attend_shared is fastest (0: none); dtype a torch dtype."""
     return int(load().approxifer_attend_shared_workspace_bytes(int(T), int(B), int(C), int(Hq), int(Hkv), int(Dh), _dtype_code(dtype),
                                                                int(max_rows), int(max_len), int(max_shared), int(window), int(sinks)))
+
+
+def approxifer_attend_shared_pays(T, B, C, Hq, Hkv, Dh, dtype, page, max_rows, max_len, max_shared, window=0, sinks=0) -> bool:
+    """Whether approxifer_attend_shared is expected to take less time than approxifer_attend; dtype a torch dtype."""
+    return bool(load().approxifer_attend_shared_pays(int(T), int(B), int(C), int(Hq), int(Hkv), int(Dh), _dtype_code(dtype), int(page),
+                                                     int(max_rows), int(max_len), int(max_shared), int(window), int(sinks)))
 
 
 def approxifer_attend_shared(q, k_pool, v_pool, table, lens, starts, groups, shared, max_rows, max_len, max_shared, window=0, sinks=0,

@@ -130,7 +130,7 @@ int check_pools(const void *d_pools, int64_t planes, int64_t page_bytes, int64_t
 
 extern "C" {
 
-int approxifer_version(void) { return 500; }   // 0.5.0: shared prefixes, attention that adds up its weights, eviction
+int approxifer_version(void) { return 501; }   // 0.5.1: shared prefixes, attention that adds up its weights, eviction
 
 const char *approxifer_strerror(int code) {
     switch (code) {
@@ -408,6 +408,17 @@ size_t approxifer_attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C,
     const int64_t most = APPROXIFER_MAX_TOKENS, length = max_len < most ? max_len : most;
     return approxifer::attend_shared_workspace_bytes(T, B, C, Hq, Hkv, Dh, dtype, max_rows, length, max_shared < length ? max_shared : length,
                                                      window < most ? window : 0, sinks < most ? sinks : most);
+}
+
+int approxifer_attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int page, int64_t max_rows,
+                                  int64_t max_len, int64_t max_shared, int64_t window, int64_t sinks) {
+    int shift = 0;
+    if (!attend_sizes_taken(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks) || C < 1 || C > APPROXIFER_MAX_SEQUENCES ||
+        max_shared < 1 || check_cache(B, 1, 1, page, &shift) != APPROXIFER_OK)
+        return 0;
+    const int64_t most = APPROXIFER_MAX_TOKENS, length = max_len < most ? max_len : most;
+    return approxifer::attend_shared_pays(T, B, C, Hq, Hkv, Dh, dtype, max_rows, length, max_shared < length ? max_shared : length,
+                                          window < most ? window : 0, sinks < most ? sinks : most, shift);
 }
 
 int approxifer_attend_mass(const approxifer_sequences *h_seq, int Hq, int Hkv, int Dh, int dtype, const void *d_q, int64_t q_stride,

@@ -23,10 +23,28 @@ namespace {
 struct SharedPlan {
     SharedCall call;
     bool common_tiles, own_tiles;                             // which kernel has which rows
-    int64_t bytes;                                            // of workspace; 0: not worth it, or not possible
+    int64_t bytes;                                            // of workspace; 0: not worth it for rows as many as these, or not possible
 };
 
 int64_t least(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// Whether what is common is long enough.  attend() reads it at about 4.5 bytes a ps for each sequence; to read it once costs the second launch and
+// the lookups, as many microseconds as `fixed`, and several times the traffic of the parts, which is written by many and read by few.  Fitted to 2600
+// random shapes of 1 to 20 groups of 2 to 100 sequences behind 48 to 20000 places (heads of 64 to 256, 1 to 8 for one of the cache): taken always,
+// time against attend()'s is 0.98 by geometric mean (16-bit) and 0.80 (float32); by this rule 0.82 and 0.75; by who knew it 0.81 and 0.74; 42 of the
+// 980 that it takes are longer by more than 2 %.  8 heads of 128, bf16: 8 groups of 8 behind 512 18.5 -> 21.6, 32 of 8 58.5 -> 51.5, one of 4 behind
+// 4000 15.8 -> 17.2; 8 of 35, two tokens of 32 heads on 8 of 96, behind 336 49 -> 80; 9 of 9 behind 1904 (4 heads of 128) 41 -> 23.
+bool shared_pays(const SharedPlan &p, int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_len, int64_t max_shared,
+                 int64_t window, int64_t sinks, int page_shift) {
+    const bool wide = dtype == APPROXIFER_F32, two = p.common_tiles != p.own_tiles && !(p.common_tiles && shared_both(Dh, dtype, page_shift));
+    // windows reach what is common over what is their own
+    const int64_t own = max_len - max_shared, seen = window > 0 ? least(max_shared, (window > own ? window - own : 0) + sinks) : max_shared;
+    const double saved = static_cast<double>(B - C) * seen * Hkv * Dh * (wide ? 8 : 4) / 4.5e6;
+    const double join = static_cast<double>(T) * Hq * Dh * 8 * (p.call.common_parts + p.call.own_parts) / 4.5e6;
+    if (wide) return saved > 8 + (p.common_tiles ? 10 : 20) * join;
+    if (p.common_tiles && p.own_tiles) return saved > 4 + 2.5 * join;
+    return saved > (two ? 50 + 8 * join : (p.common_tiles ? 15 : 26) + 12 * join);
+}
 
 SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                        int64_t max_shared, int64_t window, size_t workspace_bytes) {
@@ -43,7 +61,6 @@ SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh,
     //   the rows of attend()'s tiles of 16 has to be empty.
     //   bf16, rows 4, 32 groups behind 4000: of 2 sequences 105 -> 115, of 3 151 -> 132, of 4 173 -> 122, of 8 311 -> 154; with heads that are
     //   no group (12 of 64) of 2 119 -> 78, of 8 254 -> 105.
-    // Behind 512 places there is little to save: 8 groups of 8 18 -> 21, 32 of 8 54 -> 49.
     if (C < 1 || B < (group > 1 ? 3 : 2) * C || max_shared < 1 || rows < 1 || max_len < 1) return p;
     if (rows > (wide ? 12 * ((rows + 15) / 16) : 48)) return p;
     // Which kernel has a group's common places: tiles of 128 rows wait less for keys, tiles of 16 split finer.  Rows of a group, tokens -> tiles,
@@ -94,6 +111,12 @@ size_t attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, in
                                      int64_t max_shared, int64_t window, int64_t sinks) {
     const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, static_cast<size_t>(1) << 60);
     return p.bytes > 0 ? static_cast<size_t>(p.bytes) : attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
+}
+
+bool attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                        int64_t max_shared, int64_t window, int64_t sinks, int page_shift) {
+    const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, static_cast<size_t>(1) << 60);
+    return p.bytes > 0 && shared_pays(p, T, B, C, Hq, Hkv, Dh, dtype, max_len, max_shared, window, sinks, page_shift);
 }
 
 int launch_attend_shared(const AttendCall &c, const int32_t *groups, const int32_t *shared, int64_t C, int64_t max_shared, void *workspace,

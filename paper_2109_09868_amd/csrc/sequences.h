@@ -120,6 +120,8 @@ int launch_attend_shared(const AttendCall &c, const int32_t *groups, const int32
                          size_t workspace_bytes, hipStream_t stream);
 size_t attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                                      int64_t max_shared, int64_t window, int64_t sinks);
+bool attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
+                        int64_t max_shared, int64_t window, int64_t sinks, int page_shift);
 int launch_attend_mass(AttendCall c, float *mass, int64_t mass_stride, void *workspace, size_t workspace_bytes, hipStream_t stream);
 size_t attend_mass_least_bytes(int64_t T, int Hq);
 size_t attend_mass_workspace_bytes(int64_t T, int64_t B, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,

@@ -89,7 +89,7 @@ class SequenceCache:
 
     def share(self, groups, lengths):
         """Sequences groups[c] .. groups[c + 1] - 1 have their first lengths[c] tokens in common (lists; until the next begin(), fork() or
-        evict()): attend() then reads those once for all of them."""
+        evict()): attend() then reads those once for all of them where that takes less time."""
         import torch
         self._common = tuple(torch.tensor(x, dtype=torch.int32, device=self.device) for x in (groups, lengths)) + (max(lengths, default=0),)
 
@@ -137,7 +137,7 @@ class SequenceCache:
         """What the new tokens read in their sequences: [T, heads, head_dim]."""
         import torch
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        if self.mass is not None or self._common is not None:
+        if self.mass is not None or (self._common is not None and self._common_pays(q.shape[0], max_rows, max_len)):
             return self._attend_more(layer, q, starts, max_rows, max_len, out)
         need = binding.approxifer_attend_workspace_bytes(q.shape[0], self.sequences, self.heads, self.kv_heads, self.head_dim, self.dtype,
                                                          max_rows, max_len, self.window, self.sinks)
@@ -145,6 +145,11 @@ class SequenceCache:
         binding.approxifer_attend(q, self.pools[layer, 0], self.pools[layer, 1], self.table, self._seen, starts, max_rows, max_len,
                                   window=self.window, sinks=self.sinks, out=out, status=self.status, workspace=workspace)
         return out
+
+    def _common_pays(self, tokens, max_rows, max_len):
+        _, lengths, longest = self._common
+        return binding.approxifer_attend_shared_pays(tokens, self.sequences, lengths.numel(), self.heads, self.kv_heads, self.head_dim,
+                                                     self.dtype, self.page, max_rows, max_len, longest, self.window, self.sinks)
 
     def _attend_more(self, layer, q, starts, max_rows, max_len, out):
         """attend() that adds up its weights, or reads what is common once."""
@@ -277,7 +282,7 @@ class CodedSequences:
     or no place in its table, misses tokens from then on.  Such a worker counts as one that never answers, so a group can
     spare S of them; a group that has lost more gets APPROXIFER_GROUP_BAD_MASK from the decoder, and values of 0.
 
-    share: the prompt is attended to once for all sequences, not once for each (a cache that weighs does not).
+    share: the prompt is attended to once for all sequences, not once for each, where that takes less time (a cache that weighs does not).
     """
 
     def __init__(self, model, cache, G, K, N, S, sign_mode=binding.SIGN_SURVIVOR_RANK, nodes=None, share=False):
