@@ -75,18 +75,19 @@ def test_a_cache_reads_together_what_it_pays_to(monkeypatch, length, window, tak
 
     cache.begin(1)
     cache.reserve(length)
-    cache.append(0, draw(length, heads), draw(length, kv), draw(length, kv), torch.tensor([0, length], dtype=torch.int32, device=dev))
+    k, v = draw(length + B, kv), draw(length + B, kv)
+    cache.append(0, draw(length, heads), k[:length], v[:length], torch.tensor([0, length], dtype=torch.int32, device=dev))
     cache.fork([0] * B)
     cache.share([0, B], [length])
     cache.reserve(1)
     starts = torch.arange(B + 1, dtype=torch.int32, device=dev)
-    q = cache.append(0, draw(B, heads), draw(B, kv), draw(B, kv), starts)
+    q = cache.append(0, draw(B, heads), k[length:], v[length:], starts)
     assert not calls
     together = cache.attend(0, q, starts, 1, length + 1)
     assert calls == ["approxifer_attend_shared" if taken else "approxifer_attend"] and not cache.status.any()
     cache._common = None
     each = cache.attend(0, q, starts, 1, length + 1)
-    # float32 on either side: a score is off by (64 + 8) 2^-24 sum |q k| / 8 at most, twice that and the sums over the keys in the result
-    kp, vp = cache.pools[0, 0], cache.pools[0, 1]
-    off = 2 * 2 * (72 * 2 ** -24 * float(q.abs().amax() * kp.abs().amax()) * 64 / 8 + (length + 65) * 2 ** -24) * float(vp.abs().amax())
+    # float32 on either side: a score is off by (64 + 8) 2^-24 |q| |k| / 8 at most (a rotation keeps lengths), twice that and the sums over the keys
+    # in the result
+    off = 2 * 2 * (72 * 2 ** -24 * float(q.norm(dim=-1).amax() * k.norm(dim=-1).amax()) / 8 + (length + 65) * 2 ** -24) * float(v.abs().amax())
     assert (together - each).abs().max() <= off and off < 0.1 and each.abs().max() > 0.1
