@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(AttendCall c, S
     const int first = shared_length(c.seq, shared, lanes, b) > 0 ? 0 : shared.common_parts, parts = shared.common_parts + shared.own_parts;
     float top = -INFINITY, total = 0.0f, out[kPerLane] = {};
     for (int from = first; from < parts; from += kWave) {
-        const int p = from + lane, count = min(parts - from, kWave);
+        const int p = from + lane;
         const v2f x = p < parts ? *reinterpret_cast<const v2f *>(shared.tops + 2 * (p * all + at)) : v2f{-INFINITY, 0.0f};
         float most = fmaxf(x[0], top);
         for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
@@ -366,12 +366,15 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(AttendCall c, S
         top = most;
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) out[k] *= shrink;
+        // (a part without keys has left neither, nor sums)
+        const unsigned long long there = __ballot(!(x[0] == -INFINITY && x[1] == 0.0f));
+        const int count = there == 0 ? 0 : 64 - __clzll(there);
         for (int i = 0; i < count; i += kAhead) {
             float y[kAhead][kPerLane], w[kAhead];
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
                 const int j = min(i + a, count - 1);
-                w[a] = i + a < count ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j)) : 0.0f;
+                w[a] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), j));
                 const float *const sums = shared.sums(c, from + j, at);
 #pragma unroll
                 for (int k = 0; k < kPerLane; ++k) y[a][k] = lane + k * kWave < c.Dh ? sums[lane + k * kWave] : 0.0f;
@@ -379,7 +382,7 @@ __global__ __launch_bounds__(256) void attend_shared_join_kernel(AttendCall c, S
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
 #pragma unroll
-                for (int k = 0; k < kPerLane; ++k) out[k] += i + a < count ? w[a] * y[a][k] : 0.0f;
+                for (int k = 0; k < kPerLane; ++k) out[k] += there >> (i + a) & 1 ? w[a] * y[a][k] : 0.0f;
         }
     }
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);

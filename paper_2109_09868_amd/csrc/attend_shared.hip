@@ -23,6 +23,7 @@ namespace {
 struct SharedPlan {
     SharedCall call;
     bool common_tiles, own_tiles;                             // which kernel has which rows
+    int joined;                                               // parts of a row of a group
     int64_t bytes;                                            // of workspace; 0: not worth it for rows as many as these, or not possible
 };
 
@@ -40,14 +41,14 @@ bool shared_pays(const SharedPlan &p, int64_t T, int64_t B, int64_t C, int Hq, i
     // windows reach what is common over what is their own
     const int64_t own = max_len - max_shared, seen = window > 0 ? least(max_shared, (window > own ? window - own : 0) + sinks) : max_shared;
     const double saved = static_cast<double>(B - C) * seen * Hkv * Dh * (wide ? 8 : 4) / 4.5e6;
-    const double join = static_cast<double>(T) * Hq * Dh * 8 * (p.call.common_parts + p.call.own_parts) / 4.5e6;
+    const double join = static_cast<double>(T) * Hq * Dh * 8 * p.joined / 4.5e6;
     if (wide) return saved > 8 + (p.common_tiles ? 10 : 20) * join;
     if (p.common_tiles && p.own_tiles) return saved > 4 + 2.5 * join;
     return saved > (two ? 50 + 8 * join : (p.common_tiles ? 15 : 26) + 12 * join);
 }
 
 SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
-                       int64_t max_shared, int64_t window, size_t workspace_bytes) {
+                       int64_t max_shared, int64_t window, int64_t sinks, size_t workspace_bytes) {
     SharedPlan p{};
     const int64_t group = Hq / Hkv, rows = max_rows * group;
     const bool wide = dtype == APPROXIFER_F32;
@@ -89,9 +90,18 @@ SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh,
         *chunk = static_cast<int>(((keys + parts - 1) / parts + 127) / 128 * 128);
         return static_cast<int>((keys + *chunk - 1) / *chunk);
     };
-    const int64_t own_keys = max_len > max_shared ? max_len - max_shared : 1;
+    const int64_t own_keys = max_len > max_shared ? max_len - max_shared : 1, seen = window > 0 ? window + sinks + 64 : max_len;
+    const int64_t own_units = (s.single ? B : T * group / r + (B + 1) / 2) * Hkv;
     s.common_parts = cut(p.common_tiles, (T * group / R + (C + 1) / 2) * Hkv, window > 0 ? least(max_shared, window + 64) : max_shared, &s.common_chunk);
-    s.own_parts = cut(p.own_tiles, (s.single ? B : T * group / r + (B + 1) / 2) * Hkv, own_keys, &s.own_chunk);
+    s.own_parts = cut(p.own_tiles, own_units, least(own_keys, seen), &s.own_chunk);
+    p.joined = s.common_parts + s.own_parts;
+    // Sequences in no group, or in one with less in common, have more of their own: up to two rounds of parts, of 768 keys at least, that others
+    // leave empty.  24 sequences behind 4000 places and one of 8000 places of its own (12 heads of 64, float32) 134
+    // us -> 82; 192 behind 8003 (8 of 128, bf16), where nobody needs them, 117.9 -> 119.2.
+    if (!p.own_tiles) {
+        const int64_t more = least(1024 / own_units, least(max_len, seen) / 768);
+        if (more > s.own_parts) s.own_parts = static_cast<int>(more);
+    }
     const int64_t each = T * Hq * (Dh + 2) * 4;
     const int64_t room = static_cast<int64_t>(workspace_bytes / static_cast<size_t>(each));
     if (room < 2) return p;
@@ -109,13 +119,13 @@ SharedPlan shared_plan(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh,
 
 size_t attend_shared_workspace_bytes(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                                      int64_t max_shared, int64_t window, int64_t sinks) {
-    const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, static_cast<size_t>(1) << 60);
+    const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, sinks, static_cast<size_t>(1) << 60);
     return p.bytes > 0 ? static_cast<size_t>(p.bytes) : attend_workspace_bytes(T, B, Hq, Hkv, Dh, dtype, max_rows, max_len, window, sinks);
 }
 
 bool attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int Hkv, int Dh, int dtype, int64_t max_rows, int64_t max_len,
                         int64_t max_shared, int64_t window, int64_t sinks, int page_shift) {
-    const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, static_cast<size_t>(1) << 60);
+    const SharedPlan p = shared_plan(T, B, C, Hq, Hkv, Dh, dtype, least(max_rows, T), max_len, max_shared, window, sinks, static_cast<size_t>(1) << 60);
     return p.bytes > 0 && shared_pays(p, T, B, C, Hq, Hkv, Dh, dtype, max_len, max_shared, window, sinks, page_shift);
 }
 
@@ -123,7 +133,7 @@ int launch_attend_shared(const AttendCall &c, const int32_t *groups, const int32
                          size_t workspace_bytes, hipStream_t stream) {
     SharedPlan p{};
     if (c.seq.T > 0)
-        p = shared_plan(c.seq.T, c.seq.B, C, c.Hq, c.Hkv, c.Dh, c.dtype, c.max_rows, c.max_len, max_shared, c.window, workspace_bytes);
+        p = shared_plan(c.seq.T, c.seq.B, C, c.Hq, c.Hkv, c.Dh, c.dtype, c.max_rows, c.max_len, max_shared, c.window, c.sinks, workspace_bytes);
     if (p.bytes == 0) return launch_attend(c, workspace, workspace_bytes, stream);
     SharedCall s = p.call;
     s.groups = groups;

@@ -73,6 +73,13 @@
     const int chunk = kShared ? unit.chunk_of<kKeys>(keys.steps) : g.chunk_of<kKeys>(keys.steps);
     const int begin = part * chunk, steps = min(keys.steps, begin + chunk);       // this part's tiles: begin .. steps - 1
     if (!kShared && begin >= steps && part > 0) return;
+    if constexpr (kShared) {
+        if (begin >= steps) {                                 // nothing here: who joins the rows does not look at their sums
+            if (half == 0 && first + wave * 32 + row32 < row_count)
+                shared.settle(c, unit.sum_part, (start + token) * c.Hq + head, -INFINITY, 0.0f);
+            return;
+        }
+    }
     const bool alone = !kShared && keys.steps <= chunk;
     const auto begin_of = [&](int it) { return keys.begin_of(it); };
     const int32_t *table = c.seq.table + static_cast<int64_t>(b) * c.seq.M;

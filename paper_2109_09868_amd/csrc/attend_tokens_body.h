@@ -57,6 +57,14 @@
     const int chunk = kShared ? unit.chunk_of<kKeys>(keys.steps) : g.chunk_of(keys.steps), begin = part * chunk,
               end = min(keys.steps, begin + chunk);
     if (!kShared && begin >= end && part > 0) return;         // the parts that there are end before this one
+    if constexpr (kShared) {
+        if (begin >= end) {                                   // nothing here: who joins the rows does not look at their sums
+            const int64_t at = first + threadIdx.x;
+            if (threadIdx.x < S::kRows && at < row_count)
+                shared.settle(c, unit.sum_part, (start + at / group) * c.Hq + h * group + at % group, -INFINITY, 0.0f);
+            return;
+        }
+    }
     if (threadIdx.x == 0) dirty = 0;
 
     v4i q[S::kSteps];
