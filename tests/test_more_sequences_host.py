@@ -110,3 +110,19 @@ def test_attend_shared_refusals(lib):
         assert need(*args, torch.float16, 1, 100, 50) == 0
     assert need(2, 2, 1, 4, 2, 64, torch.float16, 1, 100, -1) == 0
     assert need(2, 2, 1, 4, 2, 64, torch.float16, 1, 100, 50) % (2 * 4 * 66 * 4) == 0
+
+
+def test_what_attend_shared_asks_for(lib):
+    import torch
+    need, plain = binding.approxifer_attend_shared_workspace_bytes, binding.approxifer_attend_workspace_bytes
+    # shared: the sums, maximum and total of every row in two parts at least
+    for T, B, C, heads, dtype, rows, length, common in ((24, 24, 1, (12, 12, 64), torch.float32, 1, 644, 500), (192, 192, 8, (32, 8, 128), torch.bfloat16, 1, 8500, 8000),
+                                                        (40, 20, 2, (8, 4, 72), torch.float16, 2, 100, 50), (300, 300, 3, (8, 8, 256), torch.float32, 1, 600, 1)):
+        each, got = T * heads[0] * (heads[2] + 2) * 4, need(T, B, C, *heads, dtype, rows, length, common)
+        assert got >= 2 * each and got % each == 0, (T, B, C, heads, got)
+    # not shared: what approxifer_attend() asks for
+    for T, B, C, heads, dtype, rows, length, common in ((2, 2, 1, (4, 2, 64), torch.float16, 1, 100, 50), (16, 16, 8, (32, 8, 128), torch.bfloat16, 1, 9000, 8000),
+                                                        (16 * 64, 16, 1, (32, 8, 128), torch.bfloat16, 64, 9000, 8000), (24, 24, 0, (12, 12, 64), torch.float32, 1, 9000, 8000),
+                                                        (24, 24, 1, (12, 12, 64), torch.float32, 1, 9000, 0), (192, 24, 1, (24, 12, 64), torch.float32, 8, 9000, 8000)):
+        assert need(T, B, C, *heads, dtype, rows, length, common) == plain(T, B, *heads, dtype, rows, length), (T, B, C, heads)
+    assert plain(16, 16, 32, 8, 128, torch.bfloat16, 1, 9000) > 0
