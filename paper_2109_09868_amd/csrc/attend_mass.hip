@@ -46,14 +46,15 @@ constexpr int kRowsAhead = 4;                                 // of scores that 
 // scores): 327 us, formed again 583; 24 of up to 129 17 and 30.
 constexpr int64_t kMostScores = int64_t{1} << 31;
 // Whether that is what is done: for the rows for which attention has its kernel of few rows, and of float32, whose products are dear, for up to
-// 256 tokens of heads of more than 64.  Formed again -> kept, prompts of 88, 129, 300 tokens: 8 heads of 96, two sequences 40 -> 22,
-// 49 -> 30, 58 -> 45 us, 48 of them 70 -> 54, 144 -> 82, 301 -> 209; 8 heads of 128 on 2, 12 sequences of 34, 129, 300 37 -> 16, 54 -> 39, 87 -> 90; 4
-// heads of 256, 12 sequences 67 -> 40, 90 -> 48, 148 -> 123, 48 of them 74 -> 88, 179 -> 138, 375 -> 409; 12 heads of 64, 12 sequences 27 -> 32,
-// 46 -> 46, 80 -> 103.  bf16, 32 heads of 128 on 8, 12 prompts of 34 24 -> 31, of 64 26 -> 48.
+// 256 rows of a sequence and head of the cache, heads of more than 64.  Attention's kernel reads keys again for every 16 rows, and
+// heads of more than 192 leave it one workgroup a CU: there while that is all there are, else up to 16 of them a CU.  Kept against formed again, by
+// geometric mean of 500 random shapes: up to 64 rows 0.63, 65 to 192 0.57, 193 to 256 0.70, 257 to 700 0.89, more 1.16; by this rule 0.66, 2 of the 500
+// longer by more than 2 %.  Microseconds, formed again -> kept: 8 heads of 96, two prompts of 88 40 -> 22; 8 heads of 128 on 2, 12
+// prompts of 34 37 -> 16; 4 heads of 256, 48 prompts of 34 55 -> 45; 16 heads on 4 of 256, 39 prompts of 192 404 -> 649; 96 heads on 12 of 96, one of 172
+// behind 120 78 -> 211; 12 heads of 64, 12 prompts of 88 27 -> 32.  bf16, 32 heads of 128 on 8, 12 prompts of 34 24 -> 31, of 64 26 -> 48.
 bool keeps_scores(int64_t B, int Hq, int Hkv, int Dh, int64_t max_rows, int dtype) {
-    const int64_t blocks = (max_rows * (Hq / Hkv) + 15) / 16;
-    return few_rows(B, Hq, Hkv, max_rows, dtype) ||
-           (dtype == APPROXIFER_F32 && Dh > 64 && max_rows <= 256 && B * Hkv * blocks + (B + 3) / 4 < 1 << 24);
+    const int64_t rows = max_rows * (Hq / Hkv), blocks = B * Hkv * ((rows + 15) / 16);
+    return few_rows(B, Hq, Hkv, max_rows, dtype) || (dtype == APPROXIFER_F32 && Dh > 64 && rows <= 256 && blocks <= (Dh > 192 ? 256 : 4096));
 }
 int64_t score_stride(int64_t max_len) { return (max_len + 255) / 256 * 256; }
 int64_t score_bytes(int64_t T, int Hq, int64_t max_len) { return T * Hq * score_stride(max_len) * 4; }
