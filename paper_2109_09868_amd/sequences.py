@@ -12,6 +12,7 @@ for the caller's hosted model (projections are torch's products, weights are dra
 from __future__ import annotations
 
 import math
+import warnings
 
 import numpy as np
 
@@ -89,8 +90,11 @@ class SequenceCache:
 
     def share(self, groups, lengths):
         """Sequences groups[c] .. groups[c + 1] - 1 have their first lengths[c] tokens in common (lists; until the next begin(), fork() or
-        evict()): attend() then reads those once for all of them where that takes less time."""
+        evict()): attend() then reads those once for all of them where that takes less time.  A cache that weighs does not, and warns.  Of 16
+        bits, weights of common tokens are then rounded once to the type where a group has 32 rows a head of the cache or more, as those of prompts are."""
         import torch
+        if self.mass is not None:
+            warnings.warn("a cache that weighs reads what sequences have in common once for each of them", stacklevel=2)
         self._common = tuple(torch.tensor(x, dtype=torch.int32, device=self.device) for x in (groups, lengths)) + (max(lengths, default=0),)
 
     def reserve(self, add, lost=None):
