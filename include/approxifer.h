@@ -473,12 +473,14 @@ int approxifer_attend_shared_pays(int64_t T, int64_t B, int64_t C, int Hq, int H
  * approxifer_attend(), which also adds up the weights that it gives: for every place j of sequence b
  *     d_mass[b][j] += sum over the rows of b and the Hq query heads of softmax_j(scale q . k_j),
  * the measure by which approxifer_cache_evict() chooses.  Places that no row sees get nothing added; a call for each layer adds the
- * layers up.  Where a row is NaN, so is the mass of all that it sees.
+ * layers up.  Where a row's scores are no numbers (a NaN in its query or in a key that it sees, a score of +infinity, a page that is not in
+ * 0 .. P - 1), so is the mass of all that it sees; what is in the values does not matter.
  *
  *   d_mass      [B][mass_stride] float32; places of a sequence's length and behind it are left as they are.  A sequence longer than
  *               mass_stride is APPROXIFER_SEQUENCE_BAD, as one beyond max_len is.
  *   d_workspace 16-byte aligned, at least 8 T Hq bytes rounded up to 256.  approxifer_attend_mass_workspace_bytes() gives the size with
- *               which the call is fastest; with less its work is split less.
+ *               which the call is fastest; with less its work is split less, or scores are formed twice.  Where few rows' scores are kept it
+ *               is 4 bytes for every row, head and place up to max_len, in all up to 2 GiB: a max_len near the lengths asks for less.
  * Others as approxifer_attend().  Weights and their sums are float32; a key's weights are added in an order that the sizes and the
  * workspace fix, so the same call gives the same bits.
  * Returns what approxifer_attend() does, or ERR_WORKSPACE; ERR_BAD_SHAPE for a negative mass_stride, ERR_ALIGNMENT for a d_mass that is not

@@ -9,7 +9,7 @@
 // that is given back is written while another sequence reads it.
 // Bound by the copies: what is kept of the changed pages is read and written once.  32 sequences of up to 4500 tokens cut to 2048 in six pools
 // (8 heads of 128, bf16; 1.6 GB read and written together) 354 us: selection 15, pages 5, copies 333 at 4.7 TB/s, where a large copy has 5.1.  24 of up
-// to 160 cut to 128 in four pools (12 heads of 64, float32) 28 us: 11, 5 and 13, each a chain of few loads.  64 that share a prompt's pages 97.
+// to 160 cut to 128 in four pools (12 heads of 64, float32) 28 us: 10, 5 and 13, each a chain of few loads.  48 that share a prompt's pages cut to 600 79: 9, 6 and 64.
 #include "page_lists.h"
 
 namespace approxifer {
@@ -195,9 +195,9 @@ __global__ __launch_bounds__(kT) void evict_select_kernel(EvictCall c, EvictSpac
     if (thread == 0) w.plans[b] = plan;
 }
 
-// 5 us for up to 64 sequences, most of it the launch and a chain of three loads: pages that sequences give away decide on others', so that it
-// cannot be part of the launch before it.  One workgroup: free pages, ascending, for the sequences in their order; where one finds too few, those
-// behind it that want any do too.
+// 5 us for up to 64 sequences, most of it the launch and a chain of three loads.  Which pages are free is known when the call begins; a launch of
+// its own, because where a sequence's begin in their list is the sum of what all before it want, which the launch before this one finds.  One workgroup:
+// free pages, ascending, for the sequences in their order; where one finds too few, those behind it that want any do too.
 __global__ __launch_bounds__(kThreads) void evict_pages_kernel(const int32_t *refs, EvictSpace w, int B, int P) {
     __shared__ int sums[16];
     __shared__ long long wide_sums[16];
