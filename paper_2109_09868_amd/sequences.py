@@ -124,13 +124,22 @@ class SequenceCache:
         self.refused.addcmul_(self.status, self.whole)
         torch.eq(self.refused, 0, out=self.whole)
 
-    def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
-        """The new tokens' heads, normed and rotated; keys and values go to their pages.  Returns the queries."""
+    def positions(self, tokens, starts):
+        """Of the new tokens, where evict() has cut sequences (places have closed up, positions go on), else None: their places.  The same for all
+        layers of a step."""
         import torch
-        if positions is None and self.dropped is not None:    # places have closed up, positions go on
-            t = torch.arange(q.shape[0], dtype=torch.int32, device=self.device)
-            b = torch.searchsorted(starts, t, right=True).sub_(1).clamp_(0, self.sequences - 1)
-            positions = (self._seen[b] - starts[b + 1] + t + self.dropped[b]).to(torch.int32)
+        if self.dropped is None:
+            return None
+        t = torch.arange(tokens, dtype=torch.int32, device=self.device)
+        b = torch.searchsorted(starts, t, right=True).sub_(1).clamp_(0, self.sequences - 1)
+        return (self._seen[b] - starts[b + 1] + t + self.dropped[b]).to(torch.int32)
+
+    def append(self, layer, q, k, v, starts, q_weight=None, k_weight=None, positions=None, axis=None):
+        """The new tokens' heads, normed and rotated; keys and values go to their pages.  positions: None for positions() of these tokens.
+        Returns the queries."""
+        import torch
+        if positions is None:
+            positions = self.positions(q.shape[0], starts)
         out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
         binding.approxifer_append(q, k, v, self.pools[layer, 0], self.pools[layer, 1], self.table,
                                   self._seen, starts, self.freq, q_weight=q_weight, k_weight=k_weight, positions=positions, axis=axis,
@@ -263,12 +272,12 @@ class SequenceModel:
 
     def read(self, cache, tokens, starts, max_rows, max_len):
         """tokens [T, width] float32: the new tokens of all sequences, reserved already.  Returns [T, classes]."""
-        x, hd = tokens, self.head_dim
+        x, hd, positions = tokens, self.head_dim, cache.positions(tokens.shape[0], starts)
         for layer in range(self.layers):
             w = self.weights
             rows = (x @ w["qkv"][layer]).view(-1, self.heads + 2 * self.kv_heads, hd)
             q, k, v = rows[:, :self.heads], rows[:, self.heads:self.heads + self.kv_heads], rows[:, self.heads + self.kv_heads:]
-            q = cache.append(layer, q, k, v, starts, w["norm"][layer][0], w["norm"][layer][1])
+            q = cache.append(layer, q, k, v, starts, w["norm"][layer][0], w["norm"][layer][1], positions=positions)
             a = cache.attend(layer, q, starts, max_rows, max_len)
             x = x + a.reshape(-1, self.width) @ w["out"][layer]
         return x @ self.weights["read"]

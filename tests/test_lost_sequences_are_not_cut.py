@@ -132,3 +132,19 @@ def test_a_refused_sequence_is_cut_and_has_room_again(device):
     kept = cache.evict(4, 1, 1, lost=lost)
     assert cache.lens.tolist() == [8, 4] and cache.refused.tolist() == [3, 0] and (kept[0] == -1).all() and (kept[1] >= 0).all()
     assert cache.whole.tolist() == [False, True] and cache.dropped.tolist() == [4, 8]
+
+
+def test_positions_are_looked_up_once_a_step(device, monkeypatch):
+    import torch
+    served = _served(device, 10 + 3 + 24)
+    cache, asked, f = served.cache, [], torch.searchsorted
+    monkeypatch.setattr(torch, "searchsorted", lambda *a, **k: (asked.append(a[1].numel()), f(*a, **k))[1])
+    _answer(served, device, 6)
+    assert asked == []                                        # nothing has been cut: positions are places
+    served.evict(24)
+    _answer(served, device, 7)
+    assert asked == [N] and served.lost.tolist() == [[0] * N]
+    # two tokens of one, none of another: behind the 40 that each has had
+    starts = torch.tensor([0, 2, 2, 3, 4], dtype=torch.int32, device=device)
+    cache.reserve(torch.tensor([2, 0, 1, 1], dtype=torch.int32, device=device))
+    assert cache.positions(4, starts).tolist() == [40, 41, 40, 40]
